@@ -307,6 +307,133 @@ int flashmask_mfma_ceiling(const void* operands, float* sink, int workgroups, in
 int flashmask_atomic_ceiling(float* acc, int heads, int n_tiles, int tiles, int workgroups, double* bytes,
                               void* hip_stream);
 
+/*
+ * --- Around the attention call: rotary positions, a paged key-value cache, attention of new tokens over it ---------
+ *
+ * The conventions at the top of this file hold here too (device pointers, streams, no allocation, no synchronisation,
+ * graph capture), with these differences: several element types, sequences of their own lengths, and index values (pages,
+ * sequences, positions) that live on the device.  An index value out of its range is never followed: what each entry
+ * point does then is said at it.
+ */
+
+/* Element types. */
+enum {
+  FM_TYPE_BF16 = 0,
+  FM_TYPE_F16 = 1,
+  FM_TYPE_F32 = 2,  /* flashmask_rope alone */
+  FM_TYPE_E4M3 = 3  /* caches alone: 8 bits, sign, 4 exponent and 3 mantissa bits, largest value 448, no infinities */
+};
+
+/* Which elements of a head's first `rot` ones are turned together: i and i + rot / 2, or 2 i and 2 i + 1. */
+enum { FM_ROPE_HALF = 0, FM_ROPE_INTERLEAVED = 1 };
+
+/*
+ * Rotary positions.  Pair i < rot / 2 of a row at position p is turned by the angle p * freqs[i]:
+ *     a' = amp (a cos - b sin),   b' = amp (b cos + a sin),
+ * elements from `rot` on are copied.  Scaled frequencies and `amp` are how contexts are stretched.  Angles, sines and
+ * cosines are computed in 64 bits, the products in 32, with one rounding to the type at the end.
+ *   q, q_out       [B,H,N,d], k, k_out [B,H_kv,N,d], of `type` (BF16, F16, F32); strides[4] describe q, k, q_out, k_out in
+ *                  elements (multiples of 16 bytes; see flashmask_strides).  An output may be its own input (same strides).
+ *   freqs          double [rot / 2]
+ *   positions      int32 [B,N], any values; NULL: 0 .. N - 1 in every batch row
+ *   rot            a multiple of 16, 0 < rot <= d; d is 64 or 128
+ * flashmask_rope_bwd takes the gradients of q_out and k_out to those of q and k: the turn by the opposite angle.
+ */
+int flashmask_rope(const void* q, const void* k, void* q_out, void* k_out, const double* freqs, const int32_t* positions,
+                   int type, int layout, double amp, int B, int H, int H_kv, int N, int d, int rot,
+                   const flashmask_strides* strides, void* hip_stream);
+int flashmask_rope_bwd(const void* dq_out, const void* dk_out, void* dq, void* dk, const double* freqs,
+                       const int32_t* positions, int type, int layout, double amp, int B, int H, int H_kv, int N, int d,
+                       int rot, const flashmask_strides* strides, void* hip_stream);
+
+/*
+ * A paged key-value cache.  Token j of sequence b lies in page table[b][j / page], slot j % page; the page's entry for
+ * head h starts h * head elements further on, the slot's token * row.  Table values outside [0, num_pages) stand for
+ * "no page" (-1 by custom).
+ */
+typedef struct {
+  void* k;                  /* pages of `type`, 16-byte aligned; strides in elements, multiples of 16 bytes: .batch from page */
+  void* v;                  /* to page, .head from head to head, .row from token to token (>= d, < 2^24); d contiguous */
+  flashmask_strides sk, sv;
+  const float* k_scale;     /* float [heads], both or neither; a cached value stands for value * scale[head]. */
+  const float* v_scale;     /* required for E4M3, NULL otherwise */
+  const int32_t* table;     /* int32 [sequences, columns] */
+  int32_t type;             /* FM_TYPE_BF16, FM_TYPE_F16 or FM_TYPE_E4M3 */
+  int32_t heads, d;         /* K/V heads; 64 or 128 */
+  int32_t num_pages, page;  /* pages; tokens of a page, a multiple of 16 */
+  int32_t sequences, columns;
+} flashmask_cache;
+
+/*
+ * Writes `tokens` new tokens to the cache, their keys rotated (flashmask_rope), and rotates their queries.
+ *   q, q_out    [tokens, H, d], k, v [tokens, heads, d] of `type` (BF16, F16; that of the cache, or the cache is E4M3);
+ *               strides[4] describe q, k, v, q_out (.row from token to token, .batch unused).  q may be NULL (no queries).
+ *   seqs        int32 [tokens]: the token's sequence; outside [0, sequences) it is padding and writes nothing
+ *   positions   int32 [tokens]: its position, which is its place in the sequence and its angle.  Where the sequence's row has no
+ *               page at that place nothing is written.
+ *   freqs, layout, amp, rot   as for flashmask_rope; freqs == NULL: nothing is rotated (q must be NULL)
+ * Keys go from the 32-bit result of the rotation to the cache's type in one rounding; an E4M3 cache takes value / scale,
+ * held to +-448.  Two tokens of one call must not have the same place.
+ */
+int flashmask_cache_append(const flashmask_cache* cache, const void* q, const void* k, const void* v, void* q_out,
+                           const int32_t* seqs, const int32_t* positions, const double* freqs, int type, int layout,
+                           double amp, int tokens, int H, int rot, const flashmask_strides* strides, void* hip_stream);
+
+/*
+ * Attention of the last T tokens of every sequence over the cache, which holds lens[b] tokens of it, the new ones among them:
+ * query t is row i = lens[b] - T + t and sees key j iff
+ *     j <= i,   j > i - window (window > 0),   and neither LTS[j] <= i < LTE[j] nor UTS[j] <= i < UTE[j].
+ * out = softmax(scale * q K^T) V and lse as for flashmask_fwd; a row that sees nothing (a sequence shorter than T, an
+ * empty one) gets 0 and -inf.  Keys that a row does not see have no influence on it, whatever they and their values hold.
+ *   q, out      [sequences, H, T, d] of `type` (BF16, F16; that of the cache, or the cache is E4M3), strides sq, so; H is a
+ *               multiple of cache->heads, query head h reads K/V head h / (H / heads)
+ *   lens        int32 [sequences], values below 0 count as 0.  A key whose place has no page is not seen.
+ *   lts..ute    int32 [sequences, bound_columns], all or none (NULL); keys from bound_columns on have no interval
+ *   window      0: none; else the row and window - 1 keys before it
+ *   lse         float [sequences, H, T]
+ *   workspace   at least flashmask_decode_workspace_bytes(), 256-byte aligned
+ * Long sequences are split over workgroups and joined by a second launch; how follows from lens on the device.  The same
+ * call gives the same bits every time.
+ */
+int flashmask_decode(const flashmask_cache* cache, const void* q, const int32_t* lens, const int32_t* lts,
+                     const int32_t* lte, const int32_t* uts, const int32_t* ute, int bound_columns, int window, float scale,
+                     void* out, float* lse, int type, int H, int T, const flashmask_strides* sq,
+                     const flashmask_strides* so, void* workspace, size_t workspace_bytes, void* hip_stream);
+/* Bytes of scratch of a call on `sequences` sequences, 0 for an invalid shape.  Host-only. */
+size_t flashmask_decode_workspace_bytes(int sequences, int H, int H_kv, int T, int d);
+
+/*
+ * Forks sequences: child r goes on from sequence parents[r], sharing its full pages.
+ *   table_out   int32 [children, columns]: the parent's row.  A child with a page of its own (new_pages[r] >= 0) keeps the full
+ *               pages lens / page; of a last page that is partly filled it gets a copy, in new_pages[r], in every pool.  Without one
+ *               (-1) it goes on in the parent's last page.
+ *   lens_out    int32 [children]: the parent's length
+ *   pools       HOST array of num_pools device pointers, each to num_pages pages of page_bytes contiguous bytes (a
+ *               multiple of 16): all layers' keys and values
+ * A parent outside [0, sequences) gives an empty child; no page is copied from or to a place outside the pools.  The pages of
+ * new_pages must differ from each other and from those in use; table_out, lens_out must not overlap table, lens.
+ */
+int flashmask_cache_fork(void* const* pools, int num_pools, size_t page_bytes, int num_pages, const int32_t* table,
+                         const int32_t* lens, const int32_t* parents, const int32_t* new_pages, int32_t* table_out,
+                         int32_t* lens_out, int sequences, int columns, int page, int children, void* hip_stream);
+
+/*
+ * The pages that no entry of the table names, in ascending order, -1 behind them, and their number.
+ *   free_pages  int32 [num_pages], count int32 [1];  workspace: flashmask_cache_plan_bytes(num_pages)
+ */
+int flashmask_cache_free_list(const int32_t* table, int entries, int num_pages, int32_t* free_pages, int32_t* count,
+                              void* workspace, size_t workspace_bytes, void* hip_stream);
+/*
+ * Moves the used pages to the front: with `used` pages named by the table, the used pages from there on go, in ascending
+ * order, to the unused ones before it, in every pool; the table's entries follow.
+ *   table_out   int32 [entries] (values outside [0, num_pages) stay as they are), used int32 [1]; neither overlaps table
+ */
+int flashmask_cache_compact(void* const* pools, int num_pools, size_t page_bytes, int num_pages, const int32_t* table,
+                            int entries, int32_t* table_out, int32_t* used, void* workspace, size_t workspace_bytes,
+                            void* hip_stream);
+/* Bytes of scratch of the two calls above, 0 for an invalid number.  Host-only. */
+size_t flashmask_cache_plan_bytes(int num_pages);
+
 #ifdef __cplusplus
 }
 #endif

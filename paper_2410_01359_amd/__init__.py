@@ -7,3 +7,8 @@ from .binding import (  # noqa: F401
     flashmask_preprocess, flashmask_setup_launches, flashmask_tile_shape, flashmask_unit_queues, flashmask_work_cut, flashmask_workspace_bytes,
     library_path, load_library,
 )
+from .serving import (  # noqa: F401
+    FM_ROPE_HALF, FM_ROPE_INTERLEAVED, flashmask_cache_append, flashmask_cache_compact, flashmask_cache_fork,
+    flashmask_cache_free_list, flashmask_cache_plan_bytes, flashmask_decode, flashmask_decode_workspace_bytes,
+    flashmask_rope, flashmask_rope_bwd,
+)

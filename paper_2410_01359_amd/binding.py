@@ -77,6 +77,24 @@ def load_library() -> ctypes.CDLL:
     lib.flashmask_atomic_ceiling.argtypes = [fp, i, i, i, i, ctypes.POINTER(ctypes.c_double), vp]
     lib.flashmask_profile_events.restype = i
     lib.flashmask_profile_events.argtypes = [ctypes.POINTER(ctypes.c_void_p), i]
+    dp, db = ctypes.c_void_p, ctypes.c_double
+    for name in ("flashmask_rope", "flashmask_rope_bwd"):
+        getattr(lib, name).restype = i
+        getattr(lib, name).argtypes = [vp, vp, vp, vp, dp, ip, i, i, db, i, i, i, i, i, i, vp, vp]
+    lib.flashmask_cache_append.restype = i
+    lib.flashmask_cache_append.argtypes = [vp, vp, vp, vp, vp, ip, ip, dp, i, i, db, i, i, i, vp, vp]
+    lib.flashmask_decode.restype = i
+    lib.flashmask_decode.argtypes = [vp, vp, ip, ip, ip, ip, ip, i, i, f, vp, fp, i, i, i, vp, vp, vp, sz, vp]
+    lib.flashmask_decode_workspace_bytes.restype = sz
+    lib.flashmask_decode_workspace_bytes.argtypes = [i, i, i, i, i]
+    lib.flashmask_cache_fork.restype = i
+    lib.flashmask_cache_fork.argtypes = [vp, i, sz, i, ip, ip, ip, ip, ip, ip, i, i, i, i, vp]
+    lib.flashmask_cache_free_list.restype = i
+    lib.flashmask_cache_free_list.argtypes = [ip, i, i, ip, ip, vp, sz, vp]
+    lib.flashmask_cache_compact.restype = i
+    lib.flashmask_cache_compact.argtypes = [vp, i, sz, i, ip, i, ip, ip, vp, sz, vp]
+    lib.flashmask_cache_plan_bytes.restype = sz
+    lib.flashmask_cache_plan_bytes.argtypes = [i]
     _LIB = lib
     return lib
 

@@ -7,6 +7,7 @@
 
 #include "../../include/flashmask.h"
 #include "fm_kernels.h"
+#include "fm_serving.h"
 
 namespace {
 
@@ -107,6 +108,8 @@ FmUnits dkdv_units(int B, int H, int Hk, int N, int d, int cus) {
 }
 
 }  // namespace
+
+int fm_hip_error(hipError_t e) { return hip_fail(e); }
 
 extern "C" {
 

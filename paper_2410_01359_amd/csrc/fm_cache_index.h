@@ -1,0 +1,72 @@
+// Where tokens lie in the paged cache, which keys a sequence's rows can see, and how those are cut into chunks.  Index values
+// come from the caller's device memory: nothing here follows one out of its range.  Plain integer code: the host compiles it too.
+#pragma once
+#include "fm_direct_order.h"
+
+// Keys are counted in groups of 16: pages hold whole groups.
+constexpr int FM_KEY_GROUP = 16;
+// Keys that a split sequence's chunk has at least.
+constexpr int FM_MIN_CHUNK = 512;
+
+// The page that a table entry names, -1: none.
+FM_HOST_DEVICE inline int fm_known_page(int entry, int num_pages) { return entry >= 0 && entry < num_pages ? entry : -1; }
+
+// Place of a token: column of its sequence's row and slot in the page; column = -1 where the table has none.
+struct FmPlace {
+  int column, slot;
+};
+FM_HOST_DEVICE inline FmPlace fm_place(int position, const FmDivisor& page, int columns) {
+  if (position < 0) return FmPlace{-1, 0};
+  const int column = fm_div(position, page);
+  return FmPlace{column < columns ? column : -1, position - column * (int)page.n};
+}
+
+// Keys of a sequence of `len` tokens that any of its last T rows can see, bounds apart: [lo, hi) with lo a multiple of
+// FM_KEY_GROUP and hi within the table; len is held to 0 from below.
+struct FmKeyRange {
+  int len, lo, hi;
+};
+FM_HOST_DEVICE inline FmKeyRange fm_key_range(int len, int T, int window, int table_keys) {
+  FmKeyRange r;
+  r.len = len > 0 ? len : 0;
+  r.hi = r.len < table_keys ? r.len : table_keys;
+  r.lo = 0;
+  if (window > 0) {
+    const long long first = (long long)r.len - T + 1 - window;   // of the first row
+    if (first > 0) r.lo = (int)(first / FM_KEY_GROUP * FM_KEY_GROUP);
+  }
+  if (r.lo >= r.hi) r.lo = r.hi = 0;
+  return r;
+}
+FM_HOST_DEVICE inline int fm_key_groups(const FmKeyRange& r) { return (r.hi - r.lo + FM_KEY_GROUP - 1) / FM_KEY_GROUP; }
+
+// Groups of a chunk where sequences of `total` groups together are meant to be cut into `chunks`: a multiple of `round`.
+FM_HOST_DEVICE inline int fm_chunk_groups(unsigned total, int chunks, int round) {
+  unsigned size = (total + chunks - 1) / chunks;
+  if (size < FM_MIN_CHUNK / FM_KEY_GROUP) size = FM_MIN_CHUNK / FM_KEY_GROUP;
+  return (int)((size + round - 1) / round * round);
+}
+// Chunks of a sequence: at least one, so that somebody writes an empty sequence's rows.
+FM_HOST_DEVICE inline int fm_chunks_of(int groups, int size) { return groups > size ? (groups + size - 1) / size : 1; }
+// Chunks of all sequences together and partial results that they leave, at most: a sequence of several chunks has fewer than
+// twice its groups / size, and any has fewer than that and one.
+FM_HOST_DEVICE inline int fm_most_units(int chunks, int sequences) { return chunks + sequences; }
+FM_HOST_DEVICE inline int fm_most_slots(int chunks, int sequences) { return chunks < sequences ? 2 * chunks : chunks + sequences; }
+
+// Row of a fork's child: what its column c holds.  `entry`: the parent's, -1 without a known parent.
+struct FmFork {
+  int last;      // column of the last page
+  bool partly;   // it is neither full nor empty
+};
+FM_HOST_DEVICE inline FmFork fm_fork(int len, const FmDivisor& page) {
+  FmFork f = {0, false};
+  if (len > 0) {
+    f.last = fm_div(len, page);
+    f.partly = len != f.last * (int)page.n;
+  }
+  return f;
+}
+FM_HOST_DEVICE inline int fm_fork_entry(const FmFork& f, int c, int entry, int fresh) {
+  if (fresh < 0 || c < f.last) return entry;
+  return c == f.last && f.partly ? fresh : -1;
+}

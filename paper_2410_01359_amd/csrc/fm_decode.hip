@@ -1,0 +1,640 @@
+// Attention of the last tokens of every sequence over a paged cache (flashmask_decode).
+//
+// The H / Hk * T query rows that share a K/V head are the columns of both products: with 16-row groups of keys
+//     S^T = K Q^T   (16 keys x 16 queries: a lane has keys 4 g + r of query c, g = lane / 16, c = lane % 16)
+//     O^T = V^T P^T (16 elements of d x 16 queries, contraction over 32 keys)
+// by the 16x16x32 matrix instruction.  Softmax statistics are per column, so rescaling and the final division stay in the lane.
+// Keys and values go straight from memory to the operands, without LDS:
+//  - K: lane (g, c) loads 16 bytes of key c; which elements of d a product takes together is free, as long as Q has them in the
+//    same order.
+//  - V: lane (g, c) loads the same piece of d (D / 16 elements, piece c) of the eight keys whose probabilities it holds of its
+//    column, and the eight 16-bit values of each element are gathered by byte permutes: product e has as its rows the
+//    elements D / 16 * m + e, m = 0..15.  The lane's results are then 4 * D / 16 consecutive elements of its query's row.
+// The probabilities go into the second product as sums of two 16-bit values, which the matrix pipe has room for: the loop is bound by memory (each wave keeps 16 KiB of keys and values in flight).
+#include <algorithm>
+
+#include "fm_common.h"
+#include "fm_serving.h"
+
+namespace fm {
+
+typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
+typedef __attribute__((ext_vector_type(2))) _Float16 f16x2;
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+
+constexpr int kGroup = FM_KEY_GROUP;
+constexpr int kWaves = 4;
+
+template <bool F16>
+__device__ __forceinline__ f32x4 mfma_keys(u32x4 a, u32x4 b, f32x4 c) {
+  if constexpr (F16) return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+  else return mfma16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c);
+}
+// Two floats to 16 bits each.
+template <bool F16>
+__device__ __forceinline__ unsigned pack2(float a, float b) {
+  if constexpr (F16) return __builtin_bit_cast(unsigned, f16x2{(_Float16)a, (_Float16)b});
+  else return __builtin_bit_cast(unsigned, bf16x2{(__bf16)a, (__bf16)b});
+}
+// Probabilities enter their product as sums hi + lo of two 16-bit values: cut off and what that left, 16 bits of the
+// value for bf16, 22 for f16.  Neither is negative, and lo is never 0 where the probability is not, so that an infinite value
+// a row sees comes out as itself and not as 0 * inf.  f16 ends at 2^-24: probabilities are taken times 2^kShift there.
+template <bool F16>
+constexpr float kShift = F16 ? 14.f : 0.f;
+template <bool F16>
+constexpr float kUnshift = F16 ? 0x1p-14f : 1.f;
+template <bool F16>
+__device__ __forceinline__ void split2(float a, float b, unsigned& hi, unsigned& lo) {
+  if constexpr (F16) {
+    constexpr float kLeast = 0x1p-24f;
+    const auto h = __builtin_amdgcn_cvt_pkrtz(a, b);
+    hi = __builtin_bit_cast(unsigned, h);
+    lo = pack2<true>(fmaxf(a - (float)h[0], fminf(a, kLeast)), fmaxf(b - (float)h[1], fminf(b, kLeast)));
+  } else {
+    const unsigned x = __builtin_bit_cast(unsigned, a) | 1u, y = __builtin_bit_cast(unsigned, b) | 1u;
+    hi = __builtin_amdgcn_perm(y, x, 0x07060302u);
+    lo = pack2<false>(__builtin_bit_cast(float, x) - __builtin_bit_cast(float, x & 0xffff0000u),
+                      __builtin_bit_cast(float, y) - __builtin_bit_cast(float, y & 0xffff0000u));
+  }
+}
+// Four e4m3 values to 16 bits each (exact in both types).
+template <bool F16>
+__device__ __forceinline__ u32x2 widen4(unsigned x) {
+  if constexpr (F16)
+    return u32x2{__builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)x, 1.f, false)),
+                 __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)x, 1.f, true))};
+  else
+    return u32x2{__builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)x, 1.f, false)),
+                 __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)x, 1.f, true))};
+}
+// The low or the high halves of two words.
+__device__ __forceinline__ unsigned pair_of(unsigned first, unsigned second, int high) {
+  return __builtin_amdgcn_perm(second, first, high ? 0x07060302u : 0x05040100u);
+}
+template <int CTRL>
+__device__ __forceinline__ unsigned dpp_or(unsigned x) {
+  return x | (unsigned)__builtin_amdgcn_update_dpp((int)x, (int)x, CTRL, 0xf, 0xf, false);
+}
+// Bits set in any of the 16 lanes of a DPP row.
+__device__ __forceinline__ unsigned row16_or(unsigned x) { return dpp_or<0x121>(dpp_or<0x122>(dpp_or<0x124>(dpp_or<0x128>(x)))); }
+// Whether one of the two 16-bit values is infinite or NaN.
+template <bool F16>
+__device__ __forceinline__ bool odd_pair(unsigned x) {
+  constexpr unsigned kExp = F16 ? 0x7c00u : 0x7f80u;
+  return (x & kExp) == kExp || (x >> 16 & kExp) == kExp;
+}
+// Maximum over the four lanes l, l ^ 16, l ^ 32, l ^ 48.
+__device__ __forceinline__ float quad_max(float x) {
+  auto r = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(int, x), __builtin_bit_cast(int, x), false, false);
+  x = fmaxf(__builtin_bit_cast(float, (int)r[0]), __builtin_bit_cast(float, (int)r[1]));
+  r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(int, x), __builtin_bit_cast(int, x), false, false);
+  return fmaxf(__builtin_bit_cast(float, (int)r[0]), __builtin_bit_cast(float, (int)r[1]));
+}
+// Exponents are taken against this: a row that has seen nothing has no maximum.
+__device__ __forceinline__ float reference(float m) { return m == -INFINITY ? 0.f : m; }
+
+__device__ __forceinline__ FmKeyRange key_range(const FmDecodeArgs& a, int b) {
+  return fm_key_range(a.lens[b], a.T, a.window, a.columns * a.page_tokens);
+}
+
+// Whether row i sees key j, as far as the bounds tell.
+__device__ __forceinline__ bool bounds_hide(const FmDecodeArgs& a, int b, int j, int i) {
+  if (j >= a.bound_columns) return false;
+  const size_t at = (size_t)b * a.bound_columns + j;
+  return (a.bounds[0][at] <= i && i < a.bounds[1][at]) || (a.bounds[2][at] <= i && i < a.bounds[3][at]);
+}
+
+template <int D, bool F16, bool E4M3, int NB>
+struct Decode {
+  static constexpr int BYTES = E4M3 ? 1 : 2;
+  // keys of a wave's step: 16 KiB of K and V, fewer where the scores of NB query blocks would not fit the registers
+  static constexpr int KT = std::min(16384 / (64 * D * BYTES), std::max(8 / NB, 1)), GROUPS = 2 * KT, KEYS = 32 * KT;
+  static constexpr int KSTEPS = D / 32;             // products of S^T
+  static constexpr int KLOADS = D * BYTES / 64;     // 16-byte loads of a lane per group of keys
+  static constexpr int E = D / 16;                  // products of O^T; elements of d in a lane's piece of a value row
+  static constexpr int VWORDS = E * BYTES / 4;      // words of that piece
+  static constexpr int ROWS = 16 * NB;              // query rows
+  static constexpr int LIST = 128;                  // steps listed at a time where bounds hide keys
+  typedef __attribute__((ext_vector_type(VWORDS))) unsigned vpiece;
+  struct Shared {
+    union {
+      struct {
+        int list[LIST], flag[LIST], count;
+      };
+      float out[kWaves][16][D + 4];
+    };
+    float2 stat[kWaves][16];
+  };
+};
+
+template <int D, bool F16, bool E4M3, int NB>
+__global__ __launch_bounds__(64 * kWaves, NB == 1 ? 2 : 1) void decode_kernel(FmDecodeArgs a, int row_blocks, FmDivisor inner,
+                                                                            FmDivisor heads, FmDivisor tokens) {
+  using C = Decode<D, F16, E4M3, NB>;
+  __shared__ typename C::Shared sh;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int g = lane >> 4, c = lane & 15;
+  // Workgroup -> chunk of a sequence, K/V head, block of query rows.  Workgroup x runs on XCD x % 8: all heads of a chunk on one,
+  // one behind the other, because they share page table entries, bounds, and cache lines where heads lie next to each other.
+  const int slot_of_xcd = blockIdx.x >> 3;
+  const int turn = fm_div(slot_of_xcd, inner), member = slot_of_xcd - turn * (int)inner.n;
+  const int unit = turn * 8 + (blockIdx.x & 7);
+  const int rb = fm_div(member, heads), hk = member - rb * (int)heads.n;
+
+  // Chunk: all sequences' keys together are cut into a.chunks pieces, each sequence into whole ones of that size.
+  int b = 0, chunk = 0, chunks = 1, slot = 0, size = INT32_MAX / 32;   // size: in groups
+  if (a.plan) {
+    unsigned total = 0;
+    for (int base = 0; base < a.B; base += 64) {
+      int n = base + lane < a.B ? fm_key_groups(key_range(a, base + lane)) : 0;
+#pragma unroll
+      for (int k = 1; k < 64; k *= 2) n += __shfl_xor(n, k);
+      total += n;
+    }
+    size = fm_chunk_groups(total, a.chunks, kWaves * C::GROUPS);
+    int units = 0, slots = 0;
+    b = -1;
+    for (int base = 0; base < a.B; base += 64) {
+      int n = 0;
+      if (base + lane < a.B) n = fm_chunks_of(fm_key_groups(key_range(a, base + lane)), size);
+      int upto = n, upto_slots = n > 1 ? n : 0;
+#pragma unroll
+      for (int k = 1; k < 64; k *= 2) {
+        const int o = __shfl_up(upto, k), os = __shfl_up(upto_slots, k);
+        if (lane >= k) {
+          upto += o;
+          upto_slots += os;
+        }
+      }
+      const unsigned long long behind = __ballot(n > 0 && units + upto > unit);
+      if (behind) {
+        const int at = __builtin_ctzll(behind);
+        b = base + at;
+        chunks = __shfl(n, at);
+        chunk = unit - (units + __shfl(upto, at) - chunks);
+        slot = slots + __shfl(upto_slots, at) - (chunks > 1 ? chunks : 0);
+        break;
+      }
+      units += __shfl(upto, 63);
+      slots += __shfl(upto_slots, 63);
+    }
+    b = __builtin_amdgcn_readfirstlane(b);
+    if (b < 0) return;
+    chunks = __builtin_amdgcn_readfirstlane(chunks);
+    chunk = __builtin_amdgcn_readfirstlane(chunk);
+    slot = __builtin_amdgcn_readfirstlane(slot);
+    if (chunk == 0 && member == 0 && threadIdx.x == 0) a.plan[b] = int2{slot, chunks};
+  } else {
+    b = unit;
+    if (b >= a.B) return;
+  }
+  const FmKeyRange range = key_range(a, b);
+  const int j_begin = range.lo + chunk * size * kGroup;
+  const int j_end = (int)std::min<long long>(range.hi, j_begin + (long long)size * kGroup);
+  const int first_row = range.len - a.T;   // row of query 0
+
+  // Queries
+  const int G = a.H / a.Hk, R = G * a.T;
+  u32x4 q[NB][C::KSTEPS];
+  int row_token[NB];   // query t of the lane's column, -1: none
+#pragma unroll
+  for (int nb = 0; nb < NB; ++nb) {
+    const int r = rb * C::ROWS + nb * 16 + c;
+    row_token[nb] = -1;
+#pragma unroll
+    for (int s = 0; s < C::KSTEPS; ++s) q[nb][s] = u32x4{0, 0, 0, 0};
+    if (r < R) {
+      const int hq = fm_div(r, tokens), t = r - hq * a.T;
+      row_token[nb] = t;
+      const char* p = (const char*)a.q + 2 * ((long long)b * a.sq.b + (long long)(hk * G + hq) * a.sq.h + (long long)t * a.sq.n);
+#pragma unroll
+      for (int s = 0; s < C::KSTEPS; ++s)
+        q[nb][s] = ldg16(p + 2 * (E4M3 ? 64 * (s / 2) + 16 * g + 8 * (s % 2) : 32 * s + 8 * g));
+    }
+  }
+  const float scale = a.scale * kLog2e * (E4M3 ? a.k_scale[hk] : 1.f);
+
+  // Where the lane's pieces of a group of keys lie
+  const char* k_head = a.k.base + (long long)hk * a.k.head;
+  const char* v_head = a.v.base + (long long)hk * a.v.head;
+  const unsigned k_lane = c * a.k.token + 16 * g, v_lane = 4 * g * a.v.token + c * (C::E * C::BYTES);
+  const int* row = a.table + (size_t)b * a.columns;
+
+  // The pages of a step's groups: -1 where there is none, or no key
+  struct Step {
+    int page[C::GROUPS], slot[C::GROUPS];
+  };
+  const auto pages_of = [&](int start) {
+    Step p;
+#pragma unroll
+    for (int i = 0; i < C::GROUPS; ++i) {
+      const int key = start + i * kGroup;
+      const bool there = key < j_end;
+      const int at = there ? key : j_begin;
+      const int column = fm_div(at, a.page);
+      const int page = fm_known_page(__builtin_amdgcn_readfirstlane(row[column]), a.num_pages);
+      p.slot[i] = at - column * (int)a.page.n;
+      p.page[i] = there ? page : -1;
+    }
+    return p;
+  };
+  u32x4 kraw[C::GROUPS][C::KLOADS];
+  typename C::vpiece vraw[C::KT][8];
+  const auto load_k = [&](const Step& p) {
+#pragma unroll
+    for (int i = 0; i < C::GROUPS; ++i) {
+      const char* base = k_head + std::max(p.page[i], 0) * a.k.page + (unsigned)p.slot[i] * (unsigned long long)a.k.token;
+#pragma unroll
+      for (int s = 0; s < C::KLOADS; ++s) kraw[i][s] = ldg16(base + k_lane + 64 * s);
+    }
+  };
+  const auto load_v = [&](const Step& p) {
+#pragma unroll
+    for (int i = 0; i < C::GROUPS; ++i) {
+      const char* base = v_head + std::max(p.page[i], 0) * a.v.page + (unsigned)p.slot[i] * (unsigned long long)a.v.token;
+#pragma unroll
+      for (int t = 0; t < 4; ++t) vraw[i / 2][i % 2 * 4 + t] = *(const typename C::vpiece*)(base + t * a.v.token + v_lane);
+    }
+  };
+
+  // Which of the lane's keys (bit 4 i + r: key 4 g + r of group i) row `row_i` sees
+  const auto seen_keys = [&](int start, unsigned pages_there, int row_i) {
+    unsigned seen = 0;
+#pragma unroll 1
+    for (int bit = 0; bit < 4 * C::GROUPS; ++bit) {
+      const int j = start + bit / 4 * kGroup + 4 * g + bit % 4;
+      const bool sees = (pages_there >> (bit / 4) & 1) && j < j_end && j <= row_i && (a.window <= 0 || j > row_i - a.window) &&
+                        !(a.bounds[0] && bounds_hide(a, b, j, row_i));
+      seen |= (sees ? 1u : 0u) << bit;
+    }
+    return seen;
+  };
+
+  float m[NB], l[NB];
+  f32x4 acc[NB][C::E];
+#pragma unroll
+  for (int nb = 0; nb < NB; ++nb) {
+    m[nb] = -INFINITY;
+    l[nb] = 0.f;
+#pragma unroll
+    for (int e = 0; e < C::E; ++e) acc[nb][e] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+
+  for (int panel = j_begin; panel < j_end; panel += a.bounds[0] ? C::LIST * C::KEYS : INT32_MAX / 2) {
+    int steps;
+    if (a.bounds[0]) {
+      // the steps of which some row sees a key, and whether it takes the element mask
+      const int end = min(j_end, panel + C::LIST * C::KEYS), all = (end - panel + C::KEYS - 1) / C::KEYS;
+      for (int i = threadIdx.x; i < all; i += 64 * kWaves) sh.flag[i] = 0;
+      __syncthreads();
+      for (int j = panel + threadIdx.x; j < end; j += 64 * kWaves) {
+        int flag = 0;
+        for (int t = 0; t < a.T; ++t) {
+          const int i = first_row + t;
+          flag |= j <= i && (a.window <= 0 || j > i - a.window) && !bounds_hide(a, b, j, i) ? 1 : 2;
+        }
+        atomicOr(&sh.flag[(j - panel) / C::KEYS], flag);
+      }
+      __syncthreads();
+      if (wave == 0) {
+        int count = 0;
+        for (int base = 0; base < all; base += 64) {
+          const int flag = base + lane < all ? sh.flag[base + lane] : 0;
+          const unsigned long long live = __ballot(flag & 1);
+          if (flag & 1) sh.list[count + __popcll(live & ((1ull << lane) - 1ull))] = (base + lane) * 4 + flag;
+          count += __popcll(live);
+        }
+        if (lane == 0) sh.count = count;
+      }
+      __syncthreads();
+      steps = sh.count;
+    } else {
+      steps = (j_end - panel + C::KEYS - 1) / C::KEYS;
+    }
+    const auto entry_of = [&](int s) { return a.bounds[0] ? __builtin_amdgcn_readfirstlane(sh.list[s]) : s * 4; };
+
+    if (wave < steps) {
+      int entry = entry_of(wave);
+      Step now = pages_of(panel + entry / 4 * C::KEYS);
+      load_k(now);
+      load_v(now);
+      int next_entry = wave + kWaves < steps ? entry_of(wave + kWaves) : entry;
+      Step next = pages_of(panel + next_entry / 4 * C::KEYS);
+      for (int s = wave; s < steps; s += kWaves) {
+        const bool more = s + kWaves < steps;
+        const int start = panel + entry / 4 * C::KEYS;
+        bool masked = (entry & 2) || start + C::KEYS > j_end || start + C::KEYS - 1 > first_row ||
+                      (a.window > 0 && start <= range.len - 1 - a.window);
+#pragma unroll
+        for (int i = 0; i < C::GROUPS; ++i) masked |= now.page[i] < 0;
+
+        // scores
+        f32x4 p[NB][C::GROUPS];
+#pragma unroll
+        for (int i = 0; i < C::GROUPS; ++i) {
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb) p[nb][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int k = 0; k < C::KSTEPS; ++k) {
+            u32x4 op;
+            if constexpr (E4M3) {
+              const u32x4 raw = kraw[i][k / 2];
+              const u32x2 x = widen4<F16>(raw[k % 2 * 2]), y = widen4<F16>(raw[k % 2 * 2 + 1]);
+              op = u32x4{x[0], x[1], y[0], y[1]};
+            } else {
+              op = kraw[i][k];
+            }
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) p[nb][i] = mfma_keys<F16>(op, q[nb][k], p[nb][i]);
+          }
+        }
+        if (more) load_k(next);
+
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+          for (int i = 0; i < C::GROUPS; ++i) p[nb][i] *= scale;
+
+        // element mask; values that no row sees become 0 (the keys of a lane's scores are those of its value pieces).  Which of its
+        // keys a column sees is gathered as bits by a loop: unrolled, the bounds' addresses alone would fill the registers.
+        bool mixed = false;   // some row sees a key that another one does not
+        unsigned pages_there = 0;
+        if (masked) {
+#pragma unroll
+          for (int i = 0; i < C::GROUPS; ++i) pages_there |= (now.page[i] >= 0 ? 1u : 0u) << i;
+          unsigned any = 0, every = ~0u;
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb) {
+            const bool real = row_token[nb] >= 0;
+            const unsigned seen = real ? seen_keys(start, pages_there, first_row + row_token[nb]) : 0u;
+            any |= row16_or(seen);
+            every &= ~row16_or(real ? ~seen : 0u);
+#pragma unroll
+            for (int i = 0; i < C::GROUPS; ++i)
+#pragma unroll
+              for (int r = 0; r < 4; ++r)
+                if (!(seen >> (4 * i + r) & 1)) p[nb][i][r] = -INFINITY;
+          }
+          mixed = __any((any & ~every) != 0);
+#pragma unroll
+          for (int i = 0; i < C::GROUPS; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+              if (!(any >> (4 * i + r) & 1)) vraw[i / 2][i % 2 * 4 + r] = (typename C::vpiece)(0u);
+        }
+
+        // softmax
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+          float top = p[nb][0][0];
+#pragma unroll
+          for (int i = 0; i < C::GROUPS; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) top = fmaxf(top, p[nb][i][r]);
+          top = fmaxf(quad_max(top), m[nb]);
+          const float ref = reference(top), alpha = fast_exp2(m[nb] - ref);
+          m[nb] = top;
+          float sum = 0.f;
+#pragma unroll
+          for (int i = 0; i < C::GROUPS; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              p[nb][i][r] = fast_exp2(p[nb][i][r] - (ref - kShift<F16>));
+              sum += p[nb][i][r];
+            }
+          l[nb] = l[nb] * alpha + sum;
+#pragma unroll
+          for (int e = 0; e < C::E; ++e) acc[nb][e] *= alpha;
+        }
+
+        // products with the values
+#pragma unroll
+        for (int kt = 0; kt < C::KT; ++kt) {
+          u32x4 hi[NB], lo[NB];
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+              unsigned h, o;
+              split2<F16>(p[nb][2 * kt + w / 2][2 * (w % 2)], p[nb][2 * kt + w / 2][2 * (w % 2) + 1], h, o);
+              hi[nb][w] = h;
+              lo[nb][w] = o;
+            }
+          unsigned v[8][C::E / 2];
+#pragma unroll
+          for (int t = 0; t < 8; ++t) {
+            if constexpr (E4M3) {
+#pragma unroll
+              for (int w = 0; w < C::VWORDS; ++w) {
+                const u32x2 x = widen4<F16>(vraw[kt][t][w]);
+                v[t][2 * w] = x[0];
+                v[t][2 * w + 1] = x[1];
+              }
+            } else {
+#pragma unroll
+              for (int w = 0; w < C::VWORDS; ++w) v[t][w] = vraw[kt][t][w];
+            }
+          }
+          bool odd = false;
+          if (mixed) {
+#pragma unroll
+            for (int t = 0; t < 8; ++t)
+#pragma unroll
+              for (int w = 0; w < C::E / 2; ++w) odd |= odd_pair<F16>(v[t][w]);
+            odd = __any(odd);
+          }
+          if (odd) {
+            // an infinity or NaN among values that not every row sees: row by row, the others' values left out
+#pragma unroll 1
+            for (int t = 0; t < a.T; ++t) {
+              const unsigned seen = seen_keys(start, pages_there, first_row + t) >> (8 * kt);
+#pragma unroll
+              for (int e = 0; e < C::E; ++e) {
+                u32x4 op;
+#pragma unroll
+                for (int w = 0; w < 4; ++w)
+                  op[w] = pair_of(seen >> (2 * w) & 1 ? v[2 * w][e / 2] : 0u, seen >> (2 * w + 1) & 1 ? v[2 * w + 1][e / 2] : 0u, e % 2);
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) {
+                  f32x4 x = mfma_keys<F16>(op, lo[nb], f32x4{0.f, 0.f, 0.f, 0.f});
+                  x = mfma_keys<F16>(op, hi[nb], x);
+                  if (row_token[nb] == t) acc[nb][e] += x;
+                }
+              }
+            }
+          } else {
+#pragma unroll
+            for (int e = 0; e < C::E; ++e) {
+              u32x4 op;
+#pragma unroll
+              for (int w = 0; w < 4; ++w) op[w] = pair_of(v[2 * w][e / 2], v[2 * w + 1][e / 2], e % 2);
+#pragma unroll
+              for (int nb = 0; nb < NB; ++nb) {
+                acc[nb][e] = mfma_keys<F16>(op, lo[nb], acc[nb][e]);
+                acc[nb][e] = mfma_keys<F16>(op, hi[nb], acc[nb][e]);
+              }
+            }
+          }
+        }
+        if (more) load_v(next);
+        entry = next_entry;
+        now = next;
+        next_entry = s + 2 * kWaves < steps ? entry_of(s + 2 * kWaves) : entry;
+        next = pages_of(panel + next_entry / 4 * C::KEYS);
+      }
+    }
+    if (a.bounds[0]) __syncthreads();
+  }
+
+  // The waves' sums meet in LDS, 16 rows at a time
+  __syncthreads();
+  constexpr int PER = 16 * D / (64 * kWaves);   // elements of a thread: neighbours of one row
+  const int my_row = threadIdx.x * PER / D, my_col = threadIdx.x * PER % D;
+  const float v_scale = E4M3 ? a.v_scale[hk] : 1.f;
+#pragma unroll
+  for (int nb = 0; nb < NB; ++nb) {
+    if (rb * C::ROWS + nb * 16 >= R) break;
+    const float sum = quad_sum(l[nb]);
+    if (g == 0) sh.stat[wave][c] = float2{m[nb], sum};
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+      for (int e = 0; e < C::E; e += 4)
+        *(f32x4*)&sh.out[wave][c][4 * C::E * g + C::E * r + e] =
+            f32x4{acc[nb][e][r], acc[nb][e + 1][r], acc[nb][e + 2][r], acc[nb][e + 3][r]};
+    __syncthreads();
+    float top = -INFINITY, total = 0.f, weight[kWaves], x[PER];
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) top = fmaxf(top, sh.stat[w][my_row].x);
+#pragma unroll
+    for (int e = 0; e < PER; ++e) x[e] = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      weight[w] = fast_exp2(sh.stat[w][my_row].x - reference(top));
+      total += weight[w] * sh.stat[w][my_row].y;
+#pragma unroll
+      for (int e = 0; e < PER; ++e) x[e] += weight[w] * sh.out[w][my_row][my_col + e];
+    }
+    const int r = rb * C::ROWS + nb * 16 + my_row;
+    if (r < R) {
+      if (chunks > 1) {
+        const size_t at = ((size_t)(slot + chunk) * a.Hk + hk) * R + r;
+#pragma unroll
+        for (int e = 0; e < PER; e += 4) *(f32x4*)(a.part + at * D + my_col + e) = f32x4{x[e], x[e + 1], x[e + 2], x[e + 3]};
+        if (my_col == 0) a.stat[at] = float2{top, total};
+      } else {
+        const int hq = fm_div(r, tokens), t = r - hq * a.T, h = hk * G + hq;
+        const float factor = total == 0.f ? 0.f : v_scale / total;
+        char* o = (char*)a.out + 2 * ((long long)b * a.so.b + (long long)h * a.so.h + (long long)t * a.so.n + my_col);
+#pragma unroll
+        for (int e = 0; e < PER; e += 2) *(unsigned*)(o + 2 * e) = pack2<F16>(x[e] * factor, x[e + 1] * factor);
+        if (my_col == 0) a.lse[((size_t)b * a.H + h) * a.T + t] = total == 0.f ? -INFINITY : (top + fast_log2(total * kUnshift<F16>)) * kLn2;
+      }
+    }
+    __syncthreads();
+  }
+}
+
+// Joins the chunks of a row of a split sequence.  D / 4 lanes take a chunk's sums of p v, the workgroup 1024 / D chunks at a time.
+template <int D, bool F16>
+__global__ __launch_bounds__(256) void join_kernel(FmDecodeArgs a, FmDivisor rows, FmDivisor tokens) {
+  constexpr int LANES = D / 4, TEAMS = 256 / LANES, BATCH = 4;
+  const int G = a.H / a.Hk, R = G * a.T;
+  const int sh_row = fm_div(blockIdx.x, rows), r = blockIdx.x - sh_row * R;   // (sequence, K/V head), row of it
+  const int b = blockIdx.y, hk = sh_row;
+  const int2 plan = a.plan[b];
+  if (plan.y <= 1) return;
+  const int team = threadIdx.x / LANES, lane = threadIdx.x % LANES;
+  float m = -INFINITY, l = 0.f;
+  f32x4 x = {0.f, 0.f, 0.f, 0.f};
+  for (int base = team; base < plan.y; base += TEAMS * BATCH) {
+    f32x4 v[BATCH];
+    float2 s[BATCH];
+#pragma unroll
+    for (int i = 0; i < BATCH; ++i) {
+      const int c = base + i * TEAMS;
+      s[i] = float2{-INFINITY, 0.f};
+      v[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+      if (c < plan.y) {
+        const size_t at = ((size_t)(plan.x + c) * a.Hk + hk) * R + r;
+        s[i] = a.stat[at];
+        v[i] = *(const f32x4*)(a.part + at * D + 4 * lane);
+      }
+    }
+    float top = m;
+#pragma unroll
+    for (int i = 0; i < BATCH; ++i) top = fmaxf(top, s[i].x);
+    const float alpha = fast_exp2(m - reference(top));
+    m = top;
+    l *= alpha;
+    x *= alpha;
+#pragma unroll
+    for (int i = 0; i < BATCH; ++i) {
+      const float w = fast_exp2(s[i].x - reference(top));
+      l += w * s[i].y;
+      x += w * v[i];
+    }
+  }
+  __shared__ f32x4 sums[TEAMS][LANES];
+  __shared__ float2 stats[TEAMS];
+  sums[team][lane] = x;
+  if (lane == 0) stats[team] = float2{m, l};
+  __syncthreads();
+  if (team > 0) return;
+  float top = -INFINITY, total = 0.f;
+#pragma unroll
+  for (int w = 0; w < TEAMS; ++w) top = fmaxf(top, stats[w].x);
+  x = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int w = 0; w < TEAMS; ++w) {
+    const float weight = fast_exp2(stats[w].x - reference(top));
+    total += weight * stats[w].y;
+    x += weight * sums[w][lane];
+  }
+  const int hq = fm_div(r, tokens), t = r - hq * a.T, h = hk * G + hq;
+  const float factor = total == 0.f ? 0.f : (a.v_scale ? a.v_scale[hk] : 1.f) / total;
+  char* o = (char*)a.out + 2 * ((long long)b * a.so.b + (long long)h * a.so.h + (long long)t * a.so.n + 4 * lane);
+  *(u32x2*)o = u32x2{pack2<F16>(x[0] * factor, x[1] * factor), pack2<F16>(x[2] * factor, x[3] * factor)};
+  if (lane == 0) a.lse[((size_t)b * a.H + h) * a.T + t] = total == 0.f ? -INFINITY : (top + fast_log2(total * kUnshift<F16>)) * kLn2;
+}
+
+template <int D, bool F16, bool E4M3>
+static void launch(const FmDecodeArgs& a, hipStream_t stream) {
+  const FmDecodeCut cut = fm_decode_cut(a.H, a.Hk, a.T, D, a.B, fm_compute_units());
+  const int units = a.plan ? fm_most_units(a.chunks, a.B) : a.B, inner = cut.row_blocks * a.Hk;
+  const dim3 grid((unsigned)((units + 7) / 8 * 8 * inner)), block(64 * kWaves);
+  const FmDivisor di = fm_divisor(inner), dh = fm_divisor(a.Hk), dt = fm_divisor(a.T);
+  if (cut.block_rows == 16) hipLaunchKernelGGL((decode_kernel<D, F16, E4M3, 1>), grid, block, 0, stream, a, cut.row_blocks, di, dh, dt);
+  else if (cut.block_rows == 32) hipLaunchKernelGGL((decode_kernel<D, F16, E4M3, 2>), grid, block, 0, stream, a, cut.row_blocks, di, dh, dt);
+  else hipLaunchKernelGGL((decode_kernel<D, F16, E4M3, 4>), grid, block, 0, stream, a, cut.row_blocks, di, dh, dt);
+  if (a.plan) {
+    const int R = a.H / a.Hk * a.T;
+    hipLaunchKernelGGL((join_kernel<D, F16>), dim3(a.Hk * R, a.B), dim3(256), 0, stream, a, fm_divisor(R), dt);
+  }
+}
+
+}  // namespace fm
+
+FmDecodeCut fm_decode_cut(int H, int Hk, int T, int d, int B, int cus) {
+  FmDecodeCut cut;
+  const int R = H / Hk * T;
+  cut.block_rows = R <= 16 ? 16 : R <= 32 ? 32 : 64;
+  cut.row_blocks = (R + cut.block_rows - 1) / cut.block_rows;
+  // two workgroups to a compute unit, a few rounds of them
+  const long long wanted = 4ll * (cus > 0 ? cus : 256) / ((long long)Hk * cut.row_blocks);
+  const long long bytes = (long long)Hk * R * (d + 2) * 4, room = (48ll << 20) / (2 * bytes);
+  cut.chunks = (int)std::max<long long>(1, std::min(wanted, room));
+  cut.slots = fm_most_slots(cut.chunks, B);
+  return cut;
+}
+
+hipError_t fm_launch_decode(const FmDecodeArgs& a, bool f16, bool e4m3, hipStream_t stream) {
+  if (a.d == 64) {
+    if (f16) e4m3 ? fm::launch<64, true, true>(a, stream) : fm::launch<64, true, false>(a, stream);
+    else e4m3 ? fm::launch<64, false, true>(a, stream) : fm::launch<64, false, false>(a, stream);
+  } else {
+    if (f16) e4m3 ? fm::launch<128, true, true>(a, stream) : fm::launch<128, true, false>(a, stream);
+    else e4m3 ? fm::launch<128, false, true>(a, stream) : fm::launch<128, false, false>(a, stream);
+  }
+  return hipGetLastError();
+}

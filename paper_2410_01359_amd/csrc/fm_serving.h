@@ -1,0 +1,84 @@
+// Launchers of the kernels around the attention call: rotary positions, the paged cache, attention over it (internal).
+#pragma once
+#include "fm_cache_index.h"
+#include "fm_kernels.h"
+
+// Keeps the text of a HIP error for flashmask_last_hip_error; returns FM_ERR_HIP.
+int fm_hip_error(hipError_t e);
+
+// q, k [B, heads, N, d] -> q_out, k_out; strides in elements, in this order.
+struct FmRopeArgs {
+  const void* in[2];
+  void* out[2];
+  FmStride si[2], so[2];
+  const double* freqs;
+  const int* positions;   // NULL: 0 .. N - 1
+  double amp;
+  int B, heads[2], N, d, rot;
+  int group;              // heads that a workgroup turns by the same angles
+  FmDivisor rows;         // N
+};
+hipError_t fm_launch_rope(FmRopeArgs a, int type, bool interleaved, bool backward, hipStream_t stream);
+
+// Strides in bytes.
+struct FmPages {
+  char* base;
+  long long page, head;
+  unsigned token;
+};
+
+struct FmAppendArgs {
+  const void* in[3];      // q, k, v; strides in elements
+  FmStride si[3];
+  void* q_out;
+  FmStride so;
+  FmPages cache[2];       // k, v
+  const float* scale[2];
+  const int *table, *seqs, *positions;
+  const double* freqs;
+  double amp;
+  int tokens, heads[3], d, rot, sequences, columns, num_pages;
+  int group;
+  FmDivisor page;
+};
+hipError_t fm_launch_append(FmAppendArgs a, bool f16, bool e4m3, bool interleaved, hipStream_t stream);
+
+struct FmDecodeArgs {
+  const void* q;
+  void* out;
+  float* lse;
+  FmStride sq, so;        // elements
+  FmPages k, v;
+  const float *k_scale, *v_scale;
+  const int *table, *lens;
+  const int* bounds[4];   // all or none
+  float scale;
+  int B, H, Hk, T, d, columns, num_pages, page_tokens, bound_columns, window;
+  FmDivisor page;
+  // scratch of split sequences: {first slot, chunks} of a sequence; per slot and K/V head the rows' sums of p v, and {max, sum of p}
+  int2* plan;
+  float* part;
+  float2* stat;
+  int chunks;             // chunks of keys that a head's work is meant to be cut into (FmDecodeCut)
+};
+// How the keys of a call are cut for `cus` compute units.
+struct FmDecodeCut {
+  int row_blocks, block_rows;   // of the H / Hk * T query rows that share a K/V head
+  int chunks, slots;            // of a head; partial results of a head at most
+};
+FmDecodeCut fm_decode_cut(int H, int Hk, int T, int d, int B, int cus);
+hipError_t fm_launch_decode(const FmDecodeArgs& a, bool f16, bool e4m3, hipStream_t stream);
+
+constexpr int FM_POOLS = 64;   // pools of one launch
+struct FmPools {
+  char* p[FM_POOLS];
+};
+hipError_t fm_launch_fork(void* const* pools, int num_pools, size_t page_bytes, int num_pages, const int* table,
+                          const int* lens, const int* parents, const int* new_pages, int* table_out, int* lens_out,
+                          int sequences, int columns, int page, int children, hipStream_t stream);
+// Scratch of the two below.
+size_t fm_plan_bytes(int num_pages);
+hipError_t fm_launch_free_list(const int* table, int entries, int num_pages, int* free_pages, int* count, void* workspace,
+                               hipStream_t stream);
+hipError_t fm_launch_compact(void* const* pools, int num_pools, size_t page_bytes, int num_pages, const int* table,
+                             int entries, int* table_out, int* used, void* workspace, hipStream_t stream);

@@ -1,0 +1,109 @@
+"""GPU: flashmask_rope and its gradient against the definition in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import cache_oracle as orc
+from serving_util import TYPES, check, f64, rounding, strided
+
+pytestmark = pytest.mark.gpu
+
+
+def _frequencies(rot, stretch=1.0):
+    return torch.tensor(10000.0 ** (-2.0 * np.arange(rot // 2) / rot) / stretch, device="cuda")
+
+
+def _bound(x, type, ref, rot, interleaved, amp):
+    """Sine and cosine are off by a rounding, each product and the sum by another: four half steps of 32 bits of both products."""
+    size = np.abs(x).copy()
+    if interleaved:
+        size[..., 0:rot:2] = size[..., 1:rot:2] = np.abs(x[..., 0:rot:2]) + np.abs(x[..., 1:rot:2])
+    else:
+        size[..., :rot // 2] = size[..., rot // 2:rot] = np.abs(x[..., :rot // 2]) + np.abs(x[..., rot // 2:rot])
+    return rounding(type, ref) * (1 + 2.0 ** -20) + 4 * 2.0 ** -24 * abs(amp) * size
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("type", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("B,H,Hk,N,d,rot,packed,positions", [
+    (1, 1, 1, 1, 64, 64, False, None),
+    (2, 3, 1, 77, 128, 128, True, "far"),
+    (1, 4, 2, 500, 64, 16, False, "documents"),
+    (3, 5, 5, 33, 128, 48, True, None),
+    (1, 8, 1, 2050, 128, 64, False, "far"),
+    (2, 2, 2, 130, 64, 48, True, "documents"),
+])
+def test_against_the_definition(B, H, Hk, N, d, rot, packed, positions, type, interleaved):
+    import paper_2410_01359_amd as fm
+    gen = torch.Generator(device="cuda").manual_seed(N + d + rot)
+    q, k = (strided(torch.randn((B, h, N, d), device="cuda", generator=gen).to(TYPES[type]), packed) for h in (H, Hk))
+    freqs, amp = _frequencies(rot, 4.0 if positions == "far" else 1.0), 1.25 if positions == "far" else 1.0
+    at = {None: np.arange(N)[None].repeat(B, 0), "far": 3_000_000 - 7 * np.arange(B * N).reshape(B, N),
+          "documents": np.arange(B * N).reshape(B, N) % 37 - 3}[positions]
+    given = None if positions is None else torch.tensor(at, dtype=torch.int32, device="cuda")
+    layout = fm.FM_ROPE_INTERLEAVED if interleaved else fm.FM_ROPE_HALF
+    for call, backward in ((fm.flashmask_rope, False), (fm.flashmask_rope_bwd, True)):
+        got = call(q, k, freqs, given, layout=layout, amp=amp)
+        for name, x, y in (("q", q, got[0]), ("k", k, got[1])):
+            assert y.dtype == x.dtype and y.shape == x.shape and y.stride() == x.stride()
+            ref = orc.rope(f64(x), at[:, None], freqs.cpu().numpy(), interleaved, amp, backward)
+            check(f64(y), ref, _bound(f64(x), type, ref, rot, interleaved, amp), f"{name} {'backward' if backward else 'forward'}")
+            assert torch.equal(y[..., rot:], x[..., rot:])
+
+
+def test_gradient_against_differences():
+    """<w, rope(x)> changes with x as rope_bwd(w) says (all in fp32; differences of a linear function are exact but for rounding)."""
+    import paper_2410_01359_amd as fm
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    q, w = (torch.randn((1, 2, 40, 64), device="cuda", generator=gen) for _ in range(2))
+    freqs = _frequencies(32)
+    for layout in (fm.FM_ROPE_HALF, fm.FM_ROPE_INTERLEAVED):
+        grad, _ = fm.flashmask_rope_bwd(w, w, freqs, layout=layout, amp=1.5)
+        step = torch.randn(q.shape, device="cuda", generator=gen)
+        up, _ = fm.flashmask_rope(q + step, q, freqs, layout=layout, amp=1.5)
+        down, _ = fm.flashmask_rope(q - step, q, freqs, layout=layout, amp=1.5)
+        change = ((up.double() - down.double()) * w.double()).sum() / 2
+        want = (grad.double() * step.double()).sum()
+        size = (w.abs().double() * (q.abs() + step.abs()).double()).sum() * 1.5
+        assert abs(float(change - want)) <= 16 * 2.0 ** -24 * float(size) * 2
+
+
+def test_infinities_and_nan_stay_in_their_pair():
+    import paper_2410_01359_amd as fm
+    x = torch.ones((1, 1, 4, 64), device="cuda", dtype=torch.bfloat16)
+    x[0, 0, 1, 3], x[0, 0, 2, 40] = torch.inf, torch.nan
+    y, _ = fm.flashmask_rope(x, x, _frequencies(32), layout=fm.FM_ROPE_INTERLEAVED)
+    odd = (~torch.isfinite(y[0, 0])).nonzero().tolist()
+    assert odd == [[1, 2], [1, 3], [2, 40]]
+    y, _ = fm.flashmask_rope(x, x, _frequencies(32), layout=fm.FM_ROPE_HALF)
+    assert (~torch.isfinite(y[0, 0])).nonzero().tolist() == [[1, 3], [1, 19], [2, 40]]
+
+
+def test_slices_of_a_projection_and_another_stream():
+    import paper_2410_01359_amd as fm
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    qkv = torch.randn((2, 50, 6, 128), device="cuda", generator=gen).bfloat16().transpose(1, 2)   # [B, 4 + 1 + 1 heads, N, d]
+    q, k = qkv[:, :4], qkv[:, 4:5]
+    freqs = _frequencies(128)
+    ref = fm.flashmask_rope(q.contiguous(), k.contiguous(), freqs)
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        got = fm.flashmask_rope(q, k, freqs)
+    torch.cuda.current_stream().wait_stream(stream)
+    assert torch.equal(ref[0], got[0]) and torch.equal(ref[1], got[1])
+
+
+def test_refusals():
+    import paper_2410_01359_amd as fm
+    q = torch.zeros((2, 4, 10, 64), device="cuda", dtype=torch.bfloat16)
+    at, freqs = torch.zeros((2, 10), device="cuda", dtype=torch.int32), _frequencies(64)
+    fm.flashmask_rope(q, q, freqs, at)
+    for wrong in ((q.double(), q.double(), freqs, at), (q, q.float(), freqs, at), (q, q[:1], freqs, at), (q, q[:, :, :9], freqs, at),
+                  (q[..., ::2], q[..., ::2], freqs[:16], at), (q, q, freqs.float(), at), (q, q, freqs[::2], at), (q, q, freqs[:5], at),
+                  (q, q, freqs.cpu(), at), (q, q, freqs, at.long()), (q, q, freqs, at[:1]), (q, q, freqs, at.cpu()), (q[0], q[0], freqs, at),
+                  (q[..., :48], q[..., :48], freqs[:16], at), (q[..., :32], q[..., :32], freqs[:16], at), (q, q, freqs.repeat(2), at),
+                  (q[:, :0], q, freqs, at), (q[:, :, :0], q[:, :, :0], freqs, at[:, :0])):
+        for call in (fm.flashmask_rope, fm.flashmask_rope_bwd):
+            with pytest.raises(fm.FlashMaskError):
+                call(*wrong)
