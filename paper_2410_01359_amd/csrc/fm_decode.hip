@@ -77,11 +77,13 @@ __device__ __forceinline__ unsigned dpp_or(unsigned x) {
 }
 // Bits set in any of the 16 lanes of a DPP row.
 __device__ __forceinline__ unsigned row16_or(unsigned x) { return dpp_or<0x121>(dpp_or<0x122>(dpp_or<0x124>(dpp_or<0x128>(x)))); }
-// Whether one of the two 16-bit values is infinite or NaN.
-template <bool F16>
-__device__ __forceinline__ bool odd_pair(unsigned x) {
-  constexpr unsigned kExp = F16 ? 0x7c00u : 0x7f80u;
-  return (x & kExp) == kExp || (x >> 16 & kExp) == kExp;
+// Whether a word of cached values has an infinity or NaN: an exponent (e4m3: all bits but the sign) of ones, to which one more bit
+// carries into the sign's place.
+template <bool F16, bool E4M3>
+__device__ __forceinline__ bool odd_word(unsigned x) {
+  constexpr unsigned kOnes = E4M3 ? 0x7f7f7f7fu : F16 ? 0x7c007c00u : 0x7f807f80u;
+  constexpr unsigned kOne = E4M3 ? 0x01010101u : F16 ? 0x04000400u : 0x00800080u, kCarry = E4M3 ? 0x80808080u : 0x80008000u;
+  return (((x & kOnes) + kOne) & kCarry) != 0;
 }
 // Maximum over the four lanes l, l ^ 16, l ^ 32, l ^ 48.
 __device__ __forceinline__ float quad_max(float x) {
@@ -97,38 +99,38 @@ __device__ __forceinline__ FmKeyRange key_range(const FmDecodeArgs& a, int b) {
   return fm_key_range(a.lens[b], a.T, a.window, a.columns * a.page_tokens);
 }
 
-// Whether row i sees key j, as far as the bounds tell.
-__device__ __forceinline__ bool bounds_hide(const FmDecodeArgs& a, int b, int j, int i) {
-  if (j >= a.bound_columns) return false;
-  const size_t at = (size_t)b * a.bound_columns + j;
-  return (a.bounds[0][at] <= i && i < a.bounds[1][at]) || (a.bounds[2][at] <= i && i < a.bounds[3][at]);
+// Whether the bounds (LTS, LTE, UTS, UTE) of a key hide it from row i.
+__device__ __forceinline__ bool hides(const i32x4& bound, int i) {
+  return (bound[0] <= i && i < bound[1]) || (bound[2] <= i && i < bound[3]);
 }
 
 template <int D, bool F16, bool E4M3, int NB>
 struct Decode {
   static constexpr int BYTES = E4M3 ? 1 : 2;
   // keys of a wave's step: 16 KiB of K and V, fewer where the scores of NB query blocks would not fit the registers
-  static constexpr int KT = std::min(16384 / (64 * D * BYTES), std::max(8 / NB, 1)), GROUPS = 2 * KT, KEYS = 32 * KT;
+  static constexpr int KT = std::min(16384 / (64 * D * BYTES), std::max(256 / (D * NB), 1)), GROUPS = 2 * KT, KEYS = 32 * KT;
   static constexpr int KSTEPS = D / 32;             // products of S^T
   static constexpr int KLOADS = D * BYTES / 64;     // 16-byte loads of a lane per group of keys
   static constexpr int E = D / 16;                  // products of O^T; elements of d in a lane's piece of a value row
   static constexpr int VWORDS = E * BYTES / 4;      // words of that piece
   static constexpr int ROWS = 16 * NB;              // query rows
-  static constexpr int LIST = 128;                  // steps listed at a time where bounds hide keys
+  static constexpr int PANEL = 2048, LIST = PANEL / KEYS;   // keys, and steps, whose bounds are looked at together
   typedef __attribute__((ext_vector_type(VWORDS))) unsigned vpiece;
   struct Shared {
     union {
       struct {
+        i32x4 bound[PANEL];
         int list[LIST], flag[LIST], count;
       };
       float out[kWaves][16][D + 4];
     };
     float2 stat[kWaves][16];
+    int odd;   // an infinity or NaN among values that some rows see and others do not
   };
 };
 
 template <int D, bool F16, bool E4M3, int NB>
-__global__ __launch_bounds__(64 * kWaves, NB == 1 ? 2 : 1) void decode_kernel(FmDecodeArgs a, int row_blocks, FmDivisor inner,
+__global__ __launch_bounds__(64 * kWaves, NB <= 2 ? 2 : 1) void decode_kernel(FmDecodeArgs a, int row_blocks, FmDivisor inner,
                                                                             FmDivisor heads, FmDivisor tokens) {
   using C = Decode<D, F16, E4M3, NB>;
   __shared__ typename C::Shared sh;
@@ -196,16 +198,16 @@ __global__ __launch_bounds__(64 * kWaves, NB == 1 ? 2 : 1) void decode_kernel(Fm
   // Queries
   const int G = a.H / a.Hk, R = G * a.T;
   u32x4 q[NB][C::KSTEPS];
-  int row_token[NB];   // query t of the lane's column, -1: none
+  int column_token[NB];   // query t of the lane's column, -1: none
 #pragma unroll
   for (int nb = 0; nb < NB; ++nb) {
     const int r = rb * C::ROWS + nb * 16 + c;
-    row_token[nb] = -1;
+    column_token[nb] = -1;
 #pragma unroll
     for (int s = 0; s < C::KSTEPS; ++s) q[nb][s] = u32x4{0, 0, 0, 0};
     if (r < R) {
       const int hq = fm_div(r, tokens), t = r - hq * a.T;
-      row_token[nb] = t;
+      column_token[nb] = t;
       const char* p = (const char*)a.q + 2 * ((long long)b * a.sq.b + (long long)(hk * G + hq) * a.sq.h + (long long)t * a.sq.n);
 #pragma unroll
       for (int s = 0; s < C::KSTEPS; ++s)
@@ -258,40 +260,61 @@ __global__ __launch_bounds__(64 * kWaves, NB == 1 ? 2 : 1) void decode_kernel(Fm
   };
 
   // Which of the lane's keys (bit 4 i + r: key 4 g + r of group i) row `row_i` sees
-  const auto seen_keys = [&](int start, unsigned pages_there, int row_i) {
+  const auto seen_keys = [&](int start, int panel, unsigned pages_there, int row_i) {
     unsigned seen = 0;
+    const int last = min(j_end - 1, row_i), first = a.window > 0 ? row_i - a.window + 1 : 0;
 #pragma unroll 1
-    for (int bit = 0; bit < 4 * C::GROUPS; ++bit) {
-      const int j = start + bit / 4 * kGroup + 4 * g + bit % 4;
-      const bool sees = (pages_there >> (bit / 4) & 1) && j < j_end && j <= row_i && (a.window <= 0 || j > row_i - a.window) &&
-                        !(a.bounds[0] && bounds_hide(a, b, j, row_i));
-      seen |= (sees ? 1u : 0u) << bit;
+    for (int i = 0; i < C::GROUPS; ++i) {
+      const int j = start + i * kGroup + 4 * g;
+      unsigned four = 0;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) four |= (j + r <= last && j + r >= first ? 1u : 0u) << r;
+      if (a.bounds[0]) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if (hides(sh.bound[min(j + r - panel, C::PANEL - 1)], row_i)) four &= ~(1u << r);
+      }
+      seen |= (pages_there >> i & 1 ? four : 0u) << (4 * i);
     }
     return seen;
   };
 
+  // Columns are worked on together.  A value that one row sees and another does not enters the other's sum times 0, so an infinity or
+  // NaN among those would reach rows that do not see it: where one turns up, the workgroup begins again and takes the
+  // rows of one query t at a time, which all see the same keys.
+  if (threadIdx.x == 0) sh.odd = 0;
+  for (int only = -1, rounds = 1; rounds > 0; --rounds) {
+  int row_token[NB];
   float m[NB], l[NB];
   f32x4 acc[NB][C::E];
 #pragma unroll
   for (int nb = 0; nb < NB; ++nb) {
+    row_token[nb] = only < 0 || column_token[nb] == only ? column_token[nb] : -1;
     m[nb] = -INFINITY;
     l[nb] = 0.f;
 #pragma unroll
     for (int e = 0; e < C::E; ++e) acc[nb][e] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
+  __syncthreads();
 
-  for (int panel = j_begin; panel < j_end; panel += a.bounds[0] ? C::LIST * C::KEYS : INT32_MAX / 2) {
+  for (int panel = j_begin; panel < j_end; panel += a.bounds[0] ? C::PANEL : INT32_MAX / 2) {
     int steps;
     if (a.bounds[0]) {
       // the steps of which some row sees a key, and whether it takes the element mask
-      const int end = min(j_end, panel + C::LIST * C::KEYS), all = (end - panel + C::KEYS - 1) / C::KEYS;
+      const int end = min(j_end, panel + C::PANEL), all = (end - panel + C::KEYS - 1) / C::KEYS;
       for (int i = threadIdx.x; i < all; i += 64 * kWaves) sh.flag[i] = 0;
       __syncthreads();
       for (int j = panel + threadIdx.x; j < end; j += 64 * kWaves) {
+        i32x4 bound = {0, 0, 0, 0};
+        if (j < a.bound_columns) {
+#pragma unroll
+          for (int w = 0; w < 4; ++w) bound[w] = a.bounds[w][(size_t)b * a.bound_columns + j];
+        }
+        sh.bound[j - panel] = bound;
         int flag = 0;
         for (int t = 0; t < a.T; ++t) {
           const int i = first_row + t;
-          flag |= j <= i && (a.window <= 0 || j > i - a.window) && !bounds_hide(a, b, j, i) ? 1 : 2;
+          flag |= j <= i && (a.window <= 0 || j > i - a.window) && !hides(bound, i) ? 1 : 2;
         }
         atomicOr(&sh.flag[(j - panel) / C::KEYS], flag);
       }
@@ -357,16 +380,15 @@ __global__ __launch_bounds__(64 * kWaves, NB == 1 ? 2 : 1) void decode_kernel(Fm
 
         // element mask; values that no row sees become 0 (the keys of a lane's scores are those of its value pieces).  Which of its
         // keys a column sees is gathered as bits by a loop: unrolled, the bounds' addresses alone would fill the registers.
-        bool mixed = false;   // some row sees a key that another one does not
-        unsigned pages_there = 0;
         if (masked) {
+          unsigned pages_there = 0;
 #pragma unroll
           for (int i = 0; i < C::GROUPS; ++i) pages_there |= (now.page[i] >= 0 ? 1u : 0u) << i;
           unsigned any = 0, every = ~0u;
 #pragma unroll
           for (int nb = 0; nb < NB; ++nb) {
             const bool real = row_token[nb] >= 0;
-            const unsigned seen = real ? seen_keys(start, pages_there, first_row + row_token[nb]) : 0u;
+            const unsigned seen = real ? seen_keys(start, panel, pages_there, first_row + row_token[nb]) : 0u;
             any |= row16_or(seen);
             every &= ~row16_or(real ? ~seen : 0u);
 #pragma unroll
@@ -375,7 +397,16 @@ __global__ __launch_bounds__(64 * kWaves, NB == 1 ? 2 : 1) void decode_kernel(Fm
               for (int r = 0; r < 4; ++r)
                 if (!(seen >> (4 * i + r) & 1)) p[nb][i][r] = -INFINITY;
           }
-          mixed = __any((any & ~every) != 0);
+          if (__any((any & ~every) != 0)) {
+            bool odd = false;
+#pragma unroll
+            for (int kt = 0; kt < C::KT; ++kt)
+#pragma unroll
+              for (int t = 0; t < 8; ++t)
+#pragma unroll
+                for (int w = 0; w < C::VWORDS; ++w) odd |= (any & ~every) >> (8 * kt + t) & 1 && odd_word<F16, E4M3>(vraw[kt][t][w]);
+            if (odd) sh.odd = 1;
+          }
 #pragma unroll
           for (int i = 0; i < C::GROUPS; ++i)
 #pragma unroll
@@ -435,44 +466,15 @@ __global__ __launch_bounds__(64 * kWaves, NB == 1 ? 2 : 1) void decode_kernel(Fm
               for (int w = 0; w < C::VWORDS; ++w) v[t][w] = vraw[kt][t][w];
             }
           }
-          bool odd = false;
-          if (mixed) {
 #pragma unroll
-            for (int t = 0; t < 8; ++t)
+          for (int e = 0; e < C::E; ++e) {
+            u32x4 op;
 #pragma unroll
-              for (int w = 0; w < C::E / 2; ++w) odd |= odd_pair<F16>(v[t][w]);
-            odd = __any(odd);
-          }
-          if (odd) {
-            // an infinity or NaN among values that not every row sees: row by row, the others' values left out
-#pragma unroll 1
-            for (int t = 0; t < a.T; ++t) {
-              const unsigned seen = seen_keys(start, pages_there, first_row + t) >> (8 * kt);
+            for (int w = 0; w < 4; ++w) op[w] = pair_of(v[2 * w][e / 2], v[2 * w + 1][e / 2], e % 2);
 #pragma unroll
-              for (int e = 0; e < C::E; ++e) {
-                u32x4 op;
-#pragma unroll
-                for (int w = 0; w < 4; ++w)
-                  op[w] = pair_of(seen >> (2 * w) & 1 ? v[2 * w][e / 2] : 0u, seen >> (2 * w + 1) & 1 ? v[2 * w + 1][e / 2] : 0u, e % 2);
-#pragma unroll
-                for (int nb = 0; nb < NB; ++nb) {
-                  f32x4 x = mfma_keys<F16>(op, lo[nb], f32x4{0.f, 0.f, 0.f, 0.f});
-                  x = mfma_keys<F16>(op, hi[nb], x);
-                  if (row_token[nb] == t) acc[nb][e] += x;
-                }
-              }
-            }
-          } else {
-#pragma unroll
-            for (int e = 0; e < C::E; ++e) {
-              u32x4 op;
-#pragma unroll
-              for (int w = 0; w < 4; ++w) op[w] = pair_of(v[2 * w][e / 2], v[2 * w + 1][e / 2], e % 2);
-#pragma unroll
-              for (int nb = 0; nb < NB; ++nb) {
-                acc[nb][e] = mfma_keys<F16>(op, lo[nb], acc[nb][e]);
-                acc[nb][e] = mfma_keys<F16>(op, hi[nb], acc[nb][e]);
-              }
+            for (int nb = 0; nb < NB; ++nb) {
+              acc[nb][e] = mfma_keys<F16>(op, lo[nb], acc[nb][e]);
+              acc[nb][e] = mfma_keys<F16>(op, hi[nb], acc[nb][e]);
             }
           }
         }
@@ -486,8 +488,14 @@ __global__ __launch_bounds__(64 * kWaves, NB == 1 ? 2 : 1) void decode_kernel(Fm
     if (a.bounds[0]) __syncthreads();
   }
 
-  // The waves' sums meet in LDS, 16 rows at a time
   __syncthreads();
+  if (only < 0 && sh.odd) {
+    only = 0;
+    rounds = a.T + 1;
+    continue;
+  }
+
+  // The waves' sums meet in LDS, 16 rows at a time
   constexpr int PER = 16 * D / (64 * kWaves);   // elements of a thread: neighbours of one row
   const int my_row = threadIdx.x * PER / D, my_col = threadIdx.x * PER % D;
   const float v_scale = E4M3 ? a.v_scale[hk] : 1.f;
@@ -516,7 +524,7 @@ __global__ __launch_bounds__(64 * kWaves, NB == 1 ? 2 : 1) void decode_kernel(Fm
       for (int e = 0; e < PER; ++e) x[e] += weight[w] * sh.out[w][my_row][my_col + e];
     }
     const int r = rb * C::ROWS + nb * 16 + my_row;
-    if (r < R) {
+    if (r < R && (only < 0 || r % a.T == only)) {
       if (chunks > 1) {
         const size_t at = ((size_t)(slot + chunk) * a.Hk + hk) * R + r;
 #pragma unroll
@@ -532,6 +540,8 @@ __global__ __launch_bounds__(64 * kWaves, NB == 1 ? 2 : 1) void decode_kernel(Fm
       }
     }
     __syncthreads();
+  }
+  if (only >= 0) ++only;
   }
 }
 
