@@ -6,6 +6,8 @@
 // Keeps the text of a HIP error for flashmask_last_hip_error; returns FM_ERR_HIP.
 int fm_hip_error(hipError_t e);
 
+constexpr int FM_MOST_HEADS = 16384;
+
 // q, k [B, heads, N, d] -> q_out, k_out; strides in elements, in this order.
 struct FmRopeArgs {
   const void* in[2];
@@ -15,7 +17,7 @@ struct FmRopeArgs {
   const int* positions;   // NULL: 0 .. N - 1
   double amp;
   int B, heads[2], N, d, rot;
-  int group;              // heads that a workgroup turns by the same angles
+  int span, group;        // tokens and heads of a workgroup
   FmDivisor rows;         // N
 };
 hipError_t fm_launch_rope(FmRopeArgs a, int type, bool interleaved, bool backward, hipStream_t stream);
@@ -38,7 +40,7 @@ struct FmAppendArgs {
   const double* freqs;
   double amp;
   int tokens, heads[3], d, rot, sequences, columns, num_pages;
-  int group;
+  int span, group;        // tokens and heads of a workgroup
   FmDivisor page;
 };
 hipError_t fm_launch_append(FmAppendArgs a, bool f16, bool e4m3, bool interleaved, hipStream_t stream);

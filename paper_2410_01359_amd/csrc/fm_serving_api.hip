@@ -32,7 +32,7 @@ int rope(const void* q, const void* k, void* q_out, void* k_out, const double* f
          double amp, int B, int H, int Hk, int N, int d, int rot, const flashmask_strides* strides, bool backward, void* hip_stream) {
   if (!q || !k || !q_out || !k_out || !freqs || !strides) return FM_ERR_NULL;
   if (type != FM_TYPE_BF16 && type != FM_TYPE_F16 && type != FM_TYPE_F32) return FM_ERR_ARG;
-  if (B <= 0 || H <= 0 || Hk <= 0 || N <= 0 || bad_head_dim(d) || H > 32767 || Hk > 32767) return FM_ERR_SHAPE;
+  if (B <= 0 || H <= 0 || Hk <= 0 || N <= 0 || bad_head_dim(d) || H > FM_MOST_HEADS || Hk > FM_MOST_HEADS) return FM_ERR_SHAPE;
   if ((long long)B * N > (1ll << 31) / 16 - 256) return FM_ERR_SHAPE;
   if (int rc = check_rotation(layout, amp, d, rot)) return rc;
   for (int t = 0; t < 4; ++t)
@@ -51,7 +51,7 @@ int check_cache(const flashmask_cache* c) {
   if (!c || !c->k || !c->v || !c->table) return FM_ERR_NULL;
   if (c->type != FM_TYPE_BF16 && c->type != FM_TYPE_F16 && c->type != FM_TYPE_E4M3) return FM_ERR_ARG;
   if ((c->type == FM_TYPE_E4M3) != (c->k_scale != nullptr) || (c->type == FM_TYPE_E4M3) != (c->v_scale != nullptr)) return FM_ERR_NULL;
-  if (c->heads <= 0 || c->heads > 32767 || bad_head_dim(c->d) || c->num_pages <= 0 || c->page <= 0 || c->page % 16 || c->page > (1 << 20) ||
+  if (c->heads <= 0 || c->heads > FM_MOST_HEADS || bad_head_dim(c->d) || c->num_pages <= 0 || c->page <= 0 || c->page % 16 || c->page > (1 << 20) ||
       c->sequences <= 0 || c->columns <= 0 || (long long)c->columns * c->page > (1 << 30))
     return FM_ERR_SHAPE;
   for (const flashmask_strides* s : {&c->sk, &c->sv})
@@ -70,7 +70,7 @@ int check_row_type(int type, const flashmask_cache& c) {
 
 // Queries that flashmask_decode's indexing has room for.
 int check_decode_shape(int sequences, int H, int Hk, int T, int d) {
-  if (sequences <= 0 || H <= 0 || H > 32767 || Hk <= 0 || H % Hk || T <= 0 || T > 65536 || bad_head_dim(d)) return FM_ERR_SHAPE;
+  if (sequences <= 0 || H <= 0 || H > FM_MOST_HEADS || Hk <= 0 || H % Hk || T <= 0 || T > 65536 || bad_head_dim(d)) return FM_ERR_SHAPE;
   if ((long long)H * T > (1 << 24) || sequences > 65535 || (long long)H * T * sequences > (1ll << 30)) return FM_ERR_SHAPE;
   return FM_OK;
 }
@@ -123,7 +123,7 @@ int flashmask_cache_append(const flashmask_cache* cache, const void* q, const vo
   if (int rc = check_cache(cache)) return rc;
   if (!k || !v || !seqs || !positions || !strides || (q && (!q_out || !freqs))) return FM_ERR_NULL;
   if (int rc = check_row_type(type, *cache)) return rc;
-  if (tokens <= 0 || tokens > (1 << 27) || (q && (H <= 0 || H > 32767))) return FM_ERR_SHAPE;
+  if (tokens <= 0 || tokens > (1 << 27) || (q && (H <= 0 || H > FM_MOST_HEADS))) return FM_ERR_SHAPE;
   if (freqs)
     if (int rc = check_rotation(layout, amp, cache->d, rot)) return rc;
   for (int t = q ? 0 : 1; t < (q ? 4 : 3); ++t)
