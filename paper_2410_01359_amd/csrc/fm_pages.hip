@@ -6,18 +6,20 @@
 
 namespace fm {
 
-// Bytes of a page that a workgroup moves at a time: four 16-byte loads of a lane in flight.
-constexpr int kPart = 256 * 64;
+// Bytes of a page that a workgroup moves at a time, two 16-byte loads of a lane in flight.  Copies go past the L2, which has no
+// use for them.  256 children of 64 prompts, six layers: 99 us with four loads and ordinary stores, 90 past the L2, 88 with two loads,
+// 95 with one.
+constexpr int kLoads = 2, kPart = 4096 * kLoads;
 
 __device__ __forceinline__ void copy_part(const char* from, char* to, size_t page_bytes, int part) {
   const size_t at = (size_t)part * kPart + threadIdx.x * 16;
-  u32x4 x[4];
+  u32x4 x[kLoads];
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
+  for (int i = 0; i < kLoads; ++i)
     if (at + i * 4096 < page_bytes) x[i] = ldg16(from + at + i * 4096);
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
-    if (at + i * 4096 < page_bytes) *(u32x4*)(to + at + i * 4096) = x[i];
+  for (int i = 0; i < kLoads; ++i)
+    if (at + i * 4096 < page_bytes) __builtin_nontemporal_store(x[i], (u32x4*)(to + at + i * 4096));
 }
 
 // Workgroups (x, child): x = 0 writes the child's row (tables == true), the others a part of the last page in a pool each.
@@ -237,9 +239,11 @@ hipError_t fm_launch_compact(void* const* pools, int num_pools, size_t page_byte
   if (hipError_t e = fm::launch_plan(a, ws, stream); e != hipSuccess) return e;
   const int parts = (int)((page_bytes + fm::kPart - 1) / fm::kPart);
   fm::pool_groups(pools, num_pools, [&](const FmPools& group, int n, bool first) {
-    // at most every second page moves
+    // At most every second page moves; how many do is known on the device alone.  Many workgroups that take few parts each keep
+    // the memory busiest: six layers (a page of 128 KiB) 324, 320, 298 us with 16, 32, 256 to a compute unit; pages of 1 KiB 143, 141, 131 and
+    // again 143 with 512.
     const long long most = (long long)(num_pages / 2) * n * parts, rows = first ? (entries + 255) / 256 : 0;
-    const int workgroups = (int)std::min<long long>(std::max<long long>(std::max(most, rows), 1), 16ll * fm_compute_units());
+    const int workgroups = (int)std::min<long long>(std::max<long long>(std::max(most, rows), 1), 256ll * fm_compute_units());
     hipLaunchKernelGGL(fm::move_kernel, dim3(workgroups), dim3(256), 0, stream, group, n, parts, page_bytes, num_pages, a.moves,
                        a.source, a.target, a.place, table, first ? entries : 0, table_out);
   });
