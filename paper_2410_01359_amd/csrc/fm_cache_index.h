@@ -41,8 +41,8 @@ FM_HOST_DEVICE inline FmKeyRange fm_key_range(int len, int T, int window, int ta
 FM_HOST_DEVICE inline int fm_key_groups(const FmKeyRange& r) { return (r.hi - r.lo + FM_KEY_GROUP - 1) / FM_KEY_GROUP; }
 
 // Groups of a chunk where sequences of `total` groups together are meant to be cut into `chunks`: a multiple of `round`.
-FM_HOST_DEVICE inline int fm_chunk_groups(unsigned total, int chunks, int round) {
-  unsigned size = (total + chunks - 1) / chunks;
+FM_HOST_DEVICE inline int fm_chunk_groups(unsigned total, const FmDivisor& chunks, int round) {
+  unsigned size = fm_div((int)(total + chunks.n - 1), chunks);
   if (size < FM_MIN_CHUNK / FM_KEY_GROUP) size = FM_MIN_CHUNK / FM_KEY_GROUP;
   return (int)((size + round - 1) / round * round);
 }

@@ -92,12 +92,22 @@ __device__ __forceinline__ float quad_max(float x) {
   r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(int, x), __builtin_bit_cast(int, x), false, false);
   return fmaxf(__builtin_bit_cast(float, (int)r[0]), __builtin_bit_cast(float, (int)r[1]));
 }
+// Sums over the lanes up to this one, and the last lane's value (uniform).
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int dpp_add(int x) {
+  return x + __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xf, false);
+}
+__device__ __forceinline__ int wave_scan(int x) {
+  x = dpp_add<0x111, 0xf>(x);   // from 1, 2, 4, 8 lanes back in the row of 16
+  x = dpp_add<0x112, 0xf>(x);
+  x = dpp_add<0x114, 0xf>(x);
+  x = dpp_add<0x118, 0xf>(x);
+  x = dpp_add<0x142, 0xa>(x);   // the last lane of rows 0 and 2 to the next row, then of row 1 to rows 2 and 3
+  return dpp_add<0x143, 0xc>(x);
+}
+__device__ __forceinline__ int wave_last(int x) { return __builtin_amdgcn_readlane(x, 63); }
 // Exponents are taken against this: a row that has seen nothing has no maximum.
 __device__ __forceinline__ float reference(float m) { return m == -INFINITY ? 0.f : m; }
-
-__device__ __forceinline__ FmKeyRange key_range(const FmDecodeArgs& a, int b) {
-  return fm_key_range(a.lens[b], a.T, a.window, a.columns * a.page_tokens);
-}
 
 // Whether the bounds (LTS, LTE, UTS, UTE) of a key hide it from row i.
 __device__ __forceinline__ bool hides(const i32x4& bound, int i) {
@@ -129,9 +139,12 @@ struct Decode {
   };
 };
 
-template <int D, bool F16, bool E4M3, int NB>
-__global__ __launch_bounds__(64 * kWaves, NB <= 2 ? 2 : 1) void decode_kernel(FmDecodeArgs a, int row_blocks, FmDivisor inner,
-                                                                            FmDivisor heads, FmDivisor tokens) {
+// TEAMS = 2: the workgroup's waves are two teams that go over the same keys together, for two blocks of query rows, or for two heads
+// whose rows share cache lines: what one team loads the other finds in the caches.
+template <int D, bool F16, bool E4M3, int NB, int TEAMS>
+__global__ __launch_bounds__(64 * kWaves, 2) void decode_kernel(FmDecodeArgs a, int members, FmDivisor inner, FmDivisor row_blocks,
+                                                              FmDivisor tokens, FmDivisor chunks_meant) {
+  constexpr int TW = kWaves / TEAMS;   // waves of a team
   using C = Decode<D, F16, E4M3, NB>;
   __shared__ typename C::Shared sh;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -139,58 +152,51 @@ __global__ __launch_bounds__(64 * kWaves, NB <= 2 ? 2 : 1) void decode_kernel(Fm
   // Workgroup -> chunk of a sequence, K/V head, block of query rows.  Workgroup x runs on XCD x % 8: all heads of a chunk on one,
   // one behind the other, because they share page table entries, bounds, and cache lines where heads lie next to each other.
   const int slot_of_xcd = blockIdx.x >> 3;
-  const int turn = fm_div(slot_of_xcd, inner), member = slot_of_xcd - turn * (int)inner.n;
+  const int turn = fm_div(slot_of_xcd, inner), pair = slot_of_xcd - turn * (int)inner.n;
   const int unit = turn * 8 + (blockIdx.x & 7);
-  const int rb = fm_div(member, heads), hk = member - rb * (int)heads.n;
+  const int team = wave % TEAMS, team_wave = wave / TEAMS, team_thread = team_wave * 64 + lane;
+  const bool idle = pair * TEAMS + team >= members;   // a last team without a partner
+  const int member = idle ? members - 1 : pair * TEAMS + team;
+  const int hk = fm_div(member, row_blocks), rb = member - hk * (int)row_blocks.n;
 
-  // Chunk: all sequences' keys together are cut into a.chunks pieces, each sequence into whole ones of that size.
-  int b = 0, chunk = 0, chunks = 1, slot = 0, size = INT32_MAX / 32;   // size: in groups
+  // Chunk: all sequences' keys together are cut into a.chunks pieces, each sequence into whole ones of that size.  Every wave works this
+  // out for itself, 64 sequences at a time; up to 64 their lengths are read once.
+  int b = unit, chunk = 0, chunks = 1, slot = 0, size = INT32_MAX / 32, len;   // size: in groups
   if (a.plan) {
+    const auto groups_of = [&](int l) { return fm_key_groups(fm_key_range(l, a.T, a.window, a.columns * a.page_tokens)); };
     unsigned total = 0;
+    int lane_len = 0;
     for (int base = 0; base < a.B; base += 64) {
-      int n = base + lane < a.B ? fm_key_groups(key_range(a, base + lane)) : 0;
-#pragma unroll
-      for (int k = 1; k < 64; k *= 2) n += __shfl_xor(n, k);
-      total += n;
+      lane_len = base + lane < a.B ? a.lens[base + lane] : 0;
+      total += wave_last(wave_scan(groups_of(lane_len)));
     }
-    size = fm_chunk_groups(total, a.chunks, kWaves * C::GROUPS);
-    int units = 0, slots = 0;
-    b = -1;
-    for (int base = 0; base < a.B; base += 64) {
-      int n = 0;
-      if (base + lane < a.B) n = fm_chunks_of(fm_key_groups(key_range(a, base + lane)), size);
-      int upto = n, upto_slots = n > 1 ? n : 0;
-#pragma unroll
-      for (int k = 1; k < 64; k *= 2) {
-        const int o = __shfl_up(upto, k), os = __shfl_up(upto_slots, k);
-        if (lane >= k) {
-          upto += o;
-          upto_slots += os;
-        }
-      }
-      const unsigned long long behind = __ballot(n > 0 && units + upto > unit);
+    size = fm_chunk_groups(total, chunks_meant, TW * C::GROUPS);
+    int units = 0, slots = 0, base = 0;
+    while (true) {
+      if (a.B > 64) lane_len = base + lane < a.B ? a.lens[base + lane] : 0;
+      const int n = base + lane < a.B ? fm_chunks_of(groups_of(lane_len), size) : 0;
+      const int upto = wave_scan(n), upto_slots = wave_scan(n > 1 ? n : 0);
+      const unsigned long long behind = __ballot(units + upto > unit);
       if (behind) {
         const int at = __builtin_ctzll(behind);
         b = base + at;
-        chunks = __shfl(n, at);
-        chunk = unit - (units + __shfl(upto, at) - chunks);
-        slot = slots + __shfl(upto_slots, at) - (chunks > 1 ? chunks : 0);
+        chunks = __builtin_amdgcn_readlane(n, at);
+        chunk = unit - (units + __builtin_amdgcn_readlane(upto, at) - chunks);
+        slot = slots + __builtin_amdgcn_readlane(upto_slots, at) - (chunks > 1 ? chunks : 0);
+        len = __builtin_amdgcn_readlane(lane_len, at);
         break;
       }
-      units += __shfl(upto, 63);
-      slots += __shfl(upto_slots, 63);
+      units += wave_last(upto);
+      slots += wave_last(upto_slots);
+      base += 64;
+      if (base >= a.B) return;
     }
-    b = __builtin_amdgcn_readfirstlane(b);
-    if (b < 0) return;
-    chunks = __builtin_amdgcn_readfirstlane(chunks);
-    chunk = __builtin_amdgcn_readfirstlane(chunk);
-    slot = __builtin_amdgcn_readfirstlane(slot);
-    if (chunk == 0 && member == 0 && threadIdx.x == 0) a.plan[b] = int2{slot, chunks};
+    if (chunk == 0 && pair == 0 && threadIdx.x == 0) a.plan[b] = int2{slot, chunks};
   } else {
-    b = unit;
     if (b >= a.B) return;
+    len = a.lens[b];
   }
-  const FmKeyRange range = key_range(a, b);
+  const FmKeyRange range = fm_key_range(len, a.T, a.window, a.columns * a.page_tokens);
   const int j_begin = range.lo + chunk * size * kGroup;
   const int j_end = (int)std::min<long long>(range.hi, j_begin + (long long)size * kGroup);
   const int first_row = range.len - a.T;   // row of query 0
@@ -336,15 +342,15 @@ __global__ __launch_bounds__(64 * kWaves, NB <= 2 ? 2 : 1) void decode_kernel(Fm
     }
     const auto entry_of = [&](int s) { return a.bounds[0] ? __builtin_amdgcn_readfirstlane(sh.list[s]) : s * 4; };
 
-    if (wave < steps) {
-      int entry = entry_of(wave);
+    if (team_wave < steps && !idle) {
+      int entry = entry_of(team_wave);
       Step now = pages_of(panel + entry / 4 * C::KEYS);
       load_k(now);
       load_v(now);
-      int next_entry = wave + kWaves < steps ? entry_of(wave + kWaves) : entry;
+      int next_entry = team_wave + TW < steps ? entry_of(team_wave + TW) : entry;
       Step next = pages_of(panel + next_entry / 4 * C::KEYS);
-      for (int s = wave; s < steps; s += kWaves) {
-        const bool more = s + kWaves < steps;
+      for (int s = team_wave; s < steps; s += TW) {
+        const bool more = s + TW < steps;
         const int start = panel + entry / 4 * C::KEYS;
         bool masked = (entry & 2) || start + C::KEYS > j_end || start + C::KEYS - 1 > first_row ||
                       (a.window > 0 && start <= range.len - 1 - a.window);
@@ -434,8 +440,10 @@ __global__ __launch_bounds__(64 * kWaves, NB <= 2 ? 2 : 1) void decode_kernel(Fm
               sum += p[nb][i][r];
             }
           l[nb] = l[nb] * alpha + sum;
+          if (__any(alpha != 1.f)) {   // seldom, after the first steps
 #pragma unroll
-          for (int e = 0; e < C::E; ++e) acc[nb][e] *= alpha;
+            for (int e = 0; e < C::E; ++e) acc[nb][e] *= alpha;
+          }
         }
 
         // products with the values
@@ -481,7 +489,7 @@ __global__ __launch_bounds__(64 * kWaves, NB <= 2 ? 2 : 1) void decode_kernel(Fm
         if (more) load_v(next);
         entry = next_entry;
         now = next;
-        next_entry = s + 2 * kWaves < steps ? entry_of(s + 2 * kWaves) : entry;
+        next_entry = s + 2 * TW < steps ? entry_of(s + 2 * TW) : entry;
         next = pages_of(panel + next_entry / 4 * C::KEYS);
       }
     }
@@ -495,13 +503,12 @@ __global__ __launch_bounds__(64 * kWaves, NB <= 2 ? 2 : 1) void decode_kernel(Fm
     continue;
   }
 
-  // The waves' sums meet in LDS, 16 rows at a time
-  constexpr int PER = 16 * D / (64 * kWaves);   // elements of a thread: neighbours of one row
-  const int my_row = threadIdx.x * PER / D, my_col = threadIdx.x * PER % D;
+  // A team's sums meet in LDS, 16 rows at a time
+  constexpr int PER = 16 * D / (64 * TW);   // elements of a thread: neighbours of one row
+  const int my_row = team_thread * PER / D, my_col = team_thread * PER % D;
   const float v_scale = E4M3 ? a.v_scale[hk] : 1.f;
 #pragma unroll
   for (int nb = 0; nb < NB; ++nb) {
-    if (rb * C::ROWS + nb * 16 >= R) break;
     const float sum = quad_sum(l[nb]);
     if (g == 0) sh.stat[wave][c] = float2{m[nb], sum};
 #pragma unroll
@@ -511,20 +518,21 @@ __global__ __launch_bounds__(64 * kWaves, NB <= 2 ? 2 : 1) void decode_kernel(Fm
         *(f32x4*)&sh.out[wave][c][4 * C::E * g + C::E * r + e] =
             f32x4{acc[nb][e][r], acc[nb][e + 1][r], acc[nb][e + 2][r], acc[nb][e + 3][r]};
     __syncthreads();
-    float top = -INFINITY, total = 0.f, weight[kWaves], x[PER];
+    float top = -INFINITY, total = 0.f, x[PER];
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) top = fmaxf(top, sh.stat[w][my_row].x);
+    for (int w = 0; w < TW; ++w) top = fmaxf(top, sh.stat[w * TEAMS + team][my_row].x);
 #pragma unroll
     for (int e = 0; e < PER; ++e) x[e] = 0.f;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-      weight[w] = fast_exp2(sh.stat[w][my_row].x - reference(top));
-      total += weight[w] * sh.stat[w][my_row].y;
+    for (int w = 0; w < TW; ++w) {
+      const float2 stat = sh.stat[w * TEAMS + team][my_row];
+      const float weight = fast_exp2(stat.x - reference(top));
+      total += weight * stat.y;
 #pragma unroll
-      for (int e = 0; e < PER; ++e) x[e] += weight[w] * sh.out[w][my_row][my_col + e];
+      for (int e = 0; e < PER; ++e) x[e] += weight * sh.out[w * TEAMS + team][my_row][my_col + e];
     }
     const int r = rb * C::ROWS + nb * 16 + my_row;
-    if (r < R && (only < 0 || r % a.T == only)) {
+    if (r < R && !idle && (only < 0 || r % a.T == only)) {
       if (chunks > 1) {
         const size_t at = ((size_t)(slot + chunk) * a.Hk + hk) * R + r;
 #pragma unroll
@@ -610,13 +618,25 @@ __global__ __launch_bounds__(256) void join_kernel(FmDecodeArgs a, FmDivisor row
 
 template <int D, bool F16, bool E4M3>
 static void launch(const FmDecodeArgs& a, hipStream_t stream) {
-  const FmDecodeCut cut = fm_decode_cut(a.H, a.Hk, a.T, D, a.B, fm_compute_units());
-  const int units = a.plan ? fm_most_units(a.chunks, a.B) : a.B, inner = cut.row_blocks * a.Hk;
-  const dim3 grid((unsigned)((units + 7) / 8 * 8 * inner)), block(64 * kWaves);
-  const FmDivisor di = fm_divisor(inner), dh = fm_divisor(a.Hk), dt = fm_divisor(a.T);
-  if (cut.block_rows == 16) hipLaunchKernelGGL((decode_kernel<D, F16, E4M3, 1>), grid, block, 0, stream, a, cut.row_blocks, di, dh, dt);
-  else if (cut.block_rows == 32) hipLaunchKernelGGL((decode_kernel<D, F16, E4M3, 2>), grid, block, 0, stream, a, cut.row_blocks, di, dh, dt);
-  else hipLaunchKernelGGL((decode_kernel<D, F16, E4M3, 4>), grid, block, 0, stream, a, cut.row_blocks, di, dh, dt);
+  const FmDecodeCut& cut = a.cut;
+  const int units = a.plan ? fm_most_units(cut.chunks, a.B) : a.B;
+  const dim3 grid((unsigned)((units + 7) / 8 * 8 * cut.workgroups)), block(64 * kWaves);
+  const FmDivisor di = fm_divisor(cut.workgroups), dr = fm_divisor(cut.row_blocks), dt = fm_divisor(a.T), dc = fm_divisor(cut.chunks);
+#define FM_DECODE(NB, TEAMS) \
+  hipLaunchKernelGGL((decode_kernel<D, F16, E4M3, NB, TEAMS>), grid, block, 0, stream, a, cut.row_blocks * a.Hk, di, dr, dt, dc)
+  if (cut.block_rows == 16) {
+    if constexpr (E4M3 && D == 64) {
+      if (cut.teams == 2) FM_DECODE(1, 2);
+      else FM_DECODE(1, 1);
+    } else {
+      FM_DECODE(1, 1);
+    }
+  } else if (cut.teams == 2) {
+    FM_DECODE(2, 2);
+  } else {
+    FM_DECODE(2, 1);
+  }
+#undef FM_DECODE
   if (a.plan) {
     const int R = a.H / a.Hk * a.T;
     hipLaunchKernelGGL((join_kernel<D, F16>), dim3(a.Hk * R, a.B), dim3(256), 0, stream, a, fm_divisor(R), dt);
@@ -625,13 +645,16 @@ static void launch(const FmDecodeArgs& a, hipStream_t stream) {
 
 }  // namespace fm
 
-FmDecodeCut fm_decode_cut(int H, int Hk, int T, int d, int B, int cus) {
+FmDecodeCut fm_decode_cut(int H, int Hk, int T, int d, int B, bool half_lines, int cus) {
   FmDecodeCut cut;
   const int R = H / Hk * T;
-  cut.block_rows = R <= 16 ? 16 : R <= 32 ? 32 : 64;
+  cut.block_rows = R <= 16 ? 16 : 32;
   cut.row_blocks = (R + cut.block_rows - 1) / cut.block_rows;
+  const int members = cut.row_blocks * Hk;
+  cut.teams = members > 1 && (cut.row_blocks > 1 || half_lines) ? 2 : 1;
+  cut.workgroups = (members + cut.teams - 1) / cut.teams;
   // two workgroups to a compute unit, a few rounds of them
-  const long long wanted = 4ll * (cus > 0 ? cus : 256) / ((long long)Hk * cut.row_blocks);
+  const long long wanted = 4ll * (cus > 0 ? cus : 256) / cut.workgroups;
   const long long bytes = (long long)Hk * R * (d + 2) * 4, room = (48ll << 20) / (2 * bytes);
   cut.chunks = (int)std::max<long long>(1, std::min(wanted, room));
   cut.slots = fm_most_slots(cut.chunks, B);

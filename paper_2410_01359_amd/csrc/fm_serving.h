@@ -45,6 +45,14 @@ struct FmAppendArgs {
 };
 hipError_t fm_launch_append(FmAppendArgs a, bool f16, bool e4m3, bool interleaved, hipStream_t stream);
 
+// How a call is cut for `cus` compute units.
+struct FmDecodeCut {
+  int row_blocks, block_rows;   // of the H / Hk * T query rows that share a K/V head
+  int teams, workgroups;        // heads and row blocks that a workgroup takes, workgroups to a chunk of keys
+  int chunks, slots;            // that all keys of a head are meant to be cut into; partial results of a head at most
+};
+// half_lines: rows of different heads lie in one 128-byte line.
+FmDecodeCut fm_decode_cut(int H, int Hk, int T, int d, int B, bool half_lines, int cus);
 struct FmDecodeArgs {
   const void* q;
   void* out;
@@ -61,14 +69,8 @@ struct FmDecodeArgs {
   int2* plan;
   float* part;
   float2* stat;
-  int chunks;             // chunks of keys that a head's work is meant to be cut into (FmDecodeCut)
+  FmDecodeCut cut;
 };
-// How the keys of a call are cut for `cus` compute units.
-struct FmDecodeCut {
-  int row_blocks, block_rows;   // of the H / Hk * T query rows that share a K/V head
-  int chunks, slots;            // of a head; partial results of a head at most
-};
-FmDecodeCut fm_decode_cut(int H, int Hk, int T, int d, int B, int cus);
 hipError_t fm_launch_decode(const FmDecodeArgs& a, bool f16, bool e4m3, hipStream_t stream);
 
 constexpr int FM_POOLS = 64;   // pools of one launch

@@ -78,7 +78,8 @@ struct DecodeSpace {
   size_t stat, part, total;   // behind the plan, which comes first
 };
 DecodeSpace decode_space(int sequences, int H, int Hk, int T, int d) {
-  const FmDecodeCut cut = fm_decode_cut(H, Hk, T, d, sequences, fm_compute_units());
+  // half lines, where they can be: the finer cut
+  const FmDecodeCut cut = fm_decode_cut(H, Hk, T, d, sequences, d == 64, fm_compute_units());
   const size_t rows = (size_t)cut.slots * H * T;
   DecodeSpace s;
   s.stat = ((size_t)sequences * sizeof(int2) + 255) / 256 * 256;
@@ -184,7 +185,8 @@ int flashmask_decode(const flashmask_cache* cache, const void* q, const int32_t*
   a.plan = split ? (int2*)ws : nullptr;
   a.stat = (float2*)(ws + space.stat);
   a.part = (float*)(ws + space.part);
-  a.chunks = fm_decode_cut(H, cache->heads, T, cache->d, cache->sequences, fm_compute_units()).chunks;
+  a.cut = fm_decode_cut(H, cache->heads, T, cache->d, cache->sequences,
+                        cache->type == FM_TYPE_E4M3 && cache->d == 64 && (a.k.head < 128 || a.v.head < 128), fm_compute_units());
   return done(fm_launch_decode(a, type == FM_TYPE_F16, cache->type == FM_TYPE_E4M3, (hipStream_t)hip_stream));
 }
 
