@@ -5,9 +5,6 @@
 
 // Keys are counted in groups of 16: pages hold whole groups.
 constexpr int FM_KEY_GROUP = 16;
-// Keys that a split sequence's chunk has at least.
-constexpr int FM_MIN_CHUNK = 512;
-
 // The page that a table entry names, -1: none.
 FM_HOST_DEVICE inline int fm_known_page(int entry, int num_pages) { return entry >= 0 && entry < num_pages ? entry : -1; }
 
@@ -40,10 +37,10 @@ FM_HOST_DEVICE inline FmKeyRange fm_key_range(int len, int T, int window, int ta
 }
 FM_HOST_DEVICE inline int fm_key_groups(const FmKeyRange& r) { return (r.hi - r.lo + FM_KEY_GROUP - 1) / FM_KEY_GROUP; }
 
-// Groups of a chunk where sequences of `total` groups together are meant to be cut into `chunks`: a multiple of `round`.
-FM_HOST_DEVICE inline int fm_chunk_groups(unsigned total, const FmDivisor& chunks, int round) {
+// Groups of a chunk where sequences of `total` groups together are meant to be cut into `chunks`: a multiple of `round`, at least `least`.
+FM_HOST_DEVICE inline int fm_chunk_groups(unsigned total, const FmDivisor& chunks, int least, int round) {
   unsigned size = fm_div((int)(total + chunks.n - 1), chunks);
-  if (size < FM_MIN_CHUNK / FM_KEY_GROUP) size = FM_MIN_CHUNK / FM_KEY_GROUP;
+  if (size < (unsigned)least) size = least;
   return (int)((size + round - 1) / round * round);
 }
 // Chunks of a sequence: at least one, so that somebody writes an empty sequence's rows.

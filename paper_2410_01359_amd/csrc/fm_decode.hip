@@ -139,14 +139,17 @@ struct Decode {
   };
 };
 
-// TEAMS = 2: the workgroup's waves are two teams that go over the same keys together, for two blocks of query rows, or for two heads
-// whose rows share cache lines: what one team loads the other finds in the caches.
+// TEAMS > 1: the workgroup's waves are teams that go over the same keys together, for blocks of query rows, which find in the caches what
+// the first of them loads, or for heads whose rows lie side by side.
 template <int D, bool F16, bool E4M3, int NB, int TEAMS>
 __global__ __launch_bounds__(64 * kWaves, 2) void decode_kernel(FmDecodeArgs a, int members, FmDivisor inner, FmDivisor row_blocks,
                                                               FmDivisor tokens, FmDivisor chunks_meant) {
   constexpr int TW = kWaves / TEAMS;   // waves of a team
   using C = Decode<D, F16, E4M3, NB>;
   __shared__ typename C::Shared sh;
+  // the launch arguments, read together: left where they are first needed, they are six round trips in a row
+  asm volatile("" ::"s"(a.plan), "s"(a.lens), "s"(a.B), "s"(a.T), "s"(a.window), "s"(a.columns), "s"(a.page_tokens), "s"(a.cut.least),
+               "s"(inner.factor), "s"(row_blocks.factor), "s"(chunks_meant.factor), "s"(members));
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int g = lane >> 4, c = lane & 15;
   // Workgroup -> chunk of a sequence, K/V head, block of query rows.  Workgroup x runs on XCD x % 8: all heads of a chunk on one,
@@ -159,22 +162,21 @@ __global__ __launch_bounds__(64 * kWaves, 2) void decode_kernel(FmDecodeArgs a, 
   const int member = idle ? members - 1 : pair * TEAMS + team;
   const int hk = fm_div(member, row_blocks), rb = member - hk * (int)row_blocks.n;
 
-  // Chunk: all sequences' keys together are cut into a.chunks pieces, each sequence into whole ones of that size.  Every wave works this
-  // out for itself, 64 sequences at a time; up to 64 their lengths are read once.
+  // Chunk: all sequences' keys together are cut into about a.cut.chunks pieces, each sequence into whole ones of that size.  Every wave works
+  // this out for itself, 64 sequences at a time; up to 64 their lengths are read once.
   int b = unit, chunk = 0, chunks = 1, slot = 0, size = INT32_MAX / 32, len;   // size: in groups
   if (a.plan) {
-    const auto groups_of = [&](int l) { return fm_key_groups(fm_key_range(l, a.T, a.window, a.columns * a.page_tokens)); };
+    int lane_len = lane < a.B ? a.lens[lane] : 0;
+    const auto lane_groups = [&](int base) {
+      if (a.B > 64) lane_len = base + lane < a.B ? a.lens[base + lane] : 0;
+      return fm_key_groups(fm_key_range(lane_len, a.T, a.window, a.columns * a.page_tokens));
+    };
     unsigned total = 0;
-    int lane_len = 0;
-    for (int base = 0; base < a.B; base += 64) {
-      lane_len = base + lane < a.B ? a.lens[base + lane] : 0;
-      total += wave_last(wave_scan(groups_of(lane_len)));
-    }
-    size = fm_chunk_groups(total, chunks_meant, TW * C::GROUPS);
+    for (int base = 0; base < a.B; base += 64) total += wave_last(wave_scan(lane_groups(base)));
+    size = fm_chunk_groups(total, chunks_meant, a.cut.least, TW * C::GROUPS);
     int units = 0, slots = 0, base = 0;
     while (true) {
-      if (a.B > 64) lane_len = base + lane < a.B ? a.lens[base + lane] : 0;
-      const int n = base + lane < a.B ? fm_chunks_of(groups_of(lane_len), size) : 0;
+      const int n = base + lane < a.B ? fm_chunks_of(lane_groups(base), size) : 0;
       const int upto = wave_scan(n), upto_slots = wave_scan(n > 1 ? n : 0);
       const unsigned long long behind = __ballot(units + upto > unit);
       if (behind) {
@@ -625,16 +627,11 @@ static void launch(const FmDecodeArgs& a, hipStream_t stream) {
 #define FM_DECODE(NB, TEAMS) \
   hipLaunchKernelGGL((decode_kernel<D, F16, E4M3, NB, TEAMS>), grid, block, 0, stream, a, cut.row_blocks * a.Hk, di, dr, dt, dc)
   if (cut.block_rows == 16) {
-    if constexpr (E4M3 && D == 64) {
-      if (cut.teams == 2) FM_DECODE(1, 2);
-      else FM_DECODE(1, 1);
-    } else {
-      FM_DECODE(1, 1);
-    }
-  } else if (cut.teams == 2) {
-    FM_DECODE(2, 2);
+    if (cut.teams == 2) FM_DECODE(1, 2);
+    else FM_DECODE(1, 1);
   } else {
-    FM_DECODE(2, 1);
+    if (cut.teams == 2) FM_DECODE(2, 2);
+    else FM_DECODE(2, 1);
   }
 #undef FM_DECODE
   if (a.plan) {
@@ -645,18 +642,23 @@ static void launch(const FmDecodeArgs& a, hipStream_t stream) {
 
 }  // namespace fm
 
-FmDecodeCut fm_decode_cut(int H, int Hk, int T, int d, int B, bool half_lines, int cus) {
+FmDecodeCut fm_decode_cut(int H, int Hk, int T, int d, int value_bytes, int B, int together, int cus) {
   FmDecodeCut cut;
   const int R = H / Hk * T;
   cut.block_rows = R <= 16 ? 16 : 32;
   cut.row_blocks = (R + cut.block_rows - 1) / cut.block_rows;
   const int members = cut.row_blocks * Hk;
-  cut.teams = members > 1 && (cut.row_blocks > 1 || half_lines) ? 2 : 1;
+  cut.teams = members > 1 && (together > 1 || cut.row_blocks > 1) ? 2 : 1;
   cut.workgroups = (members + cut.teams - 1) / cut.teams;
-  // two workgroups to a compute unit, a few rounds of them
-  const long long wanted = 4ll * (cus > 0 ? cus : 256) / cut.workgroups;
+  // Chunks that give every compute unit its two workgroups once are best where they come out even (131072 keys 102 us, twice as many
+  // 105; 16 sequences of 16384, d = 64, 102 and 107; 16 and 32 ragged ones the same).  Each sequence leaves half a chunk over
+  // on average, so for many sequences they are half as long (64 ragged ones of up to 8192, 8 heads, 104 and 88).  Partial results in
+  // 48 MiB, and 256 to a row, which its join goes through in a few steps.
+  const long long at_once = std::max(1, 2 * (cus > 0 ? cus : 256) / cut.workgroups), wanted = 2ll * B <= at_once ? at_once : 2 * at_once;
   const long long bytes = (long long)Hk * R * (d + 2) * 4, room = (48ll << 20) / (2 * bytes);
-  cut.chunks = (int)std::max<long long>(1, std::min(wanted, room));
+  cut.chunks = (int)std::max<long long>(1, std::min({wanted, room, 256ll}));
+  // Partial sums are written and read again in 32 bits: no more than a quarter of the keys and values of a chunk
+  cut.least = std::max(128 / FM_KEY_GROUP, 16 * R / value_bytes / FM_KEY_GROUP);
   cut.slots = fm_most_slots(cut.chunks, B);
   return cut;
 }

@@ -50,9 +50,10 @@ struct FmDecodeCut {
   int row_blocks, block_rows;   // of the H / Hk * T query rows that share a K/V head
   int teams, workgroups;        // heads and row blocks that a workgroup takes, workgroups to a chunk of keys
   int chunks, slots;            // that all keys of a head are meant to be cut into; partial results of a head at most
+  int least;                    // groups of keys of a chunk at least
 };
-// half_lines: rows of different heads lie in one 128-byte line.
-FmDecodeCut fm_decode_cut(int H, int Hk, int T, int d, int B, bool half_lines, int cus);
+// together: heads, 1 or 2, whose rows of a token make up a run of memory that is best read together.
+FmDecodeCut fm_decode_cut(int H, int Hk, int T, int d, int value_bytes, int B, int together, int cus);
 struct FmDecodeArgs {
   const void* q;
   void* out;

@@ -1,4 +1,6 @@
 // C ABI of the entry points around the attention call: argument validation, scratch, launches.
+#include <algorithm>
+
 #include "../../include/flashmask.h"
 #include "fm_serving.h"
 
@@ -77,9 +79,7 @@ int check_decode_shape(int sequences, int H, int Hk, int T, int d) {
 struct DecodeSpace {
   size_t stat, part, total;   // behind the plan, which comes first
 };
-DecodeSpace decode_space(int sequences, int H, int Hk, int T, int d) {
-  // half lines, where they can be: the finer cut
-  const FmDecodeCut cut = fm_decode_cut(H, Hk, T, d, sequences, d == 64, fm_compute_units());
+DecodeSpace decode_space(const FmDecodeCut& cut, int sequences, int H, int T, int d) {
   const size_t rows = (size_t)cut.slots * H * T;
   DecodeSpace s;
   s.stat = ((size_t)sequences * sizeof(int2) + 255) / 256 * 256;
@@ -87,8 +87,16 @@ DecodeSpace decode_space(int sequences, int H, int Hk, int T, int d) {
   s.total = s.part + rows * d * sizeof(float);
   return s;
 }
-// Sequences of tables up to this many keys are not split: one launch.
-constexpr long long kWholeKeys = 1024;
+// Of whatever cache.
+size_t decode_bytes(int sequences, int H, int Hk, int T, int d) {
+  size_t most = 0;
+  for (int together = 1; together <= 2; ++together)
+    most = std::max(most, decode_space(fm_decode_cut(H, Hk, T, d, 2, sequences, together, fm_compute_units()), sequences, H, T, d).total);
+  return most;
+}
+// Sequences of tables up to this many keys are not split: one launch.  A single sequence, 8 K/V heads, 384 / 512 / 1024 keys: 8.8 / 10.7 /
+// 17.6 us whole, 9.4 split; 16 of 768 / 1024: 16.0 / 19.0 and 16.3 / 18.5; 64 of 1024: 51.6 and 53.4, of up to 1024 (ragged) 22.6 and 21.0.
+long long whole_keys(int sequences, const FmDecodeCut& cut) { return std::min(1024ll, 320 + 3ll * sequences * cut.workgroups); }
 
 int check_pools(void* const* pools, int num_pools, size_t page_bytes, int num_pages) {
   if (num_pools < 0 || num_pages <= 0) return FM_ERR_SHAPE;
@@ -146,7 +154,7 @@ int flashmask_cache_append(const flashmask_cache* cache, const void* q, const vo
 }
 
 size_t flashmask_decode_workspace_bytes(int sequences, int H, int H_kv, int T, int d) {
-  return check_decode_shape(sequences, H, H_kv, T, d) == FM_OK ? decode_space(sequences, H, H_kv, T, d).total : 0;
+  return check_decode_shape(sequences, H, H_kv, T, d) == FM_OK ? decode_bytes(sequences, H, H_kv, T, d) : 0;
 }
 
 int flashmask_decode(const flashmask_cache* cache, const void* q, const int32_t* lens, const int32_t* lts,
@@ -165,8 +173,7 @@ int flashmask_decode(const flashmask_cache* cache, const void* q, const int32_t*
   for (const flashmask_strides* s : {sq, so})
     if (int rc = check_strides(*s, type, cache->sequences, H, T, cache->d)) return rc;
   if (misaligned(q) || misaligned(out)) return FM_ERR_ALIGN;
-  const DecodeSpace space = decode_space(cache->sequences, H, cache->heads, T, cache->d);
-  if (bad_workspace(workspace, workspace_bytes, space.total)) return FM_ERR_WORKSPACE;
+  if (bad_workspace(workspace, workspace_bytes, decode_bytes(cache->sequences, H, cache->heads, T, cache->d))) return FM_ERR_WORKSPACE;
   char* ws = (char*)workspace;
   FmDecodeArgs a;
   a.q = q; a.out = out; a.lse = lse; a.sq = to_kernel(*sq); a.so = to_kernel(*so);
@@ -181,12 +188,15 @@ int flashmask_decode(const flashmask_cache* cache, const void* q, const int32_t*
   a.bound_columns = bounds ? bound_columns : 0;
   a.window = window < (1 << 30) ? window : 0;   // no table holds more keys
   a.page = fm_divisor(cache->page);
-  const bool split = (long long)cache->columns * cache->page > kWholeKeys;
+  // Pages stored token by token have the rows of all heads side by side: a workgroup takes two of less than 256 bytes together.
+  const int row = cache->d * element_bytes(cache->type);
+  const bool side_by_side = a.k.head < 256 && a.v.head < 256;
+  a.cut = fm_decode_cut(H, cache->heads, T, cache->d, element_bytes(cache->type), cache->sequences, side_by_side && row < 256 ? 2 : 1, fm_compute_units());
+  const bool split = (long long)cache->columns * cache->page > whole_keys(cache->sequences, a.cut);
+  const DecodeSpace space = decode_space(a.cut, cache->sequences, H, T, cache->d);
   a.plan = split ? (int2*)ws : nullptr;
   a.stat = (float2*)(ws + space.stat);
   a.part = (float*)(ws + space.part);
-  a.cut = fm_decode_cut(H, cache->heads, T, cache->d, cache->sequences,
-                        cache->type == FM_TYPE_E4M3 && cache->d == 64 && (a.k.head < 128 || a.v.head < 128), fm_compute_units());
   return done(fm_launch_decode(a, type == FM_TYPE_F16, cache->type == FM_TYPE_E4M3, (hipStream_t)hip_stream));
 }
 

@@ -48,8 +48,8 @@ int main() {
     std::vector<int> groups(B);
     unsigned total = 0;
     for (int& g : groups) total += g = std::rand() % 5 ? (int)(((long long)std::rand() << 10 ^ std::rand()) % most) : 0;
-    const int size = fm_chunk_groups(total, fm_divisor(chunks), round);
-    CHECK(size % round == 0 && size * FM_KEY_GROUP >= FM_MIN_CHUNK);
+    const int least = 8 << std::rand() % 4, size = fm_chunk_groups(total, fm_divisor(chunks), least, round);
+    CHECK(size % round == 0 && size >= least);
     long long units = 0, slots = 0;
     for (int g : groups) {
       const int n = fm_chunks_of(g, size);
@@ -60,7 +60,7 @@ int main() {
     CHECK(units <= fm_most_units(chunks, B));
     CHECK(slots <= fm_most_slots(chunks, B));
   }
-  CHECK(fm_chunk_groups(1u << 30, fm_divisor(1), 64) >= 1 << 30);
+  CHECK(fm_chunk_groups(1u << 30, fm_divisor(1), 8, 64) >= 1 << 30);
   for (int page : {16, 48, 64})
     for (int len : {INT_MIN, -1, 0, 1, 15, 16, 17, 48, 95, 96, 128, INT_MAX}) {
       const FmFork f = fm_fork(len, fm_divisor(page));
