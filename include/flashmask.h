@@ -385,8 +385,8 @@ int flashmask_cache_append(const flashmask_cache* cache, const void* q, const vo
  *     j <= i,   j > i - window (window > 0),   and neither LTS[j] <= i < LTE[j] nor UTS[j] <= i < UTE[j].
  * out = softmax(scale * q K^T) V and lse as for flashmask_fwd; a row that sees nothing (a sequence shorter than T, an
  * empty one) gets 0 and -inf.  Keys that a row does not see have no influence on it, whatever they and their values hold.
- *   q, out      [sequences, H, T, d] of `type` (BF16, F16; that of the cache, or the cache is E4M3), strides sq, so; H is a
- *               multiple of cache->heads, query head h reads K/V head h / (H / heads)
+ *   q, out      [sequences, H, T, d] of `type` (BF16, F16; that of the cache, or the cache is E4M3); strides[2] describe q
+ *               and out; H is a multiple of cache->heads, query head h reads K/V head h / (H / heads)
  *   lens        int32 [sequences], values below 0 count as 0.  A key whose place has no page is not seen.
  *   lts..ute    int32 [sequences, bound_columns], all or none (NULL); keys from bound_columns on have no interval
  *   window      0: none; else the row and window - 1 keys before it
@@ -397,8 +397,8 @@ int flashmask_cache_append(const flashmask_cache* cache, const void* q, const vo
  */
 int flashmask_decode(const flashmask_cache* cache, const void* q, const int32_t* lens, const int32_t* lts,
                      const int32_t* lte, const int32_t* uts, const int32_t* ute, int bound_columns, int window, float scale,
-                     void* out, float* lse, int type, int H, int T, const flashmask_strides* sq,
-                     const flashmask_strides* so, void* workspace, size_t workspace_bytes, void* hip_stream);
+                     void* out, float* lse, int type, int H, int T, const flashmask_strides* strides, void* workspace,
+                     size_t workspace_bytes, void* hip_stream);
 /* Bytes of scratch of a call on `sequences` sequences, 0 for an invalid shape.  Host-only. */
 size_t flashmask_decode_workspace_bytes(int sequences, int H, int H_kv, int T, int d);
 

@@ -84,7 +84,7 @@ def load_library() -> ctypes.CDLL:
     lib.flashmask_cache_append.restype = i
     lib.flashmask_cache_append.argtypes = [vp, vp, vp, vp, vp, ip, ip, dp, i, i, db, i, i, i, vp, vp]
     lib.flashmask_decode.restype = i
-    lib.flashmask_decode.argtypes = [vp, vp, ip, ip, ip, ip, ip, i, i, f, vp, fp, i, i, i, vp, vp, vp, sz, vp]
+    lib.flashmask_decode.argtypes = [vp, vp, ip, ip, ip, ip, ip, i, i, f, vp, fp, i, i, i, vp, vp, sz, vp]
     lib.flashmask_decode_workspace_bytes.restype = sz
     lib.flashmask_decode_workspace_bytes.argtypes = [i, i, i, i, i]
     lib.flashmask_cache_fork.restype = i

@@ -159,10 +159,10 @@ size_t flashmask_decode_workspace_bytes(int sequences, int H, int H_kv, int T, i
 
 int flashmask_decode(const flashmask_cache* cache, const void* q, const int32_t* lens, const int32_t* lts,
                      const int32_t* lte, const int32_t* uts, const int32_t* ute, int bound_columns, int window, float scale,
-                     void* out, float* lse, int type, int H, int T, const flashmask_strides* sq,
-                     const flashmask_strides* so, void* workspace, size_t workspace_bytes, void* hip_stream) {
+                     void* out, float* lse, int type, int H, int T, const flashmask_strides* strides, void* workspace,
+                     size_t workspace_bytes, void* hip_stream) {
   if (int rc = check_cache(cache)) return rc;
-  if (!q || !lens || !out || !lse || !sq || !so) return FM_ERR_NULL;
+  if (!q || !lens || !out || !lse || !strides) return FM_ERR_NULL;
   const bool bounds = lts || lte || uts || ute;
   if (bounds && (!lts || !lte || !uts || !ute)) return FM_ERR_NULL;
   if (int rc = check_row_type(type, *cache)) return rc;
@@ -170,13 +170,13 @@ int flashmask_decode(const flashmask_cache* cache, const void* q, const int32_t*
   if (bounds && bound_columns <= 0) return FM_ERR_SHAPE;
   if ((long long)cache->sequences * cache->columns * cache->page > 1ll << 34) return FM_ERR_SHAPE;   // groups of 16 keys are added up in 32 bits
   if (!(scale > 0.f) || !(scale < 3.0e38f) || window < 0) return FM_ERR_ARG;
-  for (const flashmask_strides* s : {sq, so})
-    if (int rc = check_strides(*s, type, cache->sequences, H, T, cache->d)) return rc;
+  for (int t = 0; t < 2; ++t)
+    if (int rc = check_strides(strides[t], type, cache->sequences, H, T, cache->d)) return rc;
   if (misaligned(q) || misaligned(out)) return FM_ERR_ALIGN;
   if (bad_workspace(workspace, workspace_bytes, decode_bytes(cache->sequences, H, cache->heads, T, cache->d))) return FM_ERR_WORKSPACE;
   char* ws = (char*)workspace;
   FmDecodeArgs a;
-  a.q = q; a.out = out; a.lse = lse; a.sq = to_kernel(*sq); a.so = to_kernel(*so);
+  a.q = q; a.out = out; a.lse = lse; a.sq = to_kernel(strides[0]); a.so = to_kernel(strides[1]);
   a.k = pages(cache->k, cache->sk, cache->type);
   a.v = pages(cache->v, cache->sv, cache->type);
   a.k_scale = cache->k_scale; a.v_scale = cache->v_scale;

@@ -49,7 +49,7 @@ def _append(cache=None, q=P, k=P, v=P, qo=P, seqs=P, positions=P, freqs=P, type=
 def _decode(cache=None, q=P, lens=P, bounds=(None,) * 4, columns=0, window=0, scale=0.1, out=P, lse=P, type=BF16, H=16, T=2,
             sq=(4096, 256, 128), so=(4096, 256, 128), workspace=P, nbytes=1 << 40):
     return fm.load_library().flashmask_decode(_cache() if cache is None else cache, q, lens, *bounds, columns, window, scale, out, lse, type,
-                                              H, T, _longs(*sq), _longs(*so), workspace, nbytes, None)
+                                              H, T, _longs(*sq, *so), workspace, nbytes, None)
 
 
 @pytest.mark.parametrize("call", [_append, _decode])
