@@ -147,7 +147,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void decode_kernel(FmDecodeArgs a, 
   constexpr int TW = kWaves / TEAMS;   // waves of a team
   using C = Decode<D, F16, E4M3, NB>;
   __shared__ typename C::Shared sh;
-  // the launch arguments, read together: left where they are first needed, they are six round trips in a row
+  // Barriers here order LDS alone (barrier_nofence): loads stay in flight across them.  The launch arguments are read together: left where they are first needed, they are six round trips in a row
   asm volatile("" ::"s"(a.plan), "s"(a.lens), "s"(a.B), "s"(a.T), "s"(a.window), "s"(a.columns), "s"(a.page_tokens), "s"(a.cut.least),
                "s"(inner.factor), "s"(row_blocks.factor), "s"(chunks_meant.factor), "s"(members));
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -303,7 +303,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void decode_kernel(FmDecodeArgs a, 
 #pragma unroll
     for (int e = 0; e < C::E; ++e) acc[nb][e] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
-  __syncthreads();
+  barrier_nofence();
 
   for (int panel = j_begin; panel < j_end; panel += a.bounds[0] ? C::PANEL : INT32_MAX / 2) {
     int steps;
@@ -311,7 +311,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void decode_kernel(FmDecodeArgs a, 
       // the steps of which some row sees a key, and whether it takes the element mask
       const int end = min(j_end, panel + C::PANEL), all = (end - panel + C::KEYS - 1) / C::KEYS;
       for (int i = threadIdx.x; i < all; i += 64 * kWaves) sh.flag[i] = 0;
-      __syncthreads();
+      barrier_nofence();
       for (int j = panel + threadIdx.x; j < end; j += 64 * kWaves) {
         i32x4 bound = {0, 0, 0, 0};
         if (j < a.bound_columns) {
@@ -326,7 +326,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void decode_kernel(FmDecodeArgs a, 
         }
         atomicOr(&sh.flag[(j - panel) / C::KEYS], flag);
       }
-      __syncthreads();
+      barrier_nofence();
       if (wave == 0) {
         int count = 0;
         for (int base = 0; base < all; base += 64) {
@@ -337,7 +337,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void decode_kernel(FmDecodeArgs a, 
         }
         if (lane == 0) sh.count = count;
       }
-      __syncthreads();
+      barrier_nofence();
       steps = sh.count;
     } else {
       steps = (j_end - panel + C::KEYS - 1) / C::KEYS;
@@ -495,10 +495,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void decode_kernel(FmDecodeArgs a, 
         next = pages_of(panel + next_entry / 4 * C::KEYS);
       }
     }
-    if (a.bounds[0]) __syncthreads();
+    if (a.bounds[0]) barrier_nofence();
   }
 
-  __syncthreads();
+  barrier_nofence();
   if (only < 0 && sh.odd) {
     only = 0;
     rounds = a.T + 1;
@@ -519,7 +519,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void decode_kernel(FmDecodeArgs a, 
       for (int e = 0; e < C::E; e += 4)
         *(f32x4*)&sh.out[wave][c][4 * C::E * g + C::E * r + e] =
             f32x4{acc[nb][e][r], acc[nb][e + 1][r], acc[nb][e + 2][r], acc[nb][e + 3][r]};
-    __syncthreads();
+    barrier_nofence();
     float top = -INFINITY, total = 0.f, x[PER];
 #pragma unroll
     for (int w = 0; w < TW; ++w) top = fmaxf(top, sh.stat[w * TEAMS + team][my_row].x);
@@ -549,7 +549,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void decode_kernel(FmDecodeArgs a, 
         if (my_col == 0) a.lse[((size_t)b * a.H + h) * a.T + t] = total == 0.f ? -INFINITY : (top + fast_log2(total * kUnshift<F16>)) * kLn2;
       }
     }
-    __syncthreads();
+    barrier_nofence();
   }
   if (only >= 0) ++only;
   }
@@ -642,7 +642,7 @@ static void launch(const FmDecodeArgs& a, hipStream_t stream) {
 
 }  // namespace fm
 
-FmDecodeCut fm_decode_cut(int H, int Hk, int T, int d, int value_bytes, int B, int together, int cus) {
+FmDecodeCut fm_decode_cut(int H, int Hk, int T, int d, int B, int together, int cus) {
   FmDecodeCut cut;
   const int R = H / Hk * T;
   cut.block_rows = R <= 16 ? 16 : 32;
@@ -657,8 +657,9 @@ FmDecodeCut fm_decode_cut(int H, int Hk, int T, int d, int value_bytes, int B, i
   const long long at_once = std::max(1, 2 * (cus > 0 ? cus : 256) / cut.workgroups), wanted = 2ll * B <= at_once ? at_once : 2 * at_once;
   const long long bytes = (long long)Hk * R * (d + 2) * 4, room = (48ll << 20) / (2 * bytes);
   cut.chunks = (int)std::max<long long>(1, std::min({wanted, room, 256ll}));
-  // Partial sums are written and read again in 32 bits: no more than a quarter of the keys and values of a chunk
-  cut.least = std::max(128 / FM_KEY_GROUP, 16 * R / value_bytes / FM_KEY_GROUP);
+  // A chunk's partial sums cost a join more per query row than a key does: 8 keys to a row at least (64 rows, 16 ragged sequences of up to 8192,
+  // 43 us, with 4 and 16 keys 53 and 48), and two steps of the workgroup.
+  cut.least = std::max(128, 8 * R) / FM_KEY_GROUP;
   cut.slots = fm_most_slots(cut.chunks, B);
   return cut;
 }

@@ -53,7 +53,7 @@ struct FmDecodeCut {
   int least;                    // groups of keys of a chunk at least
 };
 // together: heads, 1 or 2, whose rows of a token make up a run of memory that is best read together.
-FmDecodeCut fm_decode_cut(int H, int Hk, int T, int d, int value_bytes, int B, int together, int cus);
+FmDecodeCut fm_decode_cut(int H, int Hk, int T, int d, int B, int together, int cus);
 struct FmDecodeArgs {
   const void* q;
   void* out;

@@ -91,7 +91,7 @@ DecodeSpace decode_space(const FmDecodeCut& cut, int sequences, int H, int T, in
 size_t decode_bytes(int sequences, int H, int Hk, int T, int d) {
   size_t most = 0;
   for (int together = 1; together <= 2; ++together)
-    most = std::max(most, decode_space(fm_decode_cut(H, Hk, T, d, 2, sequences, together, fm_compute_units()), sequences, H, T, d).total);
+    most = std::max(most, decode_space(fm_decode_cut(H, Hk, T, d, sequences, together, fm_compute_units()), sequences, H, T, d).total);
   return most;
 }
 // Sequences of tables up to this many keys are not split: one launch.  A single sequence, 8 K/V heads, 384 / 512 / 1024 keys: 8.8 / 10.7 /
@@ -191,7 +191,7 @@ int flashmask_decode(const flashmask_cache* cache, const void* q, const int32_t*
   // Pages stored token by token have the rows of all heads side by side: a workgroup takes two of less than 256 bytes together.
   const int row = cache->d * element_bytes(cache->type);
   const bool side_by_side = a.k.head < 256 && a.v.head < 256;
-  a.cut = fm_decode_cut(H, cache->heads, T, cache->d, element_bytes(cache->type), cache->sequences, side_by_side && row < 256 ? 2 : 1, fm_compute_units());
+  a.cut = fm_decode_cut(H, cache->heads, T, cache->d, cache->sequences, side_by_side && row < 256 ? 2 : 1, fm_compute_units());
   const bool split = (long long)cache->columns * cache->page > whole_keys(cache->sequences, a.cut);
   const DecodeSpace space = decode_space(a.cut, cache->sequences, H, T, cache->d);
   a.plan = split ? (int2*)ws : nullptr;
