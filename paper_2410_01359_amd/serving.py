@@ -104,19 +104,24 @@ def flashmask_rope_bwd(dq, dk, freqs, positions=None, *, layout: int = FM_ROPE_H
 
 
 def _cache(k_cache, v_cache, table, k_scale, v_scale, device: int):
-    """flashmask_cache as bytes, and its heads, d and type."""
-    dtype = k_cache.dtype
-    type_id = _CACHE_TYPE.get(dtype)
-    if type_id is None:
-        _wrong(k_cache, "k_cache", device, tuple(_CACHE_TYPE))
-    pages, heads, page, d = shape = _dims(k_cache, 4, "k_cache")
-    sk, sv = _rows(k_cache, shape, dtype, "k_cache", device), _rows(v_cache, shape, dtype, "v_cache", device)
-    sequences, columns = entries = _dims(table, 2, "table")
-    scales = (0, 0)
+    """flashmask_cache as bytes, and its heads, d and sequences."""
+    dtype, shape, entries = k_cache.dtype, k_cache.shape, table.shape
+    type_id, sk, sv = _CACHE_TYPE.get(dtype), k_cache.stride(), v_cache.stride()
+    if not (type_id is not None and len(shape) == 4 and v_cache.shape == shape and v_cache.dtype is dtype and sk[3] == 1 and sv[3] == 1
+            and len(entries) == 2 and table.dtype is torch.int32 and table.is_contiguous()
+            and k_cache.get_device() == v_cache.get_device() == table.get_device() == device):
+        _dims(k_cache, 4, "k_cache")
+        for t, name, types, want in ((k_cache, "k_cache", tuple(_CACHE_TYPE), shape), (v_cache, "v_cache", (dtype,), shape),
+                                     (table, "table", (torch.int32,), _dims(table, 2, "table"))):
+            if t.dtype not in types or t.shape != want or t.get_device() != device or t.stride()[-1] != 1 or t is table and not t.is_contiguous():
+                _wrong(t, name, device, types, want)
+    pages, heads, page, d = shape
+    sequences, columns = entries
+    k_at = v_at = 0
     if k_scale is not None or v_scale is not None:
-        scales = [_vector(s, heads, torch.float32, n, device) for s, n in ((k_scale, "k_scale"), (v_scale, "v_scale"))]
-    return (_CACHE.pack(k_cache.data_ptr(), v_cache.data_ptr(), sk[0], sk[1], sk[2], sv[0], sv[1], sv[2], *scales,
-                        _index(table, entries, "table", device), type_id, heads, d, pages, page, sequences, columns), heads, d)
+        k_at, v_at = (_vector(s, heads, torch.float32, n, device) for s, n in ((k_scale, "k_scale"), (v_scale, "v_scale")))
+    return (_CACHE.pack(k_cache.data_ptr(), v_cache.data_ptr(), sk[0], sk[1], sk[2], sv[0], sv[1], sv[2], k_at, v_at, table.data_ptr(),
+                        type_id, heads, d, pages, page, sequences, columns), heads, d, sequences)
 
 
 def flashmask_cache_append(k, v, k_cache, v_cache, table, seqs, positions, *, q=None, freqs=None, layout: int = FM_ROPE_HALF,
@@ -128,7 +133,7 @@ def flashmask_cache_append(k, v, k_cache, v_cache, table, seqs, positions, *, q=
     type_id = _ROW_TYPE.get(dtype)
     if type_id is None:
         _wrong(k, "k", device, tuple(_ROW_TYPE))
-    cache, heads, d = _cache(k_cache, v_cache, table, k_scale, v_scale, device)
+    cache, heads, d, _ = _cache(k_cache, v_cache, table, k_scale, v_scale, device)
     n = _dims(k, 3, "k")[0]
     sk, sv = _rows(k, (n, heads, d), dtype, "k", device), _rows(v, (n, heads, d), dtype, "v", device)
     seqs_at, positions_at = _index(seqs, (n,), "seqs", device), _index(positions, (n,), "positions", device)
@@ -163,9 +168,9 @@ def flashmask_decode(q, k_cache, v_cache, table, lens, scale: float, *, bounds=N
     type_id = _ROW_TYPE.get(dtype)
     if type_id is None:
         _wrong(q, "q", device, tuple(_ROW_TYPE))
-    cache, heads, d = _cache(k_cache, v_cache, table, k_scale, v_scale, device)
+    cache, heads, d, sequences = _cache(k_cache, v_cache, table, k_scale, v_scale, device)
     B, H, T, _ = _dims(q, 4, "q")
-    sq = _rows(q, (table.shape[0], H, T, d), dtype, "q", device)
+    sq = _rows(q, (sequences, H, T, d), dtype, "q", device)
     lens_at = _index(lens, (B,), "lens", device)
     at, columns = (0, 0, 0, 0), 0
     if bounds is not None:
@@ -185,6 +190,10 @@ def flashmask_decode(q, k_cache, v_cache, table, lens, scale: float, *, bounds=N
                                 _TWO.pack(sq[0], sq[1], sq[2], so[0], so[1], so[2]), workspace.data_ptr(),
                                 workspace.numel() * workspace.element_size(), _stream()), "flashmask_decode")
     return out, lse
+
+
+def _ints(like, *shape):
+    return torch.empty(*shape, dtype=torch.int32, device=like.device)
 
 
 def _pools(pools):
@@ -221,7 +230,7 @@ def flashmask_cache_fork(pools, table, lens, parents, new_pages, page: int):
     children = _dims(parents, 1, "parents")[0]
     at = (_index(table, entries, "table", device), _index(lens, (B,), "lens", device),
           _index(parents, (children,), "parents", device), _index(new_pages, (children,), "new_pages", device))
-    table_out, lens_out = table.new_empty((children, columns)), lens.new_empty(children)
+    table_out, lens_out = _ints(table, children, columns), _ints(table, children)
     _check(load_library().flashmask_cache_fork(where, n, page_bytes, num_pages, *at, table_out.data_ptr(), lens_out.data_ptr(), B,
                                                columns, page, children, _stream()), "flashmask_cache_fork")
     return table_out, lens_out
@@ -248,7 +257,7 @@ def flashmask_cache_free_list(table, num_pages: int, workspace: torch.Tensor | N
         raise FlashMaskError("num_pages must be positive")
     lib = load_library()
     ws = _plan(lib, num_pages, table, workspace, device)
-    free, count = table.new_empty(num_pages), table.new_empty(1)
+    free, count = _ints(table, num_pages), _ints(table, 1)
     _check(lib.flashmask_cache_free_list(at, table.numel(), num_pages, free.data_ptr(), count.data_ptr(), ws.data_ptr(),
                                          ws.numel() * ws.element_size(), _stream()), "flashmask_cache_free_list")
     return free, count
@@ -261,7 +270,7 @@ def flashmask_cache_compact(pools, table, workspace: torch.Tensor | None = None)
     at = _index(table, table.shape, "table", device)
     lib = load_library()
     ws = _plan(lib, num_pages, table, workspace, device)
-    table_out, used = torch.empty_like(table), table.new_empty(1)
+    table_out, used = torch.empty_like(table), _ints(table, 1)
     _check(lib.flashmask_cache_compact(where, n, page_bytes, num_pages, at, table.numel(), table_out.data_ptr(), used.data_ptr(),
                                        ws.data_ptr(), ws.numel() * ws.element_size(), _stream()), "flashmask_cache_compact")
     return table_out, used
