@@ -22,6 +22,8 @@ typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
 typedef __attribute__((ext_vector_type(2))) _Float16 f16x2;
 typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 
+#define FM_CONSTANT __attribute__((address_space(4)))
+
 constexpr int kGroup = FM_KEY_GROUP;
 constexpr int kWaves = 4;
 
@@ -228,42 +230,58 @@ __global__ __launch_bounds__(64 * kWaves, 2) void decode_kernel(FmDecodeArgs a, 
   const char* k_head = a.k.base + (long long)hk * a.k.head;
   const char* v_head = a.v.base + (long long)hk * a.v.head;
   const unsigned k_lane = c * a.k.token + 16 * g, v_lane = 4 * g * a.v.token + c * (C::E * C::BYTES);
-  const int* row = a.table + (size_t)b * a.columns;
+  // read through the scalar cache (nothing here writes the table): a vector load would return behind the keys and values asked for before it
+  const FM_CONSTANT int* row = (const FM_CONSTANT int*)(a.table + (size_t)b * a.columns);
 
-  // The pages of a step's groups: -1 where there is none, or no key
+  // A step's groups: their table entries, as read (a step ahead: nothing waits for them here), and slots, -1 behind the last key
   struct Step {
-    int page[C::GROUPS], slot[C::GROUPS];
+    int entry[C::GROUPS], slot[C::GROUPS];
+    int num_pages;
+    __device__ __forceinline__ int page(int i) const { return fm_known_page(slot[i] < 0 ? -1 : entry[i], num_pages); }
   };
   const auto pages_of = [&](int start) {
     Step p;
+    p.num_pages = a.num_pages;
 #pragma unroll
     for (int i = 0; i < C::GROUPS; ++i) {
-      const int key = start + i * kGroup;
-      const bool there = key < j_end;
-      const int at = there ? key : j_begin;
-      const int column = fm_div(at, a.page);
-      const int page = fm_known_page(__builtin_amdgcn_readfirstlane(row[column]), a.num_pages);
-      p.slot[i] = at - column * (int)a.page.n;
-      p.page[i] = there ? page : -1;
+      const int key = start + i * kGroup, at = key < j_end ? key : j_begin, column = fm_div(at, a.page);
+      p.entry[i] = row[column];
+      p.slot[i] = key < j_end ? at - column * (int)a.page.n : -1;
     }
     return p;
   };
   u32x4 kraw[C::GROUPS][C::KLOADS];
   typename C::vpiece vraw[C::KT][8];
-  const auto load_k = [&](const Step& p) {
+  // Through buffer descriptors of no bytes where there is no page (its sign is set), or no step (`there` = 0, not -1): such loads give 0 and
+  // touch no memory, and the loop's loads need no branch, behind which the compiler would wait for all of them at the first
+  // use of any.
+  const auto descriptor = [](const char* base, int page, int there) {
+    return __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, __builtin_amdgcn_readfirstlane(~(page >> 31) & there), 0x00020000);
+  };
+  const auto load_k = [&](const Step& p, int there) {
 #pragma unroll
     for (int i = 0; i < C::GROUPS; ++i) {
-      const char* base = k_head + std::max(p.page[i], 0) * a.k.page + (unsigned)p.slot[i] * (unsigned long long)a.k.token;
+      const int page = p.page(i);
+      const auto rows = descriptor(k_head + std::max(page, 0) * a.k.page + (unsigned)std::max(p.slot[i], 0) * (unsigned long long)a.k.token,
+                                   page, there);
 #pragma unroll
-      for (int s = 0; s < C::KLOADS; ++s) kraw[i][s] = ldg16(base + k_lane + 64 * s);
+      for (int s = 0; s < C::KLOADS; ++s)
+        kraw[i][s] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rows, k_lane + 64 * s, 0, 0));
     }
   };
-  const auto load_v = [&](const Step& p) {
+  const auto load_v = [&](const Step& p, int there) {
 #pragma unroll
     for (int i = 0; i < C::GROUPS; ++i) {
-      const char* base = v_head + std::max(p.page[i], 0) * a.v.page + (unsigned)p.slot[i] * (unsigned long long)a.v.token;
+      const int page = p.page(i);
+      const auto rows = descriptor(v_head + std::max(page, 0) * a.v.page + (unsigned)std::max(p.slot[i], 0) * (unsigned long long)a.v.token,
+                                   page, there);
 #pragma unroll
-      for (int t = 0; t < 4; ++t) vraw[i / 2][i % 2 * 4 + t] = *(const typename C::vpiece*)(base + t * a.v.token + v_lane);
+      for (int t = 0; t < 4; ++t) {
+        typename C::vpiece& x = vraw[i / 2][i % 2 * 4 + t];
+        if constexpr (C::VWORDS == 4) x = __builtin_bit_cast(typename C::vpiece, __builtin_amdgcn_raw_buffer_load_b128(rows, v_lane, t * a.v.token, 0));
+        else if constexpr (C::VWORDS == 2) x = __builtin_bit_cast(typename C::vpiece, __builtin_amdgcn_raw_buffer_load_b64(rows, v_lane, t * a.v.token, 0));
+        else x[0] = __builtin_amdgcn_raw_buffer_load_b32(rows, v_lane, t * a.v.token, 0);
+      }
     }
   };
 
@@ -338,7 +356,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void decode_kernel(FmDecodeArgs a, 
         if (lane == 0) sh.count = count;
       }
       barrier_nofence();
-      steps = sh.count;
+      steps = __builtin_amdgcn_readfirstlane(sh.count);
     } else {
       steps = (j_end - panel + C::KEYS - 1) / C::KEYS;
     }
@@ -347,17 +365,17 @@ __global__ __launch_bounds__(64 * kWaves, 2) void decode_kernel(FmDecodeArgs a, 
     if (team_wave < steps && !idle) {
       int entry = entry_of(team_wave);
       Step now = pages_of(panel + entry / 4 * C::KEYS);
-      load_k(now);
-      load_v(now);
+      load_k(now, -1);
+      load_v(now, -1);
       int next_entry = team_wave + TW < steps ? entry_of(team_wave + TW) : entry;
       Step next = pages_of(panel + next_entry / 4 * C::KEYS);
       for (int s = team_wave; s < steps; s += TW) {
-        const bool more = s + TW < steps;
+        const int more = (s + TW - steps) >> 31;   // -1: another step follows
         const int start = panel + entry / 4 * C::KEYS;
         bool masked = (entry & 2) || start + C::KEYS > j_end || start + C::KEYS - 1 > first_row ||
                       (a.window > 0 && start <= range.len - 1 - a.window);
 #pragma unroll
-        for (int i = 0; i < C::GROUPS; ++i) masked |= now.page[i] < 0;
+        for (int i = 0; i < C::GROUPS; ++i) masked |= now.page(i) < 0;
 
         // scores
         f32x4 p[NB][C::GROUPS];
@@ -379,7 +397,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void decode_kernel(FmDecodeArgs a, 
             for (int nb = 0; nb < NB; ++nb) p[nb][i] = mfma_keys<F16>(op, q[nb][k], p[nb][i]);
           }
         }
-        if (more) load_k(next);
+        load_k(next, more);
 
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb)
@@ -391,7 +409,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void decode_kernel(FmDecodeArgs a, 
         if (masked) {
           unsigned pages_there = 0;
 #pragma unroll
-          for (int i = 0; i < C::GROUPS; ++i) pages_there |= (now.page[i] >= 0 ? 1u : 0u) << i;
+          for (int i = 0; i < C::GROUPS; ++i) pages_there |= (now.page(i) >= 0 ? 1u : 0u) << i;
           unsigned any = 0, every = ~0u;
 #pragma unroll
           for (int nb = 0; nb < NB; ++nb) {
@@ -488,7 +506,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void decode_kernel(FmDecodeArgs a, 
             }
           }
         }
-        if (more) load_v(next);
+        load_v(next, more);
         entry = next_entry;
         now = next;
         next_entry = s + 2 * TW < steps ? entry_of(s + 2 * TW) : entry;
@@ -499,7 +517,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void decode_kernel(FmDecodeArgs a, 
   }
 
   barrier_nofence();
-  if (only < 0 && sh.odd) {
+  if (only < 0 && __builtin_amdgcn_readfirstlane(sh.odd)) {
     only = 0;
     rounds = a.T + 1;
     continue;
