@@ -380,7 +380,7 @@ int flashmask_cache_append(const flashmask_cache* cache, const void* q, const vo
                            double amp, int tokens, int H, int rot, const flashmask_strides* strides, void* hip_stream);
 
 /*
- * Attention of the last T tokens of every sequence over the cache, which holds lens[b] tokens of it, the new ones among them:
+ * Attention of the last T (1 to 256) tokens of every sequence over the cache, which holds lens[b] tokens of it, the new ones among them:
  * query t is row i = lens[b] - T + t and sees key j iff
  *     j <= i,   j > i - window (window > 0),   and neither LTS[j] <= i < LTE[j] nor UTS[j] <= i < UTE[j].
  * out = softmax(scale * q K^T) V and lse as for flashmask_fwd; a row that sees nothing (a sequence shorter than T, an

@@ -10,7 +10,9 @@
 //  - V: lane (g, c) loads the same piece of d (D / 16 elements, piece c) of the eight keys whose probabilities it holds of its
 //    column, and the eight 16-bit values of each element are gathered by byte permutes: product e has as its rows the
 //    elements D / 16 * m + e, m = 0..15.  The lane's results are then 4 * D / 16 consecutive elements of its query's row.
-// The probabilities go into the second product as sums of two 16-bit values, which the matrix pipe has room for: the loop is bound by memory (each wave keeps 16 KiB of keys and values in flight).
+// The probabilities go into the second product as sums of two 16-bit values, which the matrix pipe has room for.
+// Bound by memory: every wave has the next step's 16 KiB of keys and values in flight while it works on this one's.  131072 tokens, 8
+// heads of 128 elements: 96 us, 5.6 TB/s of the 6.4 that a plain reading loop reaches here, and 5 for the join.
 #include <algorithm>
 
 #include "fm_common.h"
@@ -149,7 +151,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void decode_kernel(FmDecodeArgs a, 
   constexpr int TW = kWaves / TEAMS;   // waves of a team
   using C = Decode<D, F16, E4M3, NB>;
   __shared__ typename C::Shared sh;
-  // Barriers here order LDS alone (barrier_nofence): loads stay in flight across them.  The launch arguments are read together: left where they are first needed, they are six round trips in a row
+  // Barriers here order LDS alone (barrier_nofence): loads stay in flight across them.
+  // The launch arguments that come first, read together: left where they are first needed they are six round trips in a row.
   asm volatile("" ::"s"(a.plan), "s"(a.lens), "s"(a.B), "s"(a.T), "s"(a.window), "s"(a.columns), "s"(a.page_tokens), "s"(a.cut.least),
                "s"(inner.factor), "s"(row_blocks.factor), "s"(chunks_meant.factor), "s"(members));
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -229,8 +232,12 @@ __global__ __launch_bounds__(64 * kWaves, 2) void decode_kernel(FmDecodeArgs a, 
   // Where the lane's pieces of a group of keys lie
   const char* k_head = a.k.base + (long long)hk * a.k.head;
   const char* v_head = a.v.base + (long long)hk * a.v.head;
-  const unsigned k_lane = c * a.k.token + 16 * g, v_lane = 4 * g * a.v.token + c * (C::E * C::BYTES);
-  // read through the scalar cache (nothing here writes the table): a vector load would return behind the keys and values asked for before it
+  const unsigned k_lane = c * a.k.token + 16 * g;
+  unsigned v_lane[4];
+#pragma unroll
+  for (int t = 0; t < 4; ++t) v_lane[t] = (4 * g + t) * a.v.token + c * (C::E * C::BYTES);
+  // The table is read through the scalar cache (nothing here writes it): a vector load would come back behind the keys and values asked
+  // for before it, and waiting for it meant waiting for them (64 ragged sequences 88 -> 81 us).
   const FM_CONSTANT int* row = (const FM_CONSTANT int*)(a.table + (size_t)b * a.columns);
 
   // A step's groups: their table entries, as read (a step ahead: nothing waits for them here), and slots, -1 behind the last key
@@ -278,9 +285,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void decode_kernel(FmDecodeArgs a, 
 #pragma unroll
       for (int t = 0; t < 4; ++t) {
         typename C::vpiece& x = vraw[i / 2][i % 2 * 4 + t];
-        if constexpr (C::VWORDS == 4) x = __builtin_bit_cast(typename C::vpiece, __builtin_amdgcn_raw_buffer_load_b128(rows, v_lane, t * a.v.token, 0));
-        else if constexpr (C::VWORDS == 2) x = __builtin_bit_cast(typename C::vpiece, __builtin_amdgcn_raw_buffer_load_b64(rows, v_lane, t * a.v.token, 0));
-        else x[0] = __builtin_amdgcn_raw_buffer_load_b32(rows, v_lane, t * a.v.token, 0);
+        if constexpr (C::VWORDS == 4) x = __builtin_bit_cast(typename C::vpiece, __builtin_amdgcn_raw_buffer_load_b128(rows, v_lane[t], 0, 0));
+        else if constexpr (C::VWORDS == 2) x = __builtin_bit_cast(typename C::vpiece, __builtin_amdgcn_raw_buffer_load_b64(rows, v_lane[t], 0, 0));
+        else x[0] = __builtin_amdgcn_raw_buffer_load_b32(rows, v_lane[t], 0, 0);
       }
     }
   };
@@ -310,276 +317,276 @@ __global__ __launch_bounds__(64 * kWaves, 2) void decode_kernel(FmDecodeArgs a, 
   // rows of one query t at a time, which all see the same keys.
   if (threadIdx.x == 0) sh.odd = 0;
   for (int only = -1, rounds = 1; rounds > 0; --rounds) {
-  int row_token[NB];
-  float m[NB], l[NB];
-  f32x4 acc[NB][C::E];
+    int row_token[NB];
+    float m[NB], l[NB];
+    f32x4 acc[NB][C::E];
 #pragma unroll
-  for (int nb = 0; nb < NB; ++nb) {
-    row_token[nb] = only < 0 || column_token[nb] == only ? column_token[nb] : -1;
-    m[nb] = -INFINITY;
-    l[nb] = 0.f;
+    for (int nb = 0; nb < NB; ++nb) {
+      row_token[nb] = only < 0 || column_token[nb] == only ? column_token[nb] : -1;
+      m[nb] = -INFINITY;
+      l[nb] = 0.f;
 #pragma unroll
-    for (int e = 0; e < C::E; ++e) acc[nb][e] = f32x4{0.f, 0.f, 0.f, 0.f};
-  }
-  barrier_nofence();
-
-  for (int panel = j_begin; panel < j_end; panel += a.bounds[0] ? C::PANEL : INT32_MAX / 2) {
-    int steps;
-    if (a.bounds[0]) {
-      // the steps of which some row sees a key, and whether it takes the element mask
-      const int end = min(j_end, panel + C::PANEL), all = (end - panel + C::KEYS - 1) / C::KEYS;
-      for (int i = threadIdx.x; i < all; i += 64 * kWaves) sh.flag[i] = 0;
-      barrier_nofence();
-      for (int j = panel + threadIdx.x; j < end; j += 64 * kWaves) {
-        i32x4 bound = {0, 0, 0, 0};
-        if (j < a.bound_columns) {
-#pragma unroll
-          for (int w = 0; w < 4; ++w) bound[w] = a.bounds[w][(size_t)b * a.bound_columns + j];
-        }
-        sh.bound[j - panel] = bound;
-        int flag = 0;
-        for (int t = 0; t < a.T; ++t) {
-          const int i = first_row + t;
-          flag |= j <= i && (a.window <= 0 || j > i - a.window) && !hides(bound, i) ? 1 : 2;
-        }
-        atomicOr(&sh.flag[(j - panel) / C::KEYS], flag);
-      }
-      barrier_nofence();
-      if (wave == 0) {
-        int count = 0;
-        for (int base = 0; base < all; base += 64) {
-          const int flag = base + lane < all ? sh.flag[base + lane] : 0;
-          const unsigned long long live = __ballot(flag & 1);
-          if (flag & 1) sh.list[count + __popcll(live & ((1ull << lane) - 1ull))] = (base + lane) * 4 + flag;
-          count += __popcll(live);
-        }
-        if (lane == 0) sh.count = count;
-      }
-      barrier_nofence();
-      steps = __builtin_amdgcn_readfirstlane(sh.count);
-    } else {
-      steps = (j_end - panel + C::KEYS - 1) / C::KEYS;
+      for (int e = 0; e < C::E; ++e) acc[nb][e] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    const auto entry_of = [&](int s) { return a.bounds[0] ? __builtin_amdgcn_readfirstlane(sh.list[s]) : s * 4; };
+    barrier_nofence();
 
-    if (team_wave < steps && !idle) {
-      int entry = entry_of(team_wave);
-      Step now = pages_of(panel + entry / 4 * C::KEYS);
-      load_k(now, -1);
-      load_v(now, -1);
-      int next_entry = team_wave + TW < steps ? entry_of(team_wave + TW) : entry;
-      Step next = pages_of(panel + next_entry / 4 * C::KEYS);
-      for (int s = team_wave; s < steps; s += TW) {
-        const int more = (s + TW - steps) >> 31;   // -1: another step follows
-        const int start = panel + entry / 4 * C::KEYS;
-        bool masked = (entry & 2) || start + C::KEYS > j_end || start + C::KEYS - 1 > first_row ||
-                      (a.window > 0 && start <= range.len - 1 - a.window);
+    for (int panel = j_begin; panel < j_end; panel += a.bounds[0] ? C::PANEL : INT32_MAX / 2) {
+      int steps;
+      if (a.bounds[0]) {
+        // the steps of which some row sees a key, and whether it takes the element mask
+        const int end = min(j_end, panel + C::PANEL), all = (end - panel + C::KEYS - 1) / C::KEYS;
+        for (int i = threadIdx.x; i < all; i += 64 * kWaves) sh.flag[i] = 0;
+        barrier_nofence();
+        for (int j = panel + threadIdx.x; j < end; j += 64 * kWaves) {
+          i32x4 bound = {0, 0, 0, 0};
+          if (j < a.bound_columns) {
 #pragma unroll
-        for (int i = 0; i < C::GROUPS; ++i) masked |= now.page(i) < 0;
-
-        // scores
-        f32x4 p[NB][C::GROUPS];
-#pragma unroll
-        for (int i = 0; i < C::GROUPS; ++i) {
-#pragma unroll
-          for (int nb = 0; nb < NB; ++nb) p[nb][i] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-          for (int k = 0; k < C::KSTEPS; ++k) {
-            u32x4 op;
-            if constexpr (E4M3) {
-              const u32x4 raw = kraw[i][k / 2];
-              const u32x2 x = widen4<F16>(raw[k % 2 * 2]), y = widen4<F16>(raw[k % 2 * 2 + 1]);
-              op = u32x4{x[0], x[1], y[0], y[1]};
-            } else {
-              op = kraw[i][k];
-            }
-#pragma unroll
-            for (int nb = 0; nb < NB; ++nb) p[nb][i] = mfma_keys<F16>(op, q[nb][k], p[nb][i]);
+            for (int w = 0; w < 4; ++w) bound[w] = a.bounds[w][(size_t)b * a.bound_columns + j];
           }
+          sh.bound[j - panel] = bound;
+          int flag = 0;
+          for (int t = 0; t < a.T; ++t) {
+            const int i = first_row + t;
+            flag |= j <= i && (a.window <= 0 || j > i - a.window) && !hides(bound, i) ? 1 : 2;
+          }
+          atomicOr(&sh.flag[(j - panel) / C::KEYS], flag);
         }
-        load_k(next, more);
+        barrier_nofence();
+        if (wave == 0) {
+          int count = 0;
+          for (int base = 0; base < all; base += 64) {
+            const int flag = base + lane < all ? sh.flag[base + lane] : 0;
+            const unsigned long long live = __ballot(flag & 1);
+            if (flag & 1) sh.list[count + __popcll(live & ((1ull << lane) - 1ull))] = (base + lane) * 4 + flag;
+            count += __popcll(live);
+          }
+          if (lane == 0) sh.count = count;
+        }
+        barrier_nofence();
+        steps = __builtin_amdgcn_readfirstlane(sh.count);
+      } else {
+        steps = (j_end - panel + C::KEYS - 1) / C::KEYS;
+      }
+      const auto entry_of = [&](int s) { return a.bounds[0] ? __builtin_amdgcn_readfirstlane(sh.list[s]) : s * 4; };
+
+      if (team_wave < steps && !idle) {
+        int entry = entry_of(team_wave);
+        Step now = pages_of(panel + entry / 4 * C::KEYS);
+        load_k(now, -1);
+        load_v(now, -1);
+        int next_entry = team_wave + TW < steps ? entry_of(team_wave + TW) : entry;
+        Step next = pages_of(panel + next_entry / 4 * C::KEYS);
+        for (int s = team_wave; s < steps; s += TW) {
+          const int more = (s + TW - steps) >> 31;   // -1: another step follows
+          const int start = panel + entry / 4 * C::KEYS;
+          bool masked = (entry & 2) || start + C::KEYS > j_end || start + C::KEYS - 1 > first_row ||
+                        (a.window > 0 && start <= range.len - 1 - a.window);
+#pragma unroll
+          for (int i = 0; i < C::GROUPS; ++i) masked |= now.page(i) < 0;
+
+          // scores
+          f32x4 p[NB][C::GROUPS];
+#pragma unroll
+          for (int i = 0; i < C::GROUPS; ++i) {
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) p[nb][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int k = 0; k < C::KSTEPS; ++k) {
+              u32x4 op;
+              if constexpr (E4M3) {
+                const u32x4 raw = kraw[i][k / 2];
+                const u32x2 x = widen4<F16>(raw[k % 2 * 2]), y = widen4<F16>(raw[k % 2 * 2 + 1]);
+                op = u32x4{x[0], x[1], y[0], y[1]};
+              } else {
+                op = kraw[i][k];
+              }
+#pragma unroll
+              for (int nb = 0; nb < NB; ++nb) p[nb][i] = mfma_keys<F16>(op, q[nb][k], p[nb][i]);
+            }
+          }
+          load_k(next, more);
 
 #pragma unroll
-        for (int nb = 0; nb < NB; ++nb)
+          for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-          for (int i = 0; i < C::GROUPS; ++i) p[nb][i] *= scale;
+            for (int i = 0; i < C::GROUPS; ++i) p[nb][i] *= scale;
 
-        // element mask; values that no row sees become 0 (the keys of a lane's scores are those of its value pieces).  Which of its
-        // keys a column sees is gathered as bits by a loop: unrolled, the bounds' addresses alone would fill the registers.
-        if (masked) {
-          unsigned pages_there = 0;
+          // element mask; values that no row sees become 0 (the keys of a lane's scores are those of its value pieces).  Which of its
+          // keys a column sees is gathered as bits by a loop: unrolled, the bounds' addresses alone would fill the registers.
+          if (masked) {
+            unsigned pages_there = 0;
 #pragma unroll
-          for (int i = 0; i < C::GROUPS; ++i) pages_there |= (now.page(i) >= 0 ? 1u : 0u) << i;
-          unsigned any = 0, every = ~0u;
+            for (int i = 0; i < C::GROUPS; ++i) pages_there |= (now.page(i) >= 0 ? 1u : 0u) << i;
+            unsigned any = 0, every = ~0u;
 #pragma unroll
-          for (int nb = 0; nb < NB; ++nb) {
-            const bool real = row_token[nb] >= 0;
-            const unsigned seen = real ? seen_keys(start, panel, pages_there, first_row + row_token[nb]) : 0u;
-            any |= row16_or(seen);
-            every &= ~row16_or(real ? ~seen : 0u);
+            for (int nb = 0; nb < NB; ++nb) {
+              const bool real = row_token[nb] >= 0;
+              const unsigned seen = real ? seen_keys(start, panel, pages_there, first_row + row_token[nb]) : 0u;
+              any |= row16_or(seen);
+              every &= ~row16_or(real ? ~seen : 0u);
+#pragma unroll
+              for (int i = 0; i < C::GROUPS; ++i)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                  if (!(seen >> (4 * i + r) & 1)) p[nb][i][r] = -INFINITY;
+            }
+            if (__any((any & ~every) != 0)) {
+              bool odd = false;
+#pragma unroll
+              for (int kt = 0; kt < C::KT; ++kt)
+#pragma unroll
+                for (int t = 0; t < 8; ++t)
+#pragma unroll
+                  for (int w = 0; w < C::VWORDS; ++w) odd |= (any & ~every) >> (8 * kt + t) & 1 && odd_word<F16, E4M3>(vraw[kt][t][w]);
+              if (odd) sh.odd = 1;
+            }
 #pragma unroll
             for (int i = 0; i < C::GROUPS; ++i)
 #pragma unroll
               for (int r = 0; r < 4; ++r)
-                if (!(seen >> (4 * i + r) & 1)) p[nb][i][r] = -INFINITY;
+                if (!(any >> (4 * i + r) & 1)) vraw[i / 2][i % 2 * 4 + r] = (typename C::vpiece)(0u);
           }
-          if (__any((any & ~every) != 0)) {
-            bool odd = false;
-#pragma unroll
-            for (int kt = 0; kt < C::KT; ++kt)
-#pragma unroll
-              for (int t = 0; t < 8; ++t)
-#pragma unroll
-                for (int w = 0; w < C::VWORDS; ++w) odd |= (any & ~every) >> (8 * kt + t) & 1 && odd_word<F16, E4M3>(vraw[kt][t][w]);
-            if (odd) sh.odd = 1;
-          }
-#pragma unroll
-          for (int i = 0; i < C::GROUPS; ++i)
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-              if (!(any >> (4 * i + r) & 1)) vraw[i / 2][i % 2 * 4 + r] = (typename C::vpiece)(0u);
-        }
 
-        // softmax
+          // softmax
 #pragma unroll
-        for (int nb = 0; nb < NB; ++nb) {
-          float top = p[nb][0][0];
+          for (int nb = 0; nb < NB; ++nb) {
+            float top = p[nb][0][0];
 #pragma unroll
-          for (int i = 0; i < C::GROUPS; ++i)
+            for (int i = 0; i < C::GROUPS; ++i)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) top = fmaxf(top, p[nb][i][r]);
-          top = fmaxf(quad_max(top), m[nb]);
-          const float ref = reference(top), alpha = fast_exp2(m[nb] - ref);
-          m[nb] = top;
-          float sum = 0.f;
+              for (int r = 0; r < 4; ++r) top = fmaxf(top, p[nb][i][r]);
+            top = fmaxf(quad_max(top), m[nb]);
+            const float ref = reference(top), alpha = fast_exp2(m[nb] - ref);
+            m[nb] = top;
+            float sum = 0.f;
 #pragma unroll
-          for (int i = 0; i < C::GROUPS; ++i)
+            for (int i = 0; i < C::GROUPS; ++i)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-              p[nb][i][r] = fast_exp2(p[nb][i][r] - (ref - kShift<F16>));
-              sum += p[nb][i][r];
-            }
-          l[nb] = l[nb] * alpha + sum;
-          if (__any(alpha != 1.f)) {   // seldom, after the first steps
-#pragma unroll
-            for (int e = 0; e < C::E; ++e) acc[nb][e] *= alpha;
-          }
-        }
-
-        // products with the values
-#pragma unroll
-        for (int kt = 0; kt < C::KT; ++kt) {
-          u32x4 hi[NB], lo[NB];
-#pragma unroll
-          for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-            for (int w = 0; w < 4; ++w) {
-              unsigned h, o;
-              split2<F16>(p[nb][2 * kt + w / 2][2 * (w % 2)], p[nb][2 * kt + w / 2][2 * (w % 2) + 1], h, o);
-              hi[nb][w] = h;
-              lo[nb][w] = o;
-            }
-          unsigned v[8][C::E / 2];
-#pragma unroll
-          for (int t = 0; t < 8; ++t) {
-            if constexpr (E4M3) {
-#pragma unroll
-              for (int w = 0; w < C::VWORDS; ++w) {
-                const u32x2 x = widen4<F16>(vraw[kt][t][w]);
-                v[t][2 * w] = x[0];
-                v[t][2 * w + 1] = x[1];
+              for (int r = 0; r < 4; ++r) {
+                p[nb][i][r] = fast_exp2(p[nb][i][r] - (ref - kShift<F16>));
+                sum += p[nb][i][r];
               }
-            } else {
+            l[nb] = l[nb] * alpha + sum;
+            if (__any(alpha != 1.f)) {   // seldom, after the first steps
 #pragma unroll
-              for (int w = 0; w < C::VWORDS; ++w) v[t][w] = vraw[kt][t][w];
+              for (int e = 0; e < C::E; ++e) acc[nb][e] *= alpha;
             }
           }
+
+          // products with the values
 #pragma unroll
-          for (int e = 0; e < C::E; ++e) {
-            u32x4 op;
+          for (int kt = 0; kt < C::KT; ++kt) {
+            u32x4 hi[NB], lo[NB];
 #pragma unroll
-            for (int w = 0; w < 4; ++w) op[w] = pair_of(v[2 * w][e / 2], v[2 * w + 1][e / 2], e % 2);
+            for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-            for (int nb = 0; nb < NB; ++nb) {
-              acc[nb][e] = mfma_keys<F16>(op, lo[nb], acc[nb][e]);
-              acc[nb][e] = mfma_keys<F16>(op, hi[nb], acc[nb][e]);
+              for (int w = 0; w < 4; ++w) {
+                unsigned h, o;
+                split2<F16>(p[nb][2 * kt + w / 2][2 * (w % 2)], p[nb][2 * kt + w / 2][2 * (w % 2) + 1], h, o);
+                hi[nb][w] = h;
+                lo[nb][w] = o;
+              }
+            unsigned v[8][C::E / 2];
+#pragma unroll
+            for (int t = 0; t < 8; ++t) {
+              if constexpr (E4M3) {
+#pragma unroll
+                for (int w = 0; w < C::VWORDS; ++w) {
+                  const u32x2 x = widen4<F16>(vraw[kt][t][w]);
+                  v[t][2 * w] = x[0];
+                  v[t][2 * w + 1] = x[1];
+                }
+              } else {
+#pragma unroll
+                for (int w = 0; w < C::VWORDS; ++w) v[t][w] = vraw[kt][t][w];
+              }
+            }
+#pragma unroll
+            for (int e = 0; e < C::E; ++e) {
+              u32x4 op;
+#pragma unroll
+              for (int w = 0; w < 4; ++w) op[w] = pair_of(v[2 * w][e / 2], v[2 * w + 1][e / 2], e % 2);
+#pragma unroll
+              for (int nb = 0; nb < NB; ++nb) {
+                acc[nb][e] = mfma_keys<F16>(op, lo[nb], acc[nb][e]);
+                acc[nb][e] = mfma_keys<F16>(op, hi[nb], acc[nb][e]);
+              }
             }
           }
+          load_v(next, more);
+          entry = next_entry;
+          now = next;
+          next_entry = s + 2 * TW < steps ? entry_of(s + 2 * TW) : entry;
+          next = pages_of(panel + next_entry / 4 * C::KEYS);
         }
-        load_v(next, more);
-        entry = next_entry;
-        now = next;
-        next_entry = s + 2 * TW < steps ? entry_of(s + 2 * TW) : entry;
-        next = pages_of(panel + next_entry / 4 * C::KEYS);
       }
+      if (a.bounds[0]) barrier_nofence();
     }
-    if (a.bounds[0]) barrier_nofence();
-  }
 
-  barrier_nofence();
-  if (only < 0 && __builtin_amdgcn_readfirstlane(sh.odd)) {
-    only = 0;
-    rounds = a.T + 1;
-    continue;
-  }
-
-  // A team's sums meet in LDS, 16 rows at a time
-  constexpr int PER = 16 * D / (64 * TW);   // elements of a thread: neighbours of one row
-  const int my_row = team_thread * PER / D, my_col = team_thread * PER % D;
-  const float v_scale = E4M3 ? a.v_scale[hk] : 1.f;
-#pragma unroll
-  for (int nb = 0; nb < NB; ++nb) {
-    const float sum = quad_sum(l[nb]);
-    if (g == 0) sh.stat[wave][c] = float2{m[nb], sum};
-#pragma unroll
-    for (int r = 0; r < 4; ++r)
-#pragma unroll
-      for (int e = 0; e < C::E; e += 4)
-        *(f32x4*)&sh.out[wave][c][4 * C::E * g + C::E * r + e] =
-            f32x4{acc[nb][e][r], acc[nb][e + 1][r], acc[nb][e + 2][r], acc[nb][e + 3][r]};
     barrier_nofence();
-    float top = -INFINITY, total = 0.f, x[PER];
-#pragma unroll
-    for (int w = 0; w < TW; ++w) top = fmaxf(top, sh.stat[w * TEAMS + team][my_row].x);
-#pragma unroll
-    for (int e = 0; e < PER; ++e) x[e] = 0.f;
-#pragma unroll
-    for (int w = 0; w < TW; ++w) {
-      const float2 stat = sh.stat[w * TEAMS + team][my_row];
-      const float weight = fast_exp2(stat.x - reference(top));
-      total += weight * stat.y;
-#pragma unroll
-      for (int e = 0; e < PER; ++e) x[e] += weight * sh.out[w * TEAMS + team][my_row][my_col + e];
+    if (only < 0 && __builtin_amdgcn_readfirstlane(sh.odd)) {
+      only = 0;
+      rounds = a.T + 1;
+      continue;
     }
-    const int r = rb * C::ROWS + nb * 16 + my_row;
-    if (r < R && !idle && (only < 0 || r % a.T == only)) {
-      if (chunks > 1) {
-        const size_t at = ((size_t)(slot + chunk) * a.Hk + hk) * R + r;
+
+    // A team's sums meet in LDS, 16 rows at a time
+    constexpr int PER = 16 * D / (64 * TW);   // elements of a thread: neighbours of one row
+    const int my_row = team_thread * PER / D, my_col = team_thread * PER % D;
+    const float v_scale = E4M3 ? a.v_scale[hk] : 1.f;
 #pragma unroll
-        for (int e = 0; e < PER; e += 4) *(f32x4*)(a.part + at * D + my_col + e) = f32x4{x[e], x[e + 1], x[e + 2], x[e + 3]};
-        if (my_col == 0) a.stat[at] = float2{top, total};
-      } else {
-        const int hq = fm_div(r, tokens), t = r - hq * a.T, h = hk * G + hq;
-        const float factor = total == 0.f ? 0.f : v_scale / total;
-        char* o = (char*)a.out + 2 * ((long long)b * a.so.b + (long long)h * a.so.h + (long long)t * a.so.n + my_col);
+    for (int nb = 0; nb < NB; ++nb) {
+      const float sum = quad_sum(l[nb]);
+      if (g == 0) sh.stat[wave][c] = float2{m[nb], sum};
 #pragma unroll
-        for (int e = 0; e < PER; e += 2) *(unsigned*)(o + 2 * e) = pack2<F16>(x[e] * factor, x[e + 1] * factor);
-        if (my_col == 0) a.lse[((size_t)b * a.H + h) * a.T + t] = total == 0.f ? -INFINITY : (top + fast_log2(total * kUnshift<F16>)) * kLn2;
+      for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int e = 0; e < C::E; e += 4)
+          *(f32x4*)&sh.out[wave][c][4 * C::E * g + C::E * r + e] =
+              f32x4{acc[nb][e][r], acc[nb][e + 1][r], acc[nb][e + 2][r], acc[nb][e + 3][r]};
+      barrier_nofence();
+      float top = -INFINITY, total = 0.f, x[PER];
+#pragma unroll
+      for (int w = 0; w < TW; ++w) top = fmaxf(top, sh.stat[w * TEAMS + team][my_row].x);
+#pragma unroll
+      for (int e = 0; e < PER; ++e) x[e] = 0.f;
+#pragma unroll
+      for (int w = 0; w < TW; ++w) {
+        const float2 stat = sh.stat[w * TEAMS + team][my_row];
+        const float weight = fast_exp2(stat.x - reference(top));
+        total += weight * stat.y;
+#pragma unroll
+        for (int e = 0; e < PER; ++e) x[e] += weight * sh.out[w * TEAMS + team][my_row][my_col + e];
       }
+      const int r = rb * C::ROWS + nb * 16 + my_row;
+      if (r < R && !idle && (only < 0 || r % a.T == only)) {
+        if (chunks > 1) {
+          const size_t at = ((size_t)(slot + chunk) * a.Hk + hk) * R + r;
+#pragma unroll
+          for (int e = 0; e < PER; e += 4) *(f32x4*)(a.part + at * D + my_col + e) = f32x4{x[e], x[e + 1], x[e + 2], x[e + 3]};
+          if (my_col == 0) a.stat[at] = float2{top, total};
+        } else {
+          const int hq = fm_div(r, tokens), t = r - hq * a.T, h = hk * G + hq;
+          const float factor = total == 0.f ? 0.f : v_scale / total;
+          char* o = (char*)a.out + 2 * ((long long)b * a.so.b + (long long)h * a.so.h + (long long)t * a.so.n + my_col);
+#pragma unroll
+          for (int e = 0; e < PER; e += 2) *(unsigned*)(o + 2 * e) = pack2<F16>(x[e] * factor, x[e + 1] * factor);
+          if (my_col == 0) a.lse[((size_t)b * a.H + h) * a.T + t] = total == 0.f ? -INFINITY : (top + fast_log2(total * kUnshift<F16>)) * kLn2;
+        }
+      }
+      barrier_nofence();
     }
-    barrier_nofence();
-  }
-  if (only >= 0) ++only;
+    if (only >= 0) ++only;
   }
 }
 
-// Joins the chunks of a row of a split sequence.  D / 4 lanes take a chunk's sums of p v, the workgroup 1024 / D chunks at a time.
+// Joins the chunks of a row of a split sequence: D / 4 lanes take a chunk's sums of p v, the workgroup 1024 / D chunks at a time.  Bound by
+// its chain of round trips, 4 to 5 us.
 template <int D, bool F16>
 __global__ __launch_bounds__(256) void join_kernel(FmDecodeArgs a, FmDivisor rows, FmDivisor tokens) {
   constexpr int LANES = D / 4, TEAMS = 256 / LANES, BATCH = 4;
   const int G = a.H / a.Hk, R = G * a.T;
-  const int sh_row = fm_div(blockIdx.x, rows), r = blockIdx.x - sh_row * R;   // (sequence, K/V head), row of it
-  const int b = blockIdx.y, hk = sh_row;
+  const int b = blockIdx.y, hk = fm_div(blockIdx.x, rows), r = blockIdx.x - hk * R;   // row of the K/V head
   const int2 plan = a.plan[b];
   if (plan.y <= 1) return;
   const int team = threadIdx.x / LANES, lane = threadIdx.x % LANES;

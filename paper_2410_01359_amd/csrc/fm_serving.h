@@ -7,6 +7,7 @@
 int fm_hip_error(hipError_t e);
 
 constexpr int FM_MOST_HEADS = 16384;
+constexpr int FM_MOST_NEW_TOKENS = 256;   // of a sequence in flashmask_decode
 
 // q, k [B, heads, N, d] -> q_out, k_out; strides in elements, in this order.
 struct FmRopeArgs {

@@ -72,7 +72,7 @@ int check_row_type(int type, const flashmask_cache& c) {
 
 // Queries that flashmask_decode's indexing has room for.
 int check_decode_shape(int sequences, int H, int Hk, int T, int d) {
-  if (sequences <= 0 || H <= 0 || H > FM_MOST_HEADS || Hk <= 0 || H % Hk || T <= 0 || T > 65536 || bad_head_dim(d)) return FM_ERR_SHAPE;
+  if (sequences <= 0 || H <= 0 || H > FM_MOST_HEADS || Hk <= 0 || H % Hk || T <= 0 || T > FM_MOST_NEW_TOKENS || bad_head_dim(d)) return FM_ERR_SHAPE;
   if ((long long)H * T > (1 << 24) || sequences > 65535 || (long long)H * T * sequences > (1ll << 30)) return FM_ERR_SHAPE;
   return FM_OK;
 }

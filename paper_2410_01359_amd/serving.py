@@ -161,7 +161,7 @@ def flashmask_decode_workspace_bytes(sequences: int, H: int, H_kv: int, T: int, 
 
 def flashmask_decode(q, k_cache, v_cache, table, lens, scale: float, *, bounds=None, window: int = 0, k_scale=None, v_scale=None,
                      workspace: torch.Tensor | None = None):
-    """Attention of the last T tokens of every sequence, q [sequences, H, T, d], over the cache, which holds lens[b] tokens of
+    """Attention of the last T (1 to 256) tokens of every sequence, q [sequences, H, T, d], over the cache, which holds lens[b] tokens of
     sequence b, the new ones among them.  bounds: (lts, lte, uts, ute), int32 [sequences, columns]; window: keys that a row sees,
     itself among them (0: all).  Returns out (laid out like q) and lse (fp32 [sequences, H, T])."""
     device, dtype = _device(q, "q"), q.dtype

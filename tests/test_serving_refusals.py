@@ -76,7 +76,7 @@ def test_append(wrong, code):
 @pytest.mark.parametrize("wrong,code", [
     ({"q": None}, NULL), ({"lens": None}, NULL), ({"out": None}, NULL), ({"lse": None}, NULL), ({"bounds": (P, P, P, None)}, NULL),
     ({"bounds": (None, None, P, None)}, NULL), ({"type": F32}, ARG), ({"scale": 0.0}, ARG), ({"scale": float("nan")}, ARG),
-    ({"scale": float("inf")}, ARG), ({"window": -1}, ARG), ({"H": 12}, SHAPE), ({"H": 0}, SHAPE), ({"T": 0}, SHAPE), ({"T": 1 << 17}, SHAPE),
+    ({"scale": float("inf")}, ARG), ({"window": -1}, ARG), ({"H": 12}, SHAPE), ({"H": 0}, SHAPE), ({"T": 0}, SHAPE), ({"T": 257}, SHAPE),
     ({"bounds": (P,) * 4}, SHAPE), ({"sq": (4096, 256, 120)}, SHAPE), ({"so": (4100, 256, 128)}, ALIGN), ({"q": P + 8}, ALIGN),
     ({"workspace": None}, WORKSPACE), ({"workspace": P + 16}, WORKSPACE), ({"nbytes": 100}, WORKSPACE)])
 def test_decode(wrong, code):
