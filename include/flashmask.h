@@ -52,7 +52,7 @@ enum {
   FM_ERR_ALIGN = -3,     /* a tensor pointer is not 16-byte aligned */
   FM_ERR_WORKSPACE = -4, /* workspace is NULL or smaller than flashmask_workspace_bytes() */
   FM_ERR_HIP = -5,       /* a kernel launch failed; see flashmask_last_hip_error() */
-  FM_ERR_ARG = -6,       /* unknown pass id, scale <= 0 or not finite */
+  FM_ERR_ARG = -6,       /* unknown pass id, type or layout, types that do not go together, scale <= 0 or not finite */
   FM_ERR_STATIC_LIMIT = -7 /* flashmask_fwd_noalloc: the problem does not fit the library's static scratch */
 };
 

@@ -117,11 +117,11 @@ const char* flashmask_strerror(int code) {
   switch (code) {
     case FM_OK: return "ok";
     case FM_ERR_NULL: return "a required pointer is NULL";
-    case FM_ERR_SHAPE: return "unsupported shape (need B,H,N > 0, d in {64,128})";
+    case FM_ERR_SHAPE: return "unsupported shape (need B,H,N > 0, d in {64,128}; of a cache pages of a multiple of 16 tokens, of rotations a multiple of 16 elements)";
     case FM_ERR_ALIGN: return "a tensor pointer is not 16-byte aligned";
     case FM_ERR_WORKSPACE: return "workspace is NULL, misaligned or too small";
     case FM_ERR_HIP: return "HIP launch failed (see flashmask_last_hip_error)";
-    case FM_ERR_ARG: return "bad scalar argument (unknown pass id, or scale not a positive finite number)";
+    case FM_ERR_ARG: return "bad scalar argument (unknown pass id, type or layout, or scale not a positive finite number)";
     case FM_ERR_STATIC_LIMIT:
       return "flashmask_fwd_noalloc: the problem needs more scratch than the library's static buffer holds "
              "(flashmask_workspace_bytes(FM_PASS_FWD, ...) > FLASHMASK_NOALLOC_SCRATCH_BYTES)";

@@ -329,6 +329,7 @@ static dim3 share_out(long long tokens, int heads, int lanes, bool by_token, int
   span = 16;
   if (by_token)
     for (span = 2; span < kMostTokens && span * heads * lanes < 320;) span *= 2;
+  if (tokens > (1 << 23)) span = kMostTokens;   // a launch has fewer than 2^32 lanes
   const long long workgroups = (tokens + span - 1) / span, wanted = 8ll * fm_compute_units();
   const int groups = (int)std::max<long long>(1, std::min<long long>(heads, wanted / workgroups));
   group = std::max((heads + groups - 1) / groups, 256 / (span * lanes));

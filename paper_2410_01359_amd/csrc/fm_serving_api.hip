@@ -192,6 +192,8 @@ int flashmask_decode(const flashmask_cache* cache, const void* q, const int32_t*
   const int row = cache->d * element_bytes(cache->type);
   const bool side_by_side = a.k.head < 256 && a.v.head < 256;
   a.cut = fm_decode_cut(H, cache->heads, T, cache->d, cache->sequences, side_by_side && row < 256 ? 2 : 1, fm_compute_units());
+  // a launch has fewer than 2^32 lanes
+  if ((fm_most_units(a.cut.chunks, cache->sequences) + 8ll) * a.cut.workgroups >= 1 << 24) return FM_ERR_SHAPE;
   const bool split = (long long)cache->columns * cache->page > whole_keys(cache->sequences, a.cut);
   const DecodeSpace space = decode_space(a.cut, cache->sequences, H, T, cache->d);
   a.plan = split ? (int2*)ws : nullptr;

@@ -85,6 +85,8 @@ def test_decode(wrong, code):
 
 def test_tables_beyond_32_bits_of_keys_are_refused():
     assert _decode(cache=_cache(sequences=100, columns=1 << 20, page=256)) == SHAPE
+    assert _decode(cache=_cache(sequences=65535, heads=1024, sk=(1 << 23, 8192, 128), sv=(1 << 23, 8192, 128)), H=1024, T=1,
+                   sq=(1 << 17, 128, 128), so=(1 << 17, 128, 128)) == SHAPE
 
 
 def test_decode_workspace_bytes():
