@@ -22,73 +22,47 @@ _CACHE = struct.Struct("@PP6qPPP7i")
 _TWO, _FOUR = struct.Struct("@6q"), struct.Struct("@12q")
 
 
-# Each check is one expression, and what exactly is wrong is only looked for where it fails: a call of one new token per
-# sequence takes the host about as long as the GPU.
-def _wrong(t, name: str, device: int, types=None, shape=None):
-    """Raise what is wrong with a tensor (something is)."""
-    if t.get_device() < 0:
-        raise FlashMaskError(f"{name} must live on the GPU")
-    if t.get_device() != device:
-        raise FlashMaskError(f"the tensors must be on one GPU, the current one: {name} is on {t.get_device()}")
-    if types is not None and t.dtype not in types:
-        raise FlashMaskError(f"{name} must be {' or '.join(str(x) for x in types)}, got {t.dtype}")
-    if shape is not None and tuple(t.shape) != tuple(shape):
-        raise FlashMaskError(f"{name} must be {list(shape)}, got {list(t.shape)}")
-    raise FlashMaskError(f"{name} must be contiguous (tensors of rows: along their rows)")
-
-
-def _device(t, name: str) -> int:
-    device = t.get_device()
-    if device < 0 or device != torch._C._cuda_getDevice():
-        _wrong(t, name, device if device < 0 else torch._C._cuda_getDevice())
-    return device
-
-
-def _index(t, shape, name: str, device: int) -> int:
-    """Address of an int32 tensor of this shape."""
-    if not (t.dtype is torch.int32 and t.shape == shape and t.is_contiguous() and t.get_device() == device):
-        _wrong(t, name, device, (torch.int32,), shape)
-    return t.data_ptr()
-
-
-def _rows(t, shape, dtype, name: str, device: int):
-    """Strides of a tensor of rows, the last of them 1."""
-    strides = t.stride()
-    if not (t.dtype is dtype and t.shape == shape and strides[-1] == 1 and t.get_device() == device):
-        _wrong(t, name, device, (dtype,), shape)
-    return strides
-
-
-def _vector(t, n: int, dtype, name: str, device: int) -> int:
-    """Address of a vector of n values (-1: of some); 0 for None."""
-    if t is None:
-        return 0
-    if t.dim() != 1 or t.shape[0] != n and (n >= 0 or t.shape[0] == 0):
-        raise FlashMaskError(f"{name} must be a vector of {n if n >= 0 else 'some'} values, got {list(t.shape)}")
-    if not (t.dtype is dtype and t.is_contiguous() and t.get_device() == device):
-        _wrong(t, name, device, (dtype,))
-    return t.data_ptr()
-
-
-def _dims(t, n: int, name: str):
-    if t.dim() != n:
-        raise FlashMaskError(f"{name} must have {n} dimensions, got {t.dim()}")
-    return t.shape
+# A call of few tokens takes the host longer than the GPU, so a call's checks are one expression, and what exactly is wrong is only
+# looked for where it fails.
+def _refuse(*wanted):
+    """Raise what is wrong with tensors (t, name, types, shape, contiguous along how many of their last axes); something is."""
+    device = torch._C._cuda_getDevice() if torch.cuda.is_available() else -1
+    for t, name, types, shape, dense in wanted:
+        if t is None:
+            continue
+        if not t.is_cuda:
+            raise FlashMaskError(f"{name} must live on the GPU")
+        if t.get_device() != device:
+            raise FlashMaskError(f"the tensors must be on the current GPU, {device}: {name} is on {t.get_device()}")
+        if t.dtype not in types:
+            raise FlashMaskError(f"{name} must be {' or '.join(str(x) for x in types)}, got {t.dtype}")
+        if t.dim() != len(shape) or any(want is not None and have != want for have, want in zip(t.shape, shape)):
+            raise FlashMaskError(f"{name} must be [{', '.join('n' if x is None else str(x) for x in shape)}], got {list(t.shape)}")
+        if 0 in t.shape:
+            raise FlashMaskError(f"{name} is empty: {list(t.shape)}")
+        if not (t.is_contiguous() if dense > 1 else t.stride(-1) == 1):
+            raise FlashMaskError(f"{name} must be contiguous{'' if dense > 1 else ' along its last axis'}")
+    raise FlashMaskError("the tensors do not go together")
 
 
 def _rope(entry: str, q, k, freqs, positions, layout, amp):
-    device, type_id, dtype = _device(q, "q"), _ROPE_TYPE.get(q.dtype), q.dtype
-    if type_id is None:
-        _wrong(q, "q", device, tuple(_ROPE_TYPE))
-    B, H, N, d = shape = _dims(q, 4, "q")
-    Hk = _dims(k, 4, "k")[1]
-    sq, sk = _rows(q, shape, dtype, "q", device), _rows(k, (B, Hk, N, d), dtype, "k", device)
-    at = 0 if positions is None else _index(positions, (B, N), "positions", device)
-    frequencies = _vector(freqs, -1, torch.float64, "freqs", device)
+    dtype, shape, sq, sk = q.dtype, q.shape, q.stride(), k.stride()
+    type_id, device = _ROPE_TYPE.get(dtype), q.get_device()
+    if not (type_id is not None and len(shape) == 4 and len(sk) == 4 and sq[3] == 1 and sk[3] == 1 and k.dtype is dtype
+            and k.shape == (shape[0], k.shape[1], shape[2], shape[3]) and freqs.dtype is torch.float64 and freqs.dim() == 1
+            and freqs.is_contiguous() and 0 <= device == k.get_device() == freqs.get_device() == torch._C._cuda_getDevice()
+            and (positions is None or positions.dtype is torch.int32 and positions.shape == (shape[0], shape[2])
+                 and positions.is_contiguous() and positions.get_device() == device)):
+        like = (*shape, None, None, None, None)
+        _refuse((q, "q", tuple(_ROPE_TYPE), (None,) * 4, 1), (k, "k", (dtype,), (like[0], None, like[2], like[3]), 1),
+                (freqs, "freqs", (torch.float64,), (None,), 2), (positions, "positions", (torch.int32,), (like[0], like[2]), 2))
+    B, H, N, d = shape
     q_out, k_out = torch.empty_like(q), torch.empty_like(k)
-    strides = _FOUR.pack(*sq[:3], *sk[:3], *q_out.stride()[:3], *k_out.stride()[:3])
-    _check(getattr(load_library(), entry)(q.data_ptr(), k.data_ptr(), q_out.data_ptr(), k_out.data_ptr(), frequencies, at, type_id,
-                                          layout, amp, B, H, Hk, N, d, 2 * freqs.shape[0], strides, _stream()), entry)
+    to_q, to_k = q_out.stride(), k_out.stride()
+    strides = _FOUR.pack(sq[0], sq[1], sq[2], sk[0], sk[1], sk[2], to_q[0], to_q[1], to_q[2], to_k[0], to_k[1], to_k[2])
+    _check(getattr(load_library(), entry)(q.data_ptr(), k.data_ptr(), q_out.data_ptr(), k_out.data_ptr(), freqs.data_ptr(),
+                                          0 if positions is None else positions.data_ptr(), type_id, layout, amp, B, H, k.shape[1], N, d,
+                                          2 * freqs.shape[0], strides, _stream()), entry)
     return q_out, k_out
 
 
@@ -107,20 +81,20 @@ def _cache(k_cache, v_cache, table, k_scale, v_scale, device: int):
     """flashmask_cache as bytes, and its heads, d and sequences."""
     dtype, shape, entries = k_cache.dtype, k_cache.shape, table.shape
     type_id, sk, sv = _CACHE_TYPE.get(dtype), k_cache.stride(), v_cache.stride()
-    if not (type_id is not None and len(shape) == 4 and v_cache.shape == shape and v_cache.dtype is dtype and sk[3] == 1 and sv[3] == 1
+    heads = shape[1] if len(shape) == 4 else None
+    if not (type_id is not None and heads is not None and v_cache.shape == shape and v_cache.dtype is dtype and sk[3] == 1 and sv[3] == 1
             and len(entries) == 2 and table.dtype is torch.int32 and table.is_contiguous()
-            and k_cache.get_device() == v_cache.get_device() == table.get_device() == device):
-        _dims(k_cache, 4, "k_cache")
-        for t, name, types, want in ((k_cache, "k_cache", tuple(_CACHE_TYPE), shape), (v_cache, "v_cache", (dtype,), shape),
-                                     (table, "table", (torch.int32,), _dims(table, 2, "table"))):
-            if t.dtype not in types or t.shape != want or t.get_device() != device or t.stride()[-1] != 1 or t is table and not t.is_contiguous():
-                _wrong(t, name, device, types, want)
-    pages, heads, page, d = shape
+            and 0 <= device == k_cache.get_device() == v_cache.get_device() == table.get_device() == torch._C._cuda_getDevice()
+            and (k_scale is None and v_scale is None or k_scale is not None and v_scale is not None
+                 and k_scale.dtype is torch.float32 and v_scale.dtype is torch.float32 and k_scale.shape == (heads,) == v_scale.shape
+                 and k_scale.is_contiguous() and v_scale.is_contiguous() and k_scale.get_device() == device == v_scale.get_device())):
+        _refuse((k_cache, "k_cache", tuple(_CACHE_TYPE), (None,) * 4, 1), (v_cache, "v_cache", (dtype,), tuple(shape), 1),
+                (table, "table", (torch.int32,), (None, None), 2), (k_scale, "k_scale", (torch.float32,), (heads,), 2),
+                (v_scale, "v_scale", (torch.float32,), (heads,), 2))
+    pages, _, page, d = shape
     sequences, columns = entries
-    k_at = v_at = 0
-    if k_scale is not None or v_scale is not None:
-        k_at, v_at = (_vector(s, heads, torch.float32, n, device) for s, n in ((k_scale, "k_scale"), (v_scale, "v_scale")))
-    return (_CACHE.pack(k_cache.data_ptr(), v_cache.data_ptr(), sk[0], sk[1], sk[2], sv[0], sv[1], sv[2], k_at, v_at, table.data_ptr(),
+    return (_CACHE.pack(k_cache.data_ptr(), v_cache.data_ptr(), sk[0], sk[1], sk[2], sv[0], sv[1], sv[2],
+                        0 if k_scale is None else k_scale.data_ptr(), 0 if v_scale is None else v_scale.data_ptr(), table.data_ptr(),
                         type_id, heads, d, pages, page, sequences, columns), heads, d, sequences)
 
 
@@ -129,28 +103,34 @@ def flashmask_cache_append(k, v, k_cache, v_cache, table, seqs, positions, *, q=
     """Write new tokens' keys (rotated where freqs is given) and values [tokens, H_kv, d] to the cache: token n goes to position
     positions[n] of sequence seqs[n] (outside the table's sequences: padding).  Returns the queries q [tokens, H, d], rotated, or
     None."""
-    device, dtype = _device(k, "k"), k.dtype
+    dtype, shape, device, sk, sv = k.dtype, k.shape, k.get_device(), k.stride(), v.stride()
     type_id = _ROW_TYPE.get(dtype)
-    if type_id is None:
-        _wrong(k, "k", device, tuple(_ROW_TYPE))
     cache, heads, d, _ = _cache(k_cache, v_cache, table, k_scale, v_scale, device)
-    n = _dims(k, 3, "k")[0]
-    sk, sv = _rows(k, (n, heads, d), dtype, "k", device), _rows(v, (n, heads, d), dtype, "v", device)
-    seqs_at, positions_at = _index(seqs, (n,), "seqs", device), _index(positions, (n,), "positions", device)
-    frequencies = _vector(freqs, -1, torch.float64, "freqs", device)
-    H, q_at, out_at, q_out, sq = 0, 0, 0, None, (0, 0)
-    if q is not None:
-        if freqs is None:
+    sq = (0, 0, 1) if q is None else q.stride()
+    n = shape[0] if len(shape) == 3 else None
+    if not (type_id is not None and shape == (n, heads, d) == v.shape and v.dtype is dtype and sk[2] == 1 and sv[2] == 1
+            and seqs.dtype is torch.int32 and positions.dtype is torch.int32 and seqs.shape == (n,) == positions.shape
+            and seqs.is_contiguous() and positions.is_contiguous() and device == v.get_device() == seqs.get_device() == positions.get_device()
+            and (q is None or freqs is not None and len(sq) == 3 and sq[2] == 1 and q.dtype is dtype and q.shape == (n, q.shape[1], d)
+                 and q.get_device() == device)
+            and (freqs is None or freqs.dtype is torch.float64 and freqs.dim() == 1 and freqs.numel() > 0 and freqs.is_contiguous()
+                 and freqs.get_device() == device)):
+        if q is not None and freqs is None:
             raise FlashMaskError("q is only rotated: it needs freqs")
-        H = _dims(q, 3, "q")[1]
-        sq = _rows(q, (n, H, d), dtype, "q", device)
+        _refuse((k, "k", tuple(_ROW_TYPE), (None, heads, d), 1), (v, "v", (dtype,), (n, heads, d), 1),
+                (seqs, "seqs", (torch.int32,), (n,), 2), (positions, "positions", (torch.int32,), (n,), 2),
+                (q, "q", (dtype,), (n, None, d), 1), (freqs, "freqs", (torch.float64,), (None,), 2))
+    H, q_at, out_at, q_out = 0, 0, 0, None
+    if q is not None:
+        H = q.shape[1]
         q_out = torch.empty(n, H, d, dtype=dtype, device=q.device)
         q_at, out_at = q.data_ptr(), q_out.data_ptr()
     if n == 0:
         return q_out
     strides = _FOUR.pack(0, sq[1], sq[0], 0, sk[1], sk[0], 0, sv[1], sv[0], 0, d, H * d)
-    _check(load_library().flashmask_cache_append(cache, q_at, k.data_ptr(), v.data_ptr(), out_at, seqs_at, positions_at, frequencies,
-                                                 type_id, layout, amp, n, H, 0 if freqs is None else 2 * freqs.shape[0], strides,
+    turned = 0 if freqs is None else freqs.data_ptr()
+    _check(load_library().flashmask_cache_append(cache, q_at, k.data_ptr(), v.data_ptr(), out_at, seqs.data_ptr(), positions.data_ptr(),
+                                                 turned, type_id, layout, amp, n, H, 2 * freqs.shape[0] if turned else 0, strides,
                                                  _stream()), "flashmask_cache_append")
     return q_out
 
@@ -164,29 +144,31 @@ def flashmask_decode(q, k_cache, v_cache, table, lens, scale: float, *, bounds=N
     """Attention of the last T (1 to 256) tokens of every sequence, q [sequences, H, T, d], over the cache, which holds lens[b] tokens of
     sequence b, the new ones among them.  bounds: (lts, lte, uts, ute), int32 [sequences, columns]; window: keys that a row sees,
     itself among them (0: all).  Returns out (laid out like q) and lse (fp32 [sequences, H, T])."""
-    device, dtype = _device(q, "q"), q.dtype
+    dtype, shape, device, sq = q.dtype, q.shape, q.get_device(), q.stride()
     type_id = _ROW_TYPE.get(dtype)
-    if type_id is None:
-        _wrong(q, "q", device, tuple(_ROW_TYPE))
-    cache, heads, d, sequences = _cache(k_cache, v_cache, table, k_scale, v_scale, device)
-    B, H, T, _ = _dims(q, 4, "q")
-    sq = _rows(q, (sequences, H, T, d), dtype, "q", device)
-    lens_at = _index(lens, (B,), "lens", device)
+    cache, heads, d, B = _cache(k_cache, v_cache, table, k_scale, v_scale, device)
+    if not (type_id is not None and len(shape) == 4 and shape[0] == B and shape[3] == d and sq[3] == 1 and lens.dtype is torch.int32
+            and lens.shape == (B,) and lens.is_contiguous() and lens.get_device() == device
+            and (workspace is None or workspace.get_device() == device and workspace.is_contiguous())):
+        _refuse((q, "q", tuple(_ROW_TYPE), (B, None, None, d), 1), (lens, "lens", (torch.int32,), (B,), 2),
+                *(() if workspace is None else ((workspace, "workspace", (workspace.dtype,), tuple(workspace.shape), 2),)))
+    H, T = shape[1], shape[2]
     at, columns = (0, 0, 0, 0), 0
     if bounds is not None:
-        if len(bounds) != 4 or bounds[0].numel() == 0:
+        if len(bounds) != 4:
             raise FlashMaskError("bounds must be (lts, lte, uts, ute), int32 [sequences, columns]")
         columns = bounds[0].shape[-1]
-        at = [_index(x, (B, columns), n, device) for x, n in zip(bounds, ("lts", "lte", "uts", "ute"))]
+        for x in bounds:
+            if not (x.dtype is torch.int32 and x.shape == (B, columns) and columns > 0 and x.is_contiguous() and x.get_device() == device):
+                _refuse(*((y, n, (torch.int32,), (B, columns), 2) for y, n in zip(bounds, ("lts", "lte", "uts", "ute"))))
+        at = [x.data_ptr() for x in bounds]
     out = torch.empty_like(q)
     so = out.stride()
     lse = torch.empty(B, H, T, dtype=torch.float32, device=q.device)
     lib = load_library()
     if workspace is None:
         workspace = torch.empty(max(int(lib.flashmask_decode_workspace_bytes(B, H, heads, T, d)), 256), dtype=torch.uint8, device=q.device)
-    elif workspace.get_device() != device or not workspace.is_contiguous():
-        _wrong(workspace, "workspace", device)
-    _check(lib.flashmask_decode(cache, q.data_ptr(), lens_at, *at, columns, window, scale, out.data_ptr(), lse.data_ptr(), type_id, H, T,
+    _check(lib.flashmask_decode(cache, q.data_ptr(), lens.data_ptr(), *at, columns, window, scale, out.data_ptr(), lse.data_ptr(), type_id, H, T,
                                 _TWO.pack(sq[0], sq[1], sq[2], so[0], so[1], so[2]), workspace.data_ptr(),
                                 workspace.numel() * workspace.element_size(), _stream()), "flashmask_decode")
     return out, lse
@@ -201,8 +183,7 @@ def _pools(pools):
     if not pools:
         raise FlashMaskError("no pools")
     first = pools[0]
-    device = _device(first, "pools")
-    shape, strides, dtype = first.shape, first.stride(), first.dtype
+    shape, strides, dtype, device = first.shape, first.stride(), first.dtype, first.get_device()
     pages = shape[0] if shape else 0
     entry = first.numel() // max(pages, 1)
     if not first.is_contiguous():
@@ -215,6 +196,8 @@ def _pools(pools):
                 dense *= size
     if len(shape) < 2 or pages > 1 and strides[0] != entry:
         raise FlashMaskError("a pool must be indexed [pages, ...], its pages one behind the other")
+    if device < 0 or device != torch._C._cuda_getDevice():
+        _refuse((first, "pools", (dtype,), tuple(shape), 1))
     for p in pools:
         if not (p.dtype is dtype and p.shape == shape and p.stride() == strides and p.get_device() == device):
             raise FlashMaskError("the pools must have one shape, layout and type, on one GPU")
@@ -226,13 +209,19 @@ def flashmask_cache_fork(pools, table, lens, parents, new_pages, page: int):
     last page, if partly filled, is copied there in every pool (tensors [pages, ...] of `page` tokens to a page); -1: it goes on
     in its parent's."""
     where, n, page_bytes, num_pages, device = _pools(pools)
-    B, columns = entries = _dims(table, 2, "table")
-    children = _dims(parents, 1, "parents")[0]
-    at = (_index(table, entries, "table", device), _index(lens, (B,), "lens", device),
-          _index(parents, (children,), "parents", device), _index(new_pages, (children,), "new_pages", device))
+    entries, whole, ints = table.shape, parents.shape, torch.int32
+    if not (len(entries) == 2 and len(whole) == 1 and new_pages.shape == whole and lens.shape == (entries[0],) and table.dtype is ints
+            and lens.dtype is ints and parents.dtype is ints and new_pages.dtype is ints and table.is_contiguous() and lens.is_contiguous()
+            and parents.is_contiguous() and new_pages.is_contiguous()
+            and device == table.get_device() == lens.get_device() == parents.get_device() == new_pages.get_device()):
+        _refuse((table, "table", (ints,), (None, None), 2), (lens, "lens", (ints,), (entries[0],), 2), (parents, "parents", (ints,), (None,), 2),
+                (new_pages, "new_pages", (ints,), tuple(whole), 2))
+    B, columns = entries
+    children = whole[0]
     table_out, lens_out = _ints(table, children, columns), _ints(table, children)
-    _check(load_library().flashmask_cache_fork(where, n, page_bytes, num_pages, *at, table_out.data_ptr(), lens_out.data_ptr(), B,
-                                               columns, page, children, _stream()), "flashmask_cache_fork")
+    _check(load_library().flashmask_cache_fork(where, n, page_bytes, num_pages, table.data_ptr(), lens.data_ptr(), parents.data_ptr(),
+                                               new_pages.data_ptr(), table_out.data_ptr(), lens_out.data_ptr(), B, columns, page, children,
+                                               _stream()), "flashmask_cache_fork")
     return table_out, lens_out
 
 
@@ -241,24 +230,28 @@ def flashmask_cache_plan_bytes(num_pages: int) -> int:
 
 
 def _plan(lib, num_pages: int, table, workspace, device: int) -> torch.Tensor:
+    """The scratch of the two calls below, their table checked."""
+    if not (table.dtype is torch.int32 and table.is_contiguous() and table.numel() > 0 and device == table.get_device()):
+        _refuse((table, "table", (torch.int32,), tuple(table.shape), 2))
     if workspace is None:
         return torch.empty(max(int(lib.flashmask_cache_plan_bytes(num_pages)), 256), dtype=torch.uint8, device=table.device)
     if workspace.get_device() != device or not workspace.is_contiguous():
-        _wrong(workspace, "workspace", device)
+        _refuse((workspace, "workspace", (workspace.dtype,), tuple(workspace.shape), 2))
     return workspace
 
 
 def flashmask_cache_free_list(table, num_pages: int, workspace: torch.Tensor | None = None):
     """The pages that no entry of the table names, in ascending order with -1 behind them (int32 [num_pages]), and how many
     (int32 [1])."""
-    device = _device(table, "table")
-    at = _index(table, table.shape, "table", device)
+    device = table.get_device()
+    if device < 0 or device != torch._C._cuda_getDevice():
+        _refuse((table, "table", (torch.int32,), tuple(table.shape), 2))
     if num_pages <= 0:
         raise FlashMaskError("num_pages must be positive")
     lib = load_library()
     ws = _plan(lib, num_pages, table, workspace, device)
     free, count = _ints(table, num_pages), _ints(table, 1)
-    _check(lib.flashmask_cache_free_list(at, table.numel(), num_pages, free.data_ptr(), count.data_ptr(), ws.data_ptr(),
+    _check(lib.flashmask_cache_free_list(table.data_ptr(), table.numel(), num_pages, free.data_ptr(), count.data_ptr(), ws.data_ptr(),
                                          ws.numel() * ws.element_size(), _stream()), "flashmask_cache_free_list")
     return free, count
 
@@ -267,10 +260,10 @@ def flashmask_cache_compact(pools, table, workspace: torch.Tensor | None = None)
     """Move the pages that the table names to the front of every pool; (table, used) with the pages' new places and their
     number (int32 [1])."""
     where, n, page_bytes, num_pages, device = _pools(pools)
-    at = _index(table, table.shape, "table", device)
     lib = load_library()
     ws = _plan(lib, num_pages, table, workspace, device)
     table_out, used = torch.empty_like(table), _ints(table, 1)
-    _check(lib.flashmask_cache_compact(where, n, page_bytes, num_pages, at, table.numel(), table_out.data_ptr(), used.data_ptr(),
-                                       ws.data_ptr(), ws.numel() * ws.element_size(), _stream()), "flashmask_cache_compact")
+    _check(lib.flashmask_cache_compact(where, n, page_bytes, num_pages, table.data_ptr(), table.numel(), table_out.data_ptr(),
+                                       used.data_ptr(), ws.data_ptr(), ws.numel() * ws.element_size(), _stream()),
+           "flashmask_cache_compact")
     return table_out, used
