@@ -12,7 +12,7 @@
 //    elements D / 16 * m + e, m = 0..15.  The lane's results are then 4 * D / 16 consecutive elements of its query's row.
 // The probabilities go into the second product as sums of two 16-bit values, which the matrix pipe has room for.
 // Bound by memory: every wave has the next step's 16 KiB of keys and values in flight while it works on this one's.  131072 tokens, 8
-// heads of 128 elements: 96 us, 5.6 TB/s of the 6.4 that a plain reading loop reaches here, and 5 for the join.
+// heads of 128 elements: 94 us, 5.7 TB/s of the 6.4 that a plain reading loop reaches here, and 5 for the join.
 #include <algorithm>
 
 #include "fm_common.h"
