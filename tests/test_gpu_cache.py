@@ -23,6 +23,8 @@ def _ints(*x):
     (70, 6, 3, 64, 16, 32, False, True),
     (300, 8, 1, 128, 64, 48, True, False),
     (9, 0, 2, 128, 32, 0, False, False),
+    (50, 64, 8, 128, 16, 128, False, True),
+    (700, 16, 16, 64, 32, 64, True, False),
 ])
 def test_append(tokens, H, Hk, d, page, rot, interleaved, packed, type, cache):
     import paper_2410_01359_amd as fm

@@ -112,6 +112,30 @@ def test_masks(case, mask, type, cache):
     _check(_problem(100 + case, lens, H, Hk, T, d, page, type, cache, packed=case % 2 == 0, columns=columns, mask=mask), type)
 
 
+@pytest.mark.parametrize("type,cache", [("bf16", "bf16"), ("f16", "e4m3")])
+@pytest.mark.parametrize("mask", ["none", "window"])
+@pytest.mark.parametrize("B,long", [(65, 1300), (130, 1100), (64, 2000)])
+def test_more_sequences_than_lanes(B, long, mask, type, cache):
+    """Lengths are added up 64 sequences at a time: the longest on either side of a round."""
+    rng = np.random.default_rng(B)
+    lens = rng.integers(0, 40, size=B)
+    lens[[0, 63, B - 1]] = long, long - 77, long - 1
+    _check(_problem(200 + B, lens, 4, 2, 1, 64, 16, type, cache, mask=mask), type)
+
+
+@pytest.mark.parametrize("mask", ["none", "bounds"])
+@pytest.mark.parametrize("lens,H,Hk,T,d,packed", [([90, 300, 20], 2, 1, 70, 64, False), ([1500, 260], 3, 3, 40, 128, True), ([400], 2, 2, 256, 64, False)])
+def test_many_new_tokens(lens, H, Hk, T, d, packed, mask):
+    """Several blocks of query rows to a K/V head, an odd number of them among two teams of waves."""
+    _check(_problem(300 + T, lens, H, Hk, T, d, 16, "bf16", "bf16", packed=packed, mask=mask), "bf16")
+
+
+@pytest.mark.parametrize("type,cache,d", [("bf16", "bf16", 64), ("f16", "e4m3", 64), ("bf16", "e4m3", 128)])
+@pytest.mark.parametrize("H,Hk", [(3, 3), (10, 5), (40, 1), (66, 3)])
+def test_odd_numbers_of_heads_side_by_side(H, Hk, type, cache, d):
+    _check(_problem(400 + H, [700, 1090, 5], H, Hk, 1, d, 32, type, cache, packed=True), type)
+
+
 @pytest.mark.parametrize("mask", ["none", "bounds"])
 def test_pages_that_are_none(mask):
     """Holes in the table, and lengths beyond it: keys without a page are not seen."""
@@ -127,12 +151,13 @@ def test_pages_that_are_none(mask):
 
 @pytest.mark.parametrize("mask", [None, "window", "bounds"])
 @pytest.mark.parametrize("type,cache", [("bf16", "bf16"), ("f16", "e4m3")])
-def test_odd_values_that_some_rows_see(type, cache, mask):
+@pytest.mark.parametrize("lens", [[70, 90], [1100, 1470]])
+def test_odd_values_that_some_rows_see(lens, type, cache, mask):
     """NaN and infinities among the values of keys that some new rows see and others do not reach those rows alone."""
     import paper_2410_01359_amd as fm
     T, H, Hk, d, page = 4, 12, 2, 128, 16
-    a = _problem(9, [70, 90], H, Hk, T, d, page, type, "f16" if cache == "f16" else cache)
-    table, lens = a["table"].cpu().numpy(), [70, 90]
+    a = _problem(9, lens, H, Hk, T, d, page, type, "f16" if cache == "f16" else cache)
+    table = a["table"].cpu().numpy()
     if mask == "window":
         a["window"] = 20
     elif mask == "bounds":

@@ -32,6 +32,9 @@ def _bound(x, type, ref, rot, interleaved, amp):
     (3, 5, 5, 33, 128, 48, True, None),
     (1, 8, 1, 2050, 128, 64, False, "far"),
     (2, 2, 2, 130, 64, 48, True, "documents"),
+    (1, 40, 8, 37, 128, 128, True, "far"),
+    (2, 160, 3, 5, 64, 32, False, None),
+    (1, 7, 300, 11, 64, 64, True, None),
 ])
 def test_against_the_definition(B, H, Hk, N, d, rot, packed, positions, type, interleaved):
     import paper_2410_01359_amd as fm
