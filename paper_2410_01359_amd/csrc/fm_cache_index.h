@@ -45,6 +45,11 @@ FM_HOST_DEVICE inline int fm_chunk_groups(unsigned total, const FmDivisor& chunk
 }
 // Chunks of a sequence: at least one, so that somebody writes an empty sequence's rows.
 FM_HOST_DEVICE inline int fm_chunks_of(int groups, int size) { return groups > size ? (groups + size - 1) / size : 1; }
+// Groups of each of a sequence's chunks: as equal as multiples of `round` are (a last chunk may be empty), no more than the size they
+// were counted with where that is a multiple of `round`, too.
+FM_HOST_DEVICE inline int fm_even_chunk(int groups, int chunks, int round) {
+  return (int)(((unsigned)(groups + chunks - 1) / (unsigned)chunks + round - 1) / round * round);
+}
 // Chunks of all sequences together and partial results that they leave, at most: a sequence of several chunks has fewer than
 // twice its groups / size, and any has fewer than that and one.
 FM_HOST_DEVICE inline int fm_most_units(int chunks, int sequences) { return chunks + sequences; }

@@ -204,6 +204,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void decode_kernel(FmDecodeArgs a, 
     len = a.lens[b];
   }
   const FmKeyRange range = fm_key_range(len, a.T, a.window, a.columns * a.page_tokens);
+  // a sequence's chunks alike, instead of a last short one: 64 ragged sequences 88 -> 82 us, windows 46 -> 43
+  if (chunks > 1) size = fm_even_chunk(fm_key_groups(range), chunks, C::GROUPS);
   const int j_begin = range.lo + chunk * size * kGroup;
   const int j_end = (int)std::min<long long>(range.hi, j_begin + (long long)size * kGroup);
   const int first_row = range.len - a.T;   // row of query 0
@@ -675,11 +677,11 @@ FmDecodeCut fm_decode_cut(int H, int Hk, int T, int d, int B, int together, int 
   const int members = cut.row_blocks * Hk;
   cut.teams = members > 1 && (together > 1 || cut.row_blocks > 1) ? 2 : 1;
   cut.workgroups = (members + cut.teams - 1) / cut.teams;
-  // Chunks that give every compute unit its two workgroups once are best where they come out even (131072 keys 102 us, twice as many
-  // 105; 16 sequences of 16384, d = 64, 102 and 107; 16 and 32 ragged ones the same).  Each sequence leaves half a chunk over
-  // on average, so for many sequences they are half as long (64 ragged ones of up to 8192, 8 heads, 104 and 88).  Partial results in
-  // 48 MiB, and 256 to a row, which its join goes through in a few steps.
-  const long long at_once = std::max(1, 2 * (cus > 0 ? cus : 256) / cut.workgroups), wanted = 2ll * B <= at_once ? at_once : 2 * at_once;
+  // Chunks that give every compute unit its two workgroups once (131072 keys 102 us, twice as many chunks 105; 64 sequences of 1536, 8 heads,
+  // 76 and 79, ragged ones 23 and 24), but for more sequences than that, whose lengths leave more of them over (128 ragged ones
+  // of up to 4096 103 and 95, with 16 heads 197 and 181).  Partial results in 48 MiB, and 256 to a row, which its join goes through
+  // in a few steps.
+  const long long at_once = std::max(1, 2 * (cus > 0 ? cus : 256) / cut.workgroups), wanted = B <= at_once ? at_once : 2 * at_once;
   const long long bytes = (long long)Hk * R * (d + 2) * 4, room = (48ll << 20) / (2 * bytes);
   cut.chunks = (int)std::max<long long>(1, std::min({wanted, room, 256ll}));
   // A chunk's partial sums cost a join more per query row than a key does: 8 keys to a row at least (64 rows, 16 ragged sequences of up to 8192,

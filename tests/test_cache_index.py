@@ -56,6 +56,11 @@ int main() {
       CHECK(n >= 1 && (long long)n * size >= g && (n == 1 || (long long)(n - 1) * size < g));
       units += n;
       slots += n > 1 ? n : 0;
+      for (int steps : {2, 4, 8})   // groups of a wave's step; a round is a multiple of it
+        if (round % steps == 0 && n > 1) {
+          const int even = fm_even_chunk(g, n, steps);
+          CHECK(even % steps == 0 && even <= size && (long long)n * even >= g && (long long)(n - 1) * even * 16 <= INT_MAX);
+        }
     }
     CHECK(units <= fm_most_units(chunks, B));
     CHECK(slots <= fm_most_slots(chunks, B));
