@@ -654,8 +654,12 @@ static void launch(const FmDecodeArgs& a, hipStream_t stream) {
 #define FM_DECODE(NB, TEAMS) \
   hipLaunchKernelGGL((decode_kernel<D, F16, E4M3, NB, TEAMS>), grid, block, 0, stream, a, cut.row_blocks * a.Hk, di, dr, dt, dc)
   if (cut.block_rows == 16) {
-    if (cut.teams == 2) FM_DECODE(1, 2);
-    else FM_DECODE(1, 1);
+    if constexpr (E4M3 || D == 64) {   // rows of less than 256 bytes, which may go together
+      if (cut.teams == 2) FM_DECODE(1, 2);
+      else FM_DECODE(1, 1);
+    } else {
+      FM_DECODE(1, 1);
+    }
   } else {
     if (cut.teams == 2) FM_DECODE(2, 2);
     else FM_DECODE(2, 1);

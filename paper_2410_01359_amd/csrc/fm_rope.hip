@@ -7,7 +7,6 @@
 namespace fm {
 
 typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
-typedef __attribute__((ext_vector_type(8))) float f32x8;
 
 // Cosine and sine of an angle in 64 bits: reduced to [-pi/4, pi/4] in two steps (pi/2 as a sum of two doubles), then the
 // Taylor series, cut where the next term is below 2^-32.

@@ -97,6 +97,22 @@ def test_slices_of_a_projection_and_another_stream():
     assert torch.equal(ref[0], got[0]) and torch.equal(ref[1], got[1])
 
 
+@pytest.mark.parametrize("packed", [False, True])
+def test_an_output_may_be_its_own_input(packed):
+    """Through the C ABI."""
+    import ctypes
+
+    import paper_2410_01359_amd as fm
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    q, k = (strided(torch.randn((2, h, 77, 128), device="cuda", generator=gen).half(), packed) for h in (6, 3))
+    freqs = _frequencies(96)
+    want = fm.flashmask_rope(q, k, freqs, amp=1.5)
+    strides = (ctypes.c_int64 * 12)(*(2 * (*q.stride()[:3], *k.stride()[:3])))
+    assert fm.load_library().flashmask_rope(q.data_ptr(), k.data_ptr(), q.data_ptr(), k.data_ptr(), freqs.data_ptr(), None, 1, 0, 1.5,
+                                            2, 6, 3, 77, 128, 96, strides, torch.cuda.current_stream().cuda_stream) == 0
+    assert torch.equal(q, want[0]) and torch.equal(k, want[1])
+
+
 def test_refusals():
     import paper_2410_01359_amd as fm
     q = torch.zeros((2, 4, 10, 64), device="cuda", dtype=torch.bfloat16)
