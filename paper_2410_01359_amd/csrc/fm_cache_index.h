@@ -50,6 +50,8 @@ FM_HOST_DEVICE inline int fm_chunks_of(int groups, int size) { return groups > s
 FM_HOST_DEVICE inline int fm_even_chunk(int groups, int chunks, int round) {
   return (int)(((unsigned)(groups + chunks - 1) / (unsigned)chunks + round - 1) / round * round);
 }
+// Where the panel behind the one at `panel` begins: panels have `keys` keys, or 0: one has everything up to `end`.
+FM_HOST_DEVICE inline int fm_next_panel(int panel, int end, int keys) { return keys > 0 && end - panel > keys ? panel + keys : end; }
 // Chunks of all sequences together and partial results that they leave, at most: a sequence of several chunks has fewer than
 // twice its groups / size, and any has fewer than that and one.
 FM_HOST_DEVICE inline int fm_most_units(int chunks, int sequences) { return chunks + sequences; }

@@ -332,7 +332,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void decode_kernel(FmDecodeArgs a, 
     }
     barrier_nofence();
 
-    for (int panel = j_begin; panel < j_end; panel += a.bounds[0] ? C::PANEL : INT32_MAX / 2) {
+    for (int panel = j_begin; panel < j_end; panel = fm_next_panel(panel, j_end, a.bounds[0] ? C::PANEL : 0)) {
       int steps;
       if (a.bounds[0]) {
         // the steps of which some row sees a key, and whether it takes the element mask
