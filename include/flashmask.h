@@ -384,7 +384,8 @@ int flashmask_cache_append(const flashmask_cache* cache, const void* q, const vo
  * query t is row i = lens[b] - T + t and sees key j iff
  *     j <= i,   j > i - window (window > 0),   and neither LTS[j] <= i < LTE[j] nor UTS[j] <= i < UTE[j].
  * out = softmax(scale * q K^T) V and lse as for flashmask_fwd; a row that sees nothing (a sequence shorter than T, an
- * empty one) gets 0 and -inf.  Keys that a row does not see have no influence on it, whatever they and their values hold.
+ * empty one) gets 0 and -inf.  Keys that a row does not see have no influence on it, whatever they and their values hold; an
+ * infinite value of a key that it sees makes the element infinite down to a weight of 2^-126 of the largest (below: NaN).
  *   q, out      [sequences, H, T, d] of `type` (BF16, F16; that of the cache, or the cache is E4M3); strides[2] describe q
  *               and out; H is a multiple of cache->heads, query head h reads K/V head h / (H / heads)
  *   lens        int32 [sequences], values below 0 count as 0.  A key whose place has no page is not seen.

@@ -23,6 +23,7 @@ namespace fm {
 typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
 typedef __attribute__((ext_vector_type(2))) _Float16 f16x2;
 typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+typedef __attribute__((ext_vector_type(2))) unsigned short u16x2;
 
 #define FM_CONSTANT __attribute__((address_space(4)))
 
@@ -41,24 +42,30 @@ __device__ __forceinline__ unsigned pack2(float a, float b) {
   else return __builtin_bit_cast(unsigned, bf16x2{(__bf16)a, (__bf16)b});
 }
 // Probabilities enter their product as sums hi + lo of two 16-bit values: cut off and what that left, 16 bits of the
-// value for bf16, 22 for f16.  Neither is negative, and lo is never 0 where the probability is not, so that an infinite value
-// a row sees comes out as itself and not as 0 * inf.  f16 ends at 2^-24: probabilities are taken times 2^kShift there.
+// value for bf16, 22 for f16.  Neither is negative, and neither is 0 where the probability is a normal number of 32 bits: an infinite
+// value a row sees comes out as itself and not as 0 * inf.  For that each has the type's smallest value at least where the
+// probability is above 0.  f16 ends at 2^-24: probabilities are taken times 2^kShift there, and below 2^-38 count as 2^-37.
 template <bool F16>
 constexpr float kShift = F16 ? 14.f : 0.f;
 template <bool F16>
 constexpr float kUnshift = F16 ? 0x1p-14f : 1.f;
+// Two 16-bit values, neither negative (their order is that of their bits): y, but the smallest value above 0 at least where x is not 0.
+__device__ __forceinline__ unsigned at_least(unsigned y, unsigned x) {
+  return __builtin_bit_cast(unsigned, __builtin_elementwise_max(__builtin_bit_cast(u16x2, y),
+                                                                __builtin_elementwise_min(__builtin_bit_cast(u16x2, x), u16x2{1, 1})));
+}
 template <bool F16>
 __device__ __forceinline__ void split2(float a, float b, unsigned& hi, unsigned& lo) {
   if constexpr (F16) {
-    constexpr float kLeast = 0x1p-24f;
+    constexpr float kLeast = 0x1p-24f, kAbove = 0x1p102f;   // a * kAbove is at least kLeast, or 0: the middle of the three is what is wanted
     const auto h = __builtin_amdgcn_cvt_pkrtz(a, b);
-    hi = __builtin_bit_cast(unsigned, h);
-    lo = pack2<true>(fmaxf(a - (float)h[0], fminf(a, kLeast)), fmaxf(b - (float)h[1], fminf(b, kLeast)));
+    lo = pack2<true>(__builtin_amdgcn_fmed3f(a - (float)h[0], kLeast, a * kAbove), __builtin_amdgcn_fmed3f(b - (float)h[1], kLeast, b * kAbove));
+    hi = at_least(__builtin_bit_cast(unsigned, h), lo);
   } else {
-    const unsigned x = __builtin_bit_cast(unsigned, a) | 1u, y = __builtin_bit_cast(unsigned, b) | 1u;
+    const unsigned x = __builtin_bit_cast(unsigned, a), y = __builtin_bit_cast(unsigned, b);
     hi = __builtin_amdgcn_perm(y, x, 0x07060302u);
-    lo = pack2<false>(__builtin_bit_cast(float, x) - __builtin_bit_cast(float, x & 0xffff0000u),
-                      __builtin_bit_cast(float, y) - __builtin_bit_cast(float, y & 0xffff0000u));
+    lo = at_least(pack2<false>(__builtin_bit_cast(float, x) - __builtin_bit_cast(float, x & 0xffff0000u),
+                               __builtin_bit_cast(float, y) - __builtin_bit_cast(float, y & 0xffff0000u)), hi);
   }
 }
 // Four e4m3 values to 16 bits each (exact in both types).
