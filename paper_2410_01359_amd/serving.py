@@ -45,6 +45,16 @@ def _refuse(*wanted):
     raise FlashMaskError("the tensors do not go together")
 
 
+# ctypes takes the lower 32 bits of a number that does not fit an int.
+def _fits(*numbers) -> bool:
+    return -1 << 31 <= min(numbers) and max(numbers) < 1 << 31
+
+
+def _layout(layout):
+    if layout not in (FM_ROPE_HALF, FM_ROPE_INTERLEAVED):
+        raise FlashMaskError(f"layout must be FM_ROPE_HALF or FM_ROPE_INTERLEAVED, got {layout}")
+
+
 def _rope(entry: str, q, k, freqs, positions, layout, amp):
     dtype, shape, sq, sk = q.dtype, q.shape, q.stride(), k.stride()
     type_id, device = _ROPE_TYPE.get(dtype), q.get_device()
@@ -56,6 +66,7 @@ def _rope(entry: str, q, k, freqs, positions, layout, amp):
         like = (*shape, None, None, None, None)
         _refuse((q, "q", tuple(_ROPE_TYPE), (None,) * 4, 1), (k, "k", (dtype,), (like[0], None, like[2], like[3]), 1),
                 (freqs, "freqs", (torch.float64,), (None,), 2), (positions, "positions", (torch.int32,), (like[0], like[2]), 2))
+    _layout(layout)
     B, H, N, d = shape
     q_out, k_out = torch.empty_like(q), torch.empty_like(k)
     to_q, to_k = q_out.stride(), k_out.stride()
@@ -120,6 +131,7 @@ def flashmask_cache_append(k, v, k_cache, v_cache, table, seqs, positions, *, q=
         _refuse((k, "k", tuple(_ROW_TYPE), (None, heads, d), 1), (v, "v", (dtype,), (n, heads, d), 1),
                 (seqs, "seqs", (torch.int32,), (n,), 2), (positions, "positions", (torch.int32,), (n,), 2),
                 (q, "q", (dtype,), (n, None, d), 1), (freqs, "freqs", (torch.float64,), (None,), 2))
+    _layout(layout)
     H, q_at, out_at, q_out = 0, 0, 0, None
     if q is not None:
         H = q.shape[1]
@@ -136,7 +148,7 @@ def flashmask_cache_append(k, v, k_cache, v_cache, table, seqs, positions, *, q=
 
 
 def flashmask_decode_workspace_bytes(sequences: int, H: int, H_kv: int, T: int, d: int) -> int:
-    return int(load_library().flashmask_decode_workspace_bytes(sequences, H, H_kv, T, d))
+    return int(load_library().flashmask_decode_workspace_bytes(sequences, H, H_kv, T, d)) if _fits(sequences, H, H_kv, T, d) else 0
 
 
 def flashmask_decode(q, k_cache, v_cache, table, lens, scale: float, *, bounds=None, window: int = 0, k_scale=None, v_scale=None,
@@ -152,6 +164,9 @@ def flashmask_decode(q, k_cache, v_cache, table, lens, scale: float, *, bounds=N
             and (workspace is None or workspace.get_device() == device and workspace.is_contiguous())):
         _refuse((q, "q", tuple(_ROW_TYPE), (B, None, None, d), 1), (lens, "lens", (torch.int32,), (B,), 2),
                 *(() if workspace is None else ((workspace, "workspace", (workspace.dtype,), tuple(workspace.shape), 2),)))
+    if window < 0:
+        raise FlashMaskError(f"window must not be negative, got {window}")
+    window = min(window, 0x7fffffff)    # no table holds as many keys
     H, T = shape[1], shape[2]
     at, columns = (0, 0, 0, 0), 0
     if bounds is not None:
@@ -216,6 +231,8 @@ def flashmask_cache_fork(pools, table, lens, parents, new_pages, page: int):
             and device == table.get_device() == lens.get_device() == parents.get_device() == new_pages.get_device()):
         _refuse((table, "table", (ints,), (None, None), 2), (lens, "lens", (ints,), (entries[0],), 2), (parents, "parents", (ints,), (None,), 2),
                 (new_pages, "new_pages", (ints,), tuple(whole), 2))
+    if not _fits(page):
+        raise FlashMaskError(f"page is out of range: {page}")
     B, columns = entries
     children = whole[0]
     table_out, lens_out = _ints(table, children, columns), _ints(table, children)
@@ -226,7 +243,7 @@ def flashmask_cache_fork(pools, table, lens, parents, new_pages, page: int):
 
 
 def flashmask_cache_plan_bytes(num_pages: int) -> int:
-    return int(load_library().flashmask_cache_plan_bytes(num_pages))
+    return int(load_library().flashmask_cache_plan_bytes(num_pages)) if _fits(num_pages) else 0
 
 
 def _plan(lib, num_pages: int, table, workspace, device: int) -> torch.Tensor:
@@ -246,8 +263,8 @@ def flashmask_cache_free_list(table, num_pages: int, workspace: torch.Tensor | N
     device = table.get_device()
     if device < 0 or device != torch._C._cuda_getDevice():
         _refuse((table, "table", (torch.int32,), tuple(table.shape), 2))
-    if num_pages <= 0:
-        raise FlashMaskError("num_pages must be positive")
+    if num_pages <= 0 or not _fits(num_pages):
+        raise FlashMaskError(f"num_pages must be positive and fit 32 bits, got {num_pages}")
     lib = load_library()
     ws = _plan(lib, num_pages, table, workspace, device)
     free, count = _ints(table, num_pages), _ints(table, 1)
