@@ -313,7 +313,7 @@ int flashmask_atomic_ceiling(float* acc, int heads, int n_tiles, int tiles, int 
  * The conventions at the top of this file hold here too (device pointers, streams, no allocation, no synchronisation,
  * graph capture), with these differences: several element types, sequences of their own lengths, and index values (pages,
  * sequences, positions) that live on the device.  An index value out of its range is never followed: what each entry
- * point does then is said at it.
+ * point does then is said at it.  Sizes beyond the limits that are given here are refused with FM_ERR_SHAPE before anything is launched.
  */
 
 /* Element types. */
@@ -337,6 +337,7 @@ enum { FM_ROPE_HALF = 0, FM_ROPE_INTERLEAVED = 1 };
  *   freqs          double [rot / 2]
  *   positions      int32 [B,N], any values; NULL: 0 .. N - 1 in every batch row
  *   rot            a multiple of 16, 0 < rot <= d; d is 64 or 128
+ *   H, H_kv        any, at most 16384 each;  B * N at most 2^27 - 256
  * flashmask_rope_bwd takes the gradients of q_out and k_out to those of q and k: the turn by the opposite angle.
  */
 int flashmask_rope(const void* q, const void* k, void* q_out, void* k_out, const double* freqs, const int32_t* positions,
@@ -359,9 +360,9 @@ typedef struct {
   const float* v_scale;     /* required for E4M3, NULL otherwise */
   const int32_t* table;     /* int32 [sequences, columns] */
   int32_t type;             /* FM_TYPE_BF16, FM_TYPE_F16 or FM_TYPE_E4M3 */
-  int32_t heads, d;         /* K/V heads; 64 or 128 */
-  int32_t num_pages, page;  /* pages; tokens of a page, a multiple of 16 */
-  int32_t sequences, columns;
+  int32_t heads, d;         /* K/V heads, at most 16384; 64 or 128 */
+  int32_t num_pages, page;  /* pages; tokens of a page, a multiple of 16, at most 2^20 */
+  int32_t sequences, columns;  /* columns * page at most 2^30 */
 } flashmask_cache;
 
 /*
@@ -373,7 +374,7 @@ typedef struct {
  *               page at that place nothing is written.
  *   freqs, layout, amp, rot   as for flashmask_rope; freqs == NULL: nothing is rotated (q must be NULL)
  * Keys go from the 32-bit result of the rotation to the cache's type in one rounding; an E4M3 cache takes value / scale,
- * held to +-448.  Two tokens of one call must not have the same place.
+ * held to +-448.  Two tokens of one call must not have the same place.  At most 2^27 tokens and 16384 query heads.
  */
 int flashmask_cache_append(const flashmask_cache* cache, const void* q, const void* k, const void* v, void* q_out,
                            const int32_t* seqs, const int32_t* positions, const double* freqs, int type, int layout,
@@ -395,6 +396,8 @@ int flashmask_cache_append(const flashmask_cache* cache, const void* q, const vo
  *   workspace   at least flashmask_decode_workspace_bytes(), 256-byte aligned
  * Long sequences are split over workgroups and joined by a second launch; how follows from lens on the device.  The same
  * call gives the same bits every time.
+ * Limits: 65535 sequences, H * T * sequences <= 2^30, sequences * columns * page <= 2^34, and sequences * heads * blocks (of 32 query
+ * rows that share a K/V head) below about 2^25.  Where flashmask_decode_workspace_bytes is not 0 its arguments are within them.
  */
 int flashmask_decode(const flashmask_cache* cache, const void* q, const int32_t* lens, const int32_t* lts,
                      const int32_t* lte, const int32_t* uts, const int32_t* ute, int bound_columns, int window, float scale,
@@ -412,7 +415,8 @@ size_t flashmask_decode_workspace_bytes(int sequences, int H, int H_kv, int T, i
  *   pools       HOST array of num_pools device pointers, each to num_pages pages of page_bytes contiguous bytes (a
  *               multiple of 16): all layers' keys and values
  * A parent outside [0, sequences) gives an empty child; no page is copied from or to a place outside the pools.  The pages of
- * new_pages must differ from each other and from those in use; table_out, lens_out must not overlap table, lens.
+ * new_pages must differ from each other and from those in use; table_out, lens_out must not overlap table, lens.  At most 65535 children,
+ * page_bytes at most 2^30.  Where a child gets a page of its own and its parent has none there, the page keeps what it holds.
  */
 int flashmask_cache_fork(void* const* pools, int num_pools, size_t page_bytes, int num_pages, const int32_t* table,
                          const int32_t* lens, const int32_t* parents, const int32_t* new_pages, int32_t* table_out,
@@ -420,7 +424,8 @@ int flashmask_cache_fork(void* const* pools, int num_pools, size_t page_bytes, i
 
 /*
  * The pages that no entry of the table names, in ascending order, -1 behind them, and their number.
- *   free_pages  int32 [num_pages], count int32 [1];  workspace: flashmask_cache_plan_bytes(num_pages)
+ *   free_pages  int32 [num_pages], count int32 [1];  workspace: flashmask_cache_plan_bytes(num_pages), 256-byte aligned
+ *   entries, num_pages   at most 2^30 each, here and below
  */
 int flashmask_cache_free_list(const int32_t* table, int entries, int num_pages, int32_t* free_pages, int32_t* count,
                               void* workspace, size_t workspace_bytes, void* hip_stream);

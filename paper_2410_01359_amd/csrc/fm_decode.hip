@@ -161,14 +161,14 @@ __global__ __launch_bounds__(64 * kWaves, 2) void decode_kernel(FmDecodeArgs a, 
   // Barriers here order LDS alone (barrier_nofence): loads stay in flight across them.
   // The launch arguments that come first, read together: left where they are first needed they are six round trips in a row.
   asm volatile("" ::"s"(a.plan), "s"(a.lens), "s"(a.B), "s"(a.T), "s"(a.window), "s"(a.columns), "s"(a.page_tokens), "s"(a.cut.least),
-               "s"(inner.factor), "s"(row_blocks.factor), "s"(chunks_meant.factor), "s"(members));
+               "s"(a.first_workgroup), "s"(inner.factor), "s"(row_blocks.factor), "s"(chunks_meant.factor), "s"(members));
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int g = lane >> 4, c = lane & 15;
   // Workgroup -> chunk of a sequence, K/V head, block of query rows.  Workgroup x runs on XCD x % 8: all heads of a chunk on one,
   // one behind the other, because they share page table entries, bounds, and cache lines where heads lie next to each other.
-  const int slot_of_xcd = blockIdx.x >> 3;
+  const int workgroup = a.first_workgroup + blockIdx.x, slot_of_xcd = workgroup >> 3;
   const int turn = fm_div(slot_of_xcd, inner), pair = slot_of_xcd - turn * (int)inner.n;
-  const int unit = turn * 8 + (blockIdx.x & 7);
+  const int unit = turn * 8 + (workgroup & 7);
   const int team = wave % TEAMS, team_wave = wave / TEAMS, team_thread = team_wave * 64 + lane;
   const bool idle = pair * TEAMS + team >= members;   // a last team without a partner
   const int member = idle ? members - 1 : pair * TEAMS + team;
@@ -653,23 +653,26 @@ __global__ __launch_bounds__(256) void join_kernel(FmDecodeArgs a, FmDivisor row
 }
 
 template <int D, bool F16, bool E4M3>
-static void launch(const FmDecodeArgs& a, hipStream_t stream) {
+static void launch(FmDecodeArgs a, hipStream_t stream) {
+  constexpr int kMost = 1 << 23;   // workgroups of a launch, which has fewer than 2^32 lanes
   const FmDecodeCut& cut = a.cut;
-  const int units = a.plan ? fm_most_units(cut.chunks, a.B) : a.B;
-  const dim3 grid((unsigned)((units + 7) / 8 * 8 * cut.workgroups)), block(64 * kWaves);
+  const int units = a.plan ? fm_most_units(cut.chunks, a.B) : a.B, workgroups = (units + 7) / 8 * 8 * cut.workgroups;
   const FmDivisor di = fm_divisor(cut.workgroups), dr = fm_divisor(cut.row_blocks), dt = fm_divisor(a.T), dc = fm_divisor(cut.chunks);
-#define FM_DECODE(NB, TEAMS) \
-  hipLaunchKernelGGL((decode_kernel<D, F16, E4M3, NB, TEAMS>), grid, block, 0, stream, a, cut.row_blocks * a.Hk, di, dr, dt, dc)
-  if (cut.block_rows == 16) {
-    if constexpr (E4M3 || D == 64) {   // rows of less than 256 bytes, which may go together
-      if (cut.teams == 2) FM_DECODE(1, 2);
-      else FM_DECODE(1, 1);
+#define FM_DECODE(NB, TEAMS)                                                                                                      \
+  hipLaunchKernelGGL((decode_kernel<D, F16, E4M3, NB, TEAMS>), dim3((unsigned)std::min(workgroups - a.first_workgroup, kMost)), \
+                     dim3(64 * kWaves), 0, stream, a, cut.row_blocks * a.Hk, di, dr, dt, dc)
+  for (a.first_workgroup = 0; a.first_workgroup < workgroups; a.first_workgroup += kMost) {
+    if (cut.block_rows == 16) {
+      if constexpr (E4M3 || D == 64) {   // rows of less than 256 bytes, which may go together
+        if (cut.teams == 2) FM_DECODE(1, 2);
+        else FM_DECODE(1, 1);
+      } else {
+        FM_DECODE(1, 1);
+      }
     } else {
-      FM_DECODE(1, 1);
+      if (cut.teams == 2) FM_DECODE(2, 2);
+      else FM_DECODE(2, 1);
     }
-  } else {
-    if (cut.teams == 2) FM_DECODE(2, 2);
-    else FM_DECODE(2, 1);
   }
 #undef FM_DECODE
   if (a.plan) {

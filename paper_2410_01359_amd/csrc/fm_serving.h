@@ -72,6 +72,7 @@ struct FmDecodeArgs {
   float* part;
   float2* stat;
   FmDecodeCut cut;
+  int first_workgroup;    // of the launch
 };
 hipError_t fm_launch_decode(const FmDecodeArgs& a, bool f16, bool e4m3, hipStream_t stream);
 

@@ -70,10 +70,13 @@ int check_row_type(int type, const flashmask_cache& c) {
   return c.type == FM_TYPE_E4M3 || c.type == type ? FM_OK : FM_ERR_ARG;
 }
 
-// Queries that flashmask_decode's indexing has room for.
+// Shapes that flashmask_decode's indexing and its launches have room for, whatever the cache: of workgroups that take two heads together where
+// there are several; those that take one are up to twice as many.
 int check_decode_shape(int sequences, int H, int Hk, int T, int d) {
   if (sequences <= 0 || H <= 0 || H > FM_MOST_HEADS || Hk <= 0 || H % Hk || T <= 0 || T > FM_MOST_NEW_TOKENS || bad_head_dim(d)) return FM_ERR_SHAPE;
   if ((long long)H * T > (1 << 24) || sequences > 65535 || (long long)H * T * sequences > (1ll << 30)) return FM_ERR_SHAPE;
+  const FmDecodeCut cut = fm_decode_cut(H, Hk, T, d, sequences, 2, fm_compute_units());
+  if ((fm_most_units(cut.chunks, sequences) + 8ll) * cut.workgroups >= 1 << 24) return FM_ERR_SHAPE;
   return FM_OK;
 }
 struct DecodeSpace {
@@ -192,8 +195,6 @@ int flashmask_decode(const flashmask_cache* cache, const void* q, const int32_t*
   const int row = cache->d * element_bytes(cache->type);
   const bool side_by_side = a.k.head < 256 && a.v.head < 256;
   a.cut = fm_decode_cut(H, cache->heads, T, cache->d, cache->sequences, side_by_side && row < 256 ? 2 : 1, fm_compute_units());
-  // a launch has fewer than 2^32 lanes
-  if ((fm_most_units(a.cut.chunks, cache->sequences) + 8ll) * a.cut.workgroups >= 1 << 24) return FM_ERR_SHAPE;
   const bool split = (long long)cache->columns * cache->page > whole_keys(cache->sequences, a.cut);
   const DecodeSpace space = decode_space(a.cut, cache->sequences, H, T, cache->d);
   a.plan = split ? (int2*)ws : nullptr;
