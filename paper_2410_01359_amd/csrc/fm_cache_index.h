@@ -57,6 +57,10 @@ FM_HOST_DEVICE inline int fm_next_panel(int panel, int end, int keys) { return k
 FM_HOST_DEVICE inline int fm_most_units(int chunks, int sequences) { return chunks + sequences; }
 FM_HOST_DEVICE inline int fm_most_slots(int chunks, int sequences) { return chunks < sequences ? 2 * chunks : chunks + sequences; }
 
+// Split sequences at most: each has two partial results at least.  Units of a launch: those above, in whole rounds of the XCDs.
+FM_HOST_DEVICE inline int fm_most_splits(int chunks, int sequences) { return chunks < sequences ? chunks : sequences; }
+FM_HOST_DEVICE inline int fm_listed_units(int chunks, int sequences) { return (fm_most_units(chunks, sequences) + 7) / 8 * 8; }
+
 // Row of a fork's child: what its column c holds.  `entry`: the parent's, -1 without a known parent.
 struct FmFork {
   int last;      // column of the last page

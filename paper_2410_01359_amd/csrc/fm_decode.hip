@@ -160,7 +160,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void decode_kernel(FmDecodeArgs a, 
   __shared__ typename C::Shared sh;
   // Barriers here order LDS alone (barrier_nofence): loads stay in flight across them.
   // The launch arguments that come first, read together: left where they are first needed they are six round trips in a row.
-  asm volatile("" ::"s"(a.plan), "s"(a.lens), "s"(a.B), "s"(a.T), "s"(a.window), "s"(a.columns), "s"(a.page_tokens), "s"(a.cut.least),
+  asm volatile("" ::"s"(a.units), "s"(a.plan), "s"(a.lens), "s"(a.B), "s"(a.T), "s"(a.window), "s"(a.columns), "s"(a.page_tokens), "s"(a.cut.least),
                "s"(a.first_workgroup), "s"(inner.factor), "s"(row_blocks.factor), "s"(chunks_meant.factor), "s"(members));
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int g = lane >> 4, c = lane & 15;
@@ -175,9 +175,17 @@ __global__ __launch_bounds__(64 * kWaves, 2) void decode_kernel(FmDecodeArgs a, 
   const int hk = fm_div(member, row_blocks), rb = member - hk * (int)row_blocks.n;
 
   // Chunk: all sequences' keys together are cut into about a.cut.chunks pieces, each sequence into whole ones of that size.  Every wave works
-  // this out for itself, 64 sequences at a time; up to 64 their lengths are read once.
-  int b = unit, chunk = 0, chunks = 1, slot = 0, size = INT32_MAX / 32, len;   // size: in groups
-  if (a.plan) {
+  // this out for itself, 64 sequences at a time; up to 64 their lengths are read once.  Where that is too much work the list of units has it.
+  int b = unit, chunk = 0, chunks = 1, slot = 0, size = 1 << 26, len;   // size: in groups, more than any table's
+  if (a.units) {
+    const FM_CONSTANT int* entry = (const FM_CONSTANT int*)(a.units + unit);
+    b = entry[0];
+    if (b < 0) return;
+    len = entry[1];
+    chunk = entry[2] & 0xffff;
+    chunks = entry[2] >> 16;
+    slot = entry[3];
+  } else if (a.plan) {
     int lane_len = lane < a.B ? a.lens[lane] : 0;
     const auto lane_groups = [&](int base) {
       if (a.B > 64) lane_len = base + lane < a.B ? a.lens[base + lane] : 0;
@@ -589,13 +597,61 @@ __global__ __launch_bounds__(64 * kWaves, 2) void decode_kernel(FmDecodeArgs a, 
   }
 }
 
+// The list of units: one workgroup goes over the lengths twice, 1024 at a time, and lists each sequence's chunks, for workgroups that do not go
+// over all lengths themselves, which takes a call time with the square of its sequences.
+constexpr int kPlanThreads = 1024;
+__global__ __launch_bounds__(kPlanThreads) void plan_units_kernel(FmDecodeArgs a, FmDivisor chunks_meant, int round, int units, int splits) {
+  __shared__ int sums[2][3][kPlanThreads / 64];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const auto groups_of = [&](int len) { return fm_key_groups(fm_key_range(len, a.T, a.window, a.columns * a.page_tokens)); };
+  int mine = 0;
+  for (int b = tid; b < a.B; b += kPlanThreads) mine += groups_of(a.lens[b]);
+  const int upto = wave_scan(mine);
+  if (lane == 63) sums[1][0][wave] = upto;
+  __syncthreads();
+  unsigned total = 0;
+#pragma unroll
+  for (int w = 0; w < kPlanThreads / 64; ++w) total += sums[1][0][w];
+  const int size = fm_chunk_groups(total, chunks_meant, a.cut.least, round);
+  int before[3] = {0, 0, 0};   // units, slots, split sequences
+  for (int base = 0, turn = 0; base < a.B; base += kPlanThreads, turn ^= 1) {
+    const int b = base + tid, len = b < a.B ? a.lens[b] : 0, n = b < a.B ? fm_chunks_of(groups_of(len), size) : 0;
+    const int x[3] = {n, n > 1 ? n : 0, n > 1};
+    int at[3];
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+      at[i] = wave_scan(x[i]);
+      if (lane == 63) sums[turn][i][wave] = at[i];
+    }
+    __syncthreads();   // the other turn's sums have been read before this one's are written again
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+      at[i] += before[i] - x[i];
+#pragma unroll
+      for (int w = 0; w < kPlanThreads / 64; ++w) {
+        const int sum = sums[turn][i][w];
+        if (w < wave) at[i] += sum;
+        before[i] += sum;
+      }
+    }
+    for (int c = 0; c < n; ++c) a.units[at[0] + c] = int4{b, len, c | n << 16, at[1]};
+    if (n > 1) {
+      a.plan[b] = int2{at[1], n};
+      a.split[at[2]] = b;
+    }
+  }
+  for (int i = before[0] + tid; i < units; i += kPlanThreads) a.units[i] = int4{-1, 0, 0, 0};
+  for (int i = before[2] + tid; i < splits; i += kPlanThreads) a.split[i] = -1;
+}
+
 // Joins the chunks of a row of a split sequence: D / 4 lanes take a chunk's sums of p v, the workgroup 1024 / D chunks at a time.  Bound by
 // its chain of round trips, 4 to 5 us.
 template <int D, bool F16>
 __global__ __launch_bounds__(256) void join_kernel(FmDecodeArgs a, FmDivisor rows, FmDivisor tokens) {
   constexpr int LANES = D / 4, TEAMS = 256 / LANES, BATCH = 4;
   const int G = a.H / a.Hk, R = G * a.T;
-  const int b = blockIdx.y, hk = fm_div(blockIdx.x, rows), r = blockIdx.x - hk * R;   // row of the K/V head
+  const int b = a.split ? a.split[blockIdx.y] : blockIdx.y, hk = fm_div(blockIdx.x, rows), r = blockIdx.x - hk * R;   // row of the K/V head
+  if (b < 0) return;
   const int2 plan = a.plan[b];
   if (plan.y <= 1) return;
   const int team = threadIdx.x / LANES, lane = threadIdx.x % LANES;
@@ -656,11 +712,15 @@ template <int D, bool F16, bool E4M3>
 static void launch(FmDecodeArgs a, hipStream_t stream) {
   constexpr int kMost = 1 << 23;   // workgroups of a launch, which has fewer than 2^32 lanes
   const FmDecodeCut& cut = a.cut;
-  const int units = a.plan ? fm_most_units(cut.chunks, a.B) : a.B, workgroups = (units + 7) / 8 * 8 * cut.workgroups;
+  const int units = a.plan ? fm_listed_units(cut.chunks, a.B) : (a.B + 7) / 8 * 8, workgroups = units * cut.workgroups;
   const FmDivisor di = fm_divisor(cut.workgroups), dr = fm_divisor(cut.row_blocks), dt = fm_divisor(a.T), dc = fm_divisor(cut.chunks);
 #define FM_DECODE(NB, TEAMS)                                                                                                      \
   hipLaunchKernelGGL((decode_kernel<D, F16, E4M3, NB, TEAMS>), dim3((unsigned)std::min(workgroups - a.first_workgroup, kMost)), \
                      dim3(64 * kWaves), 0, stream, a, cut.row_blocks * a.Hk, di, dr, dt, dc)
+  if (a.units)   // (round: groups of a workgroup's step)
+    hipLaunchKernelGGL(plan_units_kernel, dim3(1), dim3(kPlanThreads), 0, stream, a, dc,
+                       kWaves / cut.teams * (cut.block_rows == 16 ? Decode<D, F16, E4M3, 1>::GROUPS : Decode<D, F16, E4M3, 2>::GROUPS),
+                       units, fm_most_splits(cut.chunks, a.B));
   for (a.first_workgroup = 0; a.first_workgroup < workgroups; a.first_workgroup += kMost) {
     if (cut.block_rows == 16) {
       if constexpr (E4M3 || D == 64) {   // rows of less than 256 bytes, which may go together
@@ -677,7 +737,7 @@ static void launch(FmDecodeArgs a, hipStream_t stream) {
 #undef FM_DECODE
   if (a.plan) {
     const int R = a.H / a.Hk * a.T;
-    hipLaunchKernelGGL((join_kernel<D, F16>), dim3(a.Hk * R, a.B), dim3(256), 0, stream, a, fm_divisor(R), dt);
+    hipLaunchKernelGGL((join_kernel<D, F16>), dim3(a.Hk * R, a.split ? fm_most_splits(cut.chunks, a.B) : a.B), dim3(256), 0, stream, a, fm_divisor(R), dt);
   }
 }
 
@@ -702,6 +762,11 @@ FmDecodeCut fm_decode_cut(int H, int Hk, int T, int d, int B, int together, int 
   // 43 us, with 4 and 16 keys 53 and 48), and two steps of the workgroup.
   cut.least = std::max(128, 8 * R) / FM_KEY_GROUP;
   cut.slots = fm_most_slots(cut.chunks, B);
+  // A workgroup goes over all lengths in rounds of 64, about 1 us each; the list of units takes a launch of 3 us before them all.  Rounds of all
+  // workgroups over their 2 * cus places, without and with the list: 8 heads and 128 / 192 / 1024 / 8192 sequences of up to 40
+  // keys (4, 9, 256, 16384) 18.7, 26.5, 187, 6821 us and 17.8, 22.4, 80, 611; of 400 to 1100 keys 81, 111, 541 and 85, 115, 527; a single head,
+  // 384 and 512 of up to 200 (4.5, 8) 15.2, 19.3 and 15.9, 16.5; 32 and 64 heads, 64 sequences of up to 200 (4, 8) 36, 61 and 37, 60.
+  cut.listed = (B + 63) / 64 * (long long)B * cut.workgroups > 4 * 2ll * (cus > 0 ? cus : 256);
   return cut;
 }
 

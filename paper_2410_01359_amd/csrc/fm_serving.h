@@ -52,6 +52,7 @@ struct FmDecodeCut {
   int teams, workgroups;        // heads and row blocks that a workgroup takes, workgroups to a chunk of keys
   int chunks, slots;            // that all keys of a head are meant to be cut into; partial results of a head at most
   int least;                    // groups of keys of a chunk at least
+  bool listed;                  // whether a launch of its own lists the chunks of split calls
 };
 // together: heads, 1 or 2, whose rows of a token make up a run of memory that is best read together.
 FmDecodeCut fm_decode_cut(int H, int Hk, int T, int d, int B, int together, int cus);
@@ -69,6 +70,8 @@ struct FmDecodeArgs {
   FmDivisor page;
   // scratch of split sequences: {first slot, chunks} of a sequence; per slot and K/V head the rows' sums of p v, and {max, sum of p}
   int2* plan;
+  int4* units;            // (cut.listed) {sequence, length, chunk | chunks << 16, first slot}, sequence = -1: none
+  int* split;             // and the split sequences, -1 behind them
   float* part;
   float2* stat;
   FmDecodeCut cut;

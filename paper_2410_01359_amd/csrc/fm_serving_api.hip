@@ -80,12 +80,14 @@ int check_decode_shape(int sequences, int H, int Hk, int T, int d) {
   return FM_OK;
 }
 struct DecodeSpace {
-  size_t stat, part, total;   // behind the plan, which comes first
+  size_t units, split, stat, part, total;   // behind the plan, which comes first
 };
 DecodeSpace decode_space(const FmDecodeCut& cut, int sequences, int H, int T, int d) {
   const size_t rows = (size_t)cut.slots * H * T;
   DecodeSpace s;
-  s.stat = ((size_t)sequences * sizeof(int2) + 255) / 256 * 256;
+  s.units = ((size_t)sequences * sizeof(int2) + 255) / 256 * 256;
+  s.split = s.units + (cut.listed ? (size_t)fm_listed_units(cut.chunks, sequences) * sizeof(int4) : 0);
+  s.stat = (s.split + (cut.listed ? (size_t)fm_most_splits(cut.chunks, sequences) * sizeof(int) : 0) + 255) / 256 * 256;
   s.part = (s.stat + rows * sizeof(float2) + 255) / 256 * 256;
   s.total = s.part + rows * d * sizeof(float);
   return s;
@@ -197,7 +199,10 @@ int flashmask_decode(const flashmask_cache* cache, const void* q, const int32_t*
   a.cut = fm_decode_cut(H, cache->heads, T, cache->d, cache->sequences, side_by_side && row < 256 ? 2 : 1, fm_compute_units());
   const bool split = (long long)cache->columns * cache->page > whole_keys(cache->sequences, a.cut);
   const DecodeSpace space = decode_space(a.cut, cache->sequences, H, T, cache->d);
+  const bool listed = split && a.cut.listed;
   a.plan = split ? (int2*)ws : nullptr;
+  a.units = listed ? (int4*)(ws + space.units) : nullptr;
+  a.split = listed ? (int*)(ws + space.split) : nullptr;
   a.stat = (float2*)(ws + space.stat);
   a.part = (float*)(ws + space.part);
   return done(fm_launch_decode(a, type == FM_TYPE_F16, cache->type == FM_TYPE_E4M3, (hipStream_t)hip_stream));
