@@ -57,6 +57,20 @@ FM_HOST_DEVICE inline int fm_next_panel(int panel, int end, int keys) { return k
 FM_HOST_DEVICE inline int fm_most_units(int chunks, int sequences) { return chunks + sequences; }
 FM_HOST_DEVICE inline int fm_most_slots(int chunks, int sequences) { return chunks < sequences ? 2 * chunks : chunks + sequences; }
 
+// Sequences of tables up to this many keys are not split: one launch.  round, least: groups that the waves of a team take in a step, and of a
+// chunk at least; workgroups: of such a call.  What cannot be split goes whole; a splitting call's second launch and longer way to
+// its first keys cost about three steps, and the more the fuller the chip is; a table says how long sequences may be, not how long they
+// are, so that 1024 keys are the most.  Steps of 64 keys (two teams of 32 query rows) count as 128, of 512 (d = 64, 8 bits) as 256.
+// us whole / split, 8 K/V heads, d = 128, 16 bits (step 128): one sequence of 384 / 512 / 640 keys 8.7/9.9, 9.8/9.8, 10.8/9.9; 16 of 768
+// 14.1/17.6, of up to 768 12.9/13.3, of up to 1280 18.3/17.4; 64 of 1024 44.8/47.4.  One sequence, d = 64 (step 256), 768 / 1024 keys 9.9/10.8,
+// 11.4/10.8; 8 bits 11.6/12.3, 11.7/12.6, of 1280 14.4/12.6.  Over 1068 such points calls take 0.2 % more than on the better side of each.
+FM_HOST_DEVICE inline long long fm_whole_keys(int round, long long workgroups, int least, int cus) {
+  long long keys = round * FM_KEY_GROUP;
+  keys = keys < 128 ? 128 : keys > 256 ? 256 : keys;
+  keys *= 3 + 6 * workgroups / (cus > 0 ? cus : 256);
+  if (keys > 1024) keys = 1024;
+  return keys > (long long)least * FM_KEY_GROUP ? keys : (long long)least * FM_KEY_GROUP;
+}
 // Split sequences at most: each has two partial results at least.  Units of a launch: those above, in whole rounds of the XCDs.
 FM_HOST_DEVICE inline int fm_most_splits(int chunks, int sequences) { return chunks < sequences ? chunks : sequences; }
 FM_HOST_DEVICE inline int fm_listed_units(int chunks, int sequences) { return (fm_most_units(chunks, sequences) + 7) / 8 * 8; }

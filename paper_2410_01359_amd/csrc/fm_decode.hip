@@ -708,6 +708,11 @@ __global__ __launch_bounds__(256) void join_kernel(FmDecodeArgs a, FmDivisor row
   if (lane == 0) a.lse[((size_t)b * a.H + h) * a.T + t] = total == 0.f ? -INFINITY : (top + fast_log2(total * kUnshift<F16>)) * kLn2;
 }
 
+template <int D, bool E4M3>
+static int round_groups(const FmDecodeCut& cut) {
+  return kWaves / cut.teams * (cut.block_rows == 16 ? Decode<D, false, E4M3, 1>::GROUPS : Decode<D, false, E4M3, 2>::GROUPS);
+}
+
 template <int D, bool F16, bool E4M3>
 static void launch(FmDecodeArgs a, hipStream_t stream) {
   constexpr int kMost = 1 << 23;   // workgroups of a launch, which has fewer than 2^32 lanes
@@ -717,10 +722,9 @@ static void launch(FmDecodeArgs a, hipStream_t stream) {
 #define FM_DECODE(NB, TEAMS)                                                                                                      \
   hipLaunchKernelGGL((decode_kernel<D, F16, E4M3, NB, TEAMS>), dim3((unsigned)std::min(workgroups - a.first_workgroup, kMost)), \
                      dim3(64 * kWaves), 0, stream, a, cut.row_blocks * a.Hk, di, dr, dt, dc)
-  if (a.units)   // (round: groups of a workgroup's step)
+  if (a.units)
     hipLaunchKernelGGL(plan_units_kernel, dim3(1), dim3(kPlanThreads), 0, stream, a, dc,
-                       kWaves / cut.teams * (cut.block_rows == 16 ? Decode<D, F16, E4M3, 1>::GROUPS : Decode<D, F16, E4M3, 2>::GROUPS),
-                       units, fm_most_splits(cut.chunks, a.B));
+                       round_groups<D, E4M3>(cut), units, fm_most_splits(cut.chunks, a.B));
   for (a.first_workgroup = 0; a.first_workgroup < workgroups; a.first_workgroup += kMost) {
     if (cut.block_rows == 16) {
       if constexpr (E4M3 || D == 64) {   // rows of less than 256 bytes, which may go together
@@ -768,6 +772,11 @@ FmDecodeCut fm_decode_cut(int H, int Hk, int T, int d, int B, int together, int 
   // 384 and 512 of up to 200 (4.5, 8) 15.2, 19.3 and 15.9, 16.5; 32 and 64 heads, 64 sequences of up to 200 (4, 8) 36, 61 and 37, 60.
   cut.listed = (B + 63) / 64 * (long long)B * cut.workgroups > 4 * 2ll * (cus > 0 ? cus : 256);
   return cut;
+}
+
+int fm_decode_round_groups(int d, bool e4m3, const FmDecodeCut& cut) {
+  if (d == 64) return e4m3 ? fm::round_groups<64, true>(cut) : fm::round_groups<64, false>(cut);
+  return e4m3 ? fm::round_groups<128, true>(cut) : fm::round_groups<128, false>(cut);
 }
 
 hipError_t fm_launch_decode(const FmDecodeArgs& a, bool f16, bool e4m3, hipStream_t stream) {

@@ -56,6 +56,8 @@ struct FmDecodeCut {
 };
 // together: heads, 1 or 2, whose rows of a token make up a run of memory that is best read together.
 FmDecodeCut fm_decode_cut(int H, int Hk, int T, int d, int B, int together, int cus);
+// Groups of 16 keys that the waves of a team take in one step.
+int fm_decode_round_groups(int d, bool e4m3, const FmDecodeCut& cut);
 struct FmDecodeArgs {
   const void* q;
   void* out;

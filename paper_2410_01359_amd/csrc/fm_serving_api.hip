@@ -99,10 +99,6 @@ size_t decode_bytes(int sequences, int H, int Hk, int T, int d) {
     most = std::max(most, decode_space(fm_decode_cut(H, Hk, T, d, sequences, together, fm_compute_units()), sequences, H, T, d).total);
   return most;
 }
-// Sequences of tables up to this many keys are not split: one launch.  A single sequence, 8 K/V heads, 384 / 512 / 1024 keys: 8.8 / 10.7 /
-// 17.6 us whole, 9.4 split; 16 of 768 / 1024: 16.0 / 19.0 and 16.3 / 18.5; 64 of 1024: 51.6 and 53.4, of up to 1024 (ragged) 22.6 and 21.0.
-long long whole_keys(int sequences, const FmDecodeCut& cut) { return std::min(1024ll, 320 + 3ll * sequences * cut.workgroups); }
-
 int check_pools(void* const* pools, int num_pools, size_t page_bytes, int num_pages) {
   if (num_pools < 0 || num_pages <= 0) return FM_ERR_SHAPE;
   if (num_pools == 0) return FM_OK;
@@ -197,7 +193,9 @@ int flashmask_decode(const flashmask_cache* cache, const void* q, const int32_t*
   const int row = cache->d * element_bytes(cache->type);
   const bool side_by_side = a.k.head < 256 && a.v.head < 256;
   a.cut = fm_decode_cut(H, cache->heads, T, cache->d, cache->sequences, side_by_side && row < 256 ? 2 : 1, fm_compute_units());
-  const bool split = (long long)cache->columns * cache->page > whole_keys(cache->sequences, a.cut);
+  const bool split = (long long)cache->columns * cache->page >
+                     fm_whole_keys(fm_decode_round_groups(cache->d, cache->type == FM_TYPE_E4M3, a.cut), (long long)cache->sequences * a.cut.workgroups,
+                                   a.cut.least, fm_compute_units());
   const DecodeSpace space = decode_space(a.cut, cache->sequences, H, T, cache->d);
   const bool listed = split && a.cut.listed;
   a.plan = split ? (int2*)ws : nullptr;
