@@ -49,23 +49,27 @@ template <bool F16>
 constexpr float kShift = F16 ? 14.f : 0.f;
 template <bool F16>
 constexpr float kUnshift = F16 ? 0x1p-14f : 1.f;
-// Two 16-bit values, neither negative (their order is that of their bits): y, but the smallest value above 0 at least where x is not 0.
-__device__ __forceinline__ unsigned at_least(unsigned y, unsigned x) {
-  return __builtin_bit_cast(unsigned, __builtin_elementwise_max(__builtin_bit_cast(u16x2, y),
-                                                                __builtin_elementwise_min(__builtin_bit_cast(u16x2, x), u16x2{1, 1})));
+// Two 16-bit values at least as large as two others, none of them negative: their order is that of their bits.
+__device__ __forceinline__ unsigned at_least(unsigned x, u16x2 least) {
+  return __builtin_bit_cast(unsigned, __builtin_elementwise_max(__builtin_bit_cast(u16x2, x), least));
 }
 template <bool F16>
 __device__ __forceinline__ void split2(float a, float b, unsigned& hi, unsigned& lo) {
+  const unsigned x = __builtin_bit_cast(unsigned, a), y = __builtin_bit_cast(unsigned, b);
+  const unsigned upper = __builtin_amdgcn_perm(y, x, 0x07060302u);   // not 0 from 2^-133 on
+  unsigned ones = 0x00010001u;
+  asm("" : "+s"(ones));   // of a minimum with a known 1 the compiler makes comparisons of the halves one by one
+  const u16x2 least = __builtin_elementwise_min(__builtin_bit_cast(u16x2, upper), __builtin_bit_cast(u16x2, ones));
   if constexpr (F16) {
-    constexpr float kLeast = 0x1p-24f, kAbove = 0x1p102f;   // a * kAbove is at least kLeast, or 0: the middle of the three is what is wanted
     const auto h = __builtin_amdgcn_cvt_pkrtz(a, b);
-    lo = pack2<true>(__builtin_amdgcn_fmed3f(a - (float)h[0], kLeast, a * kAbove), __builtin_amdgcn_fmed3f(b - (float)h[1], kLeast, b * kAbove));
-    hi = at_least(__builtin_bit_cast(unsigned, h), lo);
+    hi = at_least(__builtin_bit_cast(unsigned, h), least);
+    unsigned rest = pack2<true>(a - (float)h[0], b - (float)h[1]);
+    asm("" : "+v"(rest));   // one conversion of both: the compiler would take it apart
+    lo = at_least(rest, least);
   } else {
-    const unsigned x = __builtin_bit_cast(unsigned, a), y = __builtin_bit_cast(unsigned, b);
-    hi = __builtin_amdgcn_perm(y, x, 0x07060302u);
+    hi = upper;
     lo = at_least(pack2<false>(__builtin_bit_cast(float, x) - __builtin_bit_cast(float, x & 0xffff0000u),
-                               __builtin_bit_cast(float, y) - __builtin_bit_cast(float, y & 0xffff0000u)), hi);
+                               __builtin_bit_cast(float, y) - __builtin_bit_cast(float, y & 0xffff0000u)), least);
   }
 }
 // Four e4m3 values to 16 bits each (exact in both types).
@@ -649,6 +653,7 @@ __global__ __launch_bounds__(kPlanThreads) void plan_units_kernel(FmDecodeArgs a
 template <int D, bool F16>
 __global__ __launch_bounds__(256) void join_kernel(FmDecodeArgs a, FmDivisor rows, FmDivisor tokens) {
   constexpr int LANES = D / 4, TEAMS = 256 / LANES, BATCH = 4;
+  asm volatile("" ::"s"(a.split), "s"(a.plan), "s"(a.part), "s"(a.stat), "s"(a.H), "s"(rows.factor));   // read together
   const int G = a.H / a.Hk, R = G * a.T;
   const int b = a.split ? a.split[blockIdx.y] : blockIdx.y, hk = fm_div(blockIdx.x, rows), r = blockIdx.x - hk * R;   // row of the K/V head
   if (b < 0) return;
