@@ -51,11 +51,13 @@ __global__ __launch_bounds__(256) void fork_kernel(FmPools pools, int parts, siz
 
 // --- which pages are in use -----------------------------------------------------------------------------------
 // One workgroup marks the pages that the table names in a bit map, counts the bits in front of each word, and deals every
-// page its number among the used or the unused ones.  Map and counts lie in LDS up to kMapPages pages; a larger map, or a
-// table that a workgroup alone would read for long, goes through global memory and is marked by the whole chip first.
+// page its number among the used or the unused ones.  Map and counts lie in LDS where they fit 32 KiB; a larger map, or one of many words
+// with a table that a workgroup alone reads for longer, lies in global memory and is marked by the whole chip first.  us in LDS / global memory:
+// 2^17 pages, 2^17 / 2^18 / 2^20 entries 46/51, 66/58, 186/84; 2^16 pages 35/37, 54/48, 169/102; 2^14 pages, where the marks of a word
+// wait for each other, 26/40, 45/69, 159/240.
 constexpr int kPlanThreads = 1024;
-constexpr int kMapPages = 1 << 17;   // 32 KiB of map and counts
-constexpr int kMapEntries = 1 << 18;
+constexpr int kMapPages = 1 << 17;                                // LDS up to these,
+constexpr int kMarkedPages = 1 << 16, kMarkedEntries = 1 << 17;   // but from these pages on with more entries than these
 
 struct PlanArgs {
   const int* table;
@@ -177,7 +179,7 @@ static size_t pages_bytes(int num_pages) { return ((size_t)num_pages * 4 + 255) 
 static hipError_t launch_plan(PlanArgs a, char* workspace, hipStream_t stream) {
   const int words = (a.num_pages + 31) / 32;
   size_t lds = (size_t)words * 8;
-  if (a.num_pages > kMapPages || a.entries > kMapEntries) {
+  if (a.num_pages > kMapPages || (a.num_pages >= kMarkedPages && a.entries > kMarkedEntries)) {
     a.map = (unsigned*)workspace;
     a.before = (unsigned*)(workspace + words_bytes(a.num_pages));
     lds = 0;
