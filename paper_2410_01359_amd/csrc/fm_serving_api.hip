@@ -70,13 +70,17 @@ int check_row_type(int type, const flashmask_cache& c) {
   return c.type == FM_TYPE_E4M3 || c.type == type ? FM_OK : FM_ERR_ARG;
 }
 
+// How calls of a shape are cut whose workgroups take one head, and two together; the cache decides which.
+struct DecodeCuts {
+  FmDecodeCut of[2];
+};
 // Shapes that flashmask_decode's indexing and its launches have room for, whatever the cache: of workgroups that take two heads together where
 // there are several; those that take one are up to twice as many.
-int check_decode_shape(int sequences, int H, int Hk, int T, int d) {
+int check_decode_shape(int sequences, int H, int Hk, int T, int d, DecodeCuts& cuts) {
   if (sequences <= 0 || H <= 0 || H > FM_MOST_HEADS || Hk <= 0 || H % Hk || T <= 0 || T > FM_MOST_NEW_TOKENS || bad_head_dim(d)) return FM_ERR_SHAPE;
   if ((long long)H * T > (1 << 24) || sequences > 65535 || (long long)H * T * sequences > (1ll << 30)) return FM_ERR_SHAPE;
-  const FmDecodeCut cut = fm_decode_cut(H, Hk, T, d, sequences, 2, fm_compute_units());
-  if ((fm_most_units(cut.chunks, sequences) + 8ll) * cut.workgroups >= 1 << 24) return FM_ERR_SHAPE;
+  for (int i = 0; i < 2; ++i) cuts.of[i] = fm_decode_cut(H, Hk, T, d, sequences, 1 + i, fm_compute_units());
+  if ((fm_most_units(cuts.of[1].chunks, sequences) + 8ll) * cuts.of[1].workgroups >= 1 << 24) return FM_ERR_SHAPE;
   return FM_OK;
 }
 struct DecodeSpace {
@@ -93,12 +97,10 @@ DecodeSpace decode_space(const FmDecodeCut& cut, int sequences, int H, int T, in
   return s;
 }
 // Of whatever cache.
-size_t decode_bytes(int sequences, int H, int Hk, int T, int d) {
-  size_t most = 0;
-  for (int together = 1; together <= 2; ++together)
-    most = std::max(most, decode_space(fm_decode_cut(H, Hk, T, d, sequences, together, fm_compute_units()), sequences, H, T, d).total);
-  return most;
+size_t decode_bytes(const DecodeCuts& cuts, int sequences, int H, int T, int d) {
+  return std::max(decode_space(cuts.of[0], sequences, H, T, d).total, decode_space(cuts.of[1], sequences, H, T, d).total);
 }
+
 int check_pools(void* const* pools, int num_pools, size_t page_bytes, int num_pages) {
   if (num_pools < 0 || num_pages <= 0) return FM_ERR_SHAPE;
   if (num_pools == 0) return FM_OK;
@@ -155,7 +157,8 @@ int flashmask_cache_append(const flashmask_cache* cache, const void* q, const vo
 }
 
 size_t flashmask_decode_workspace_bytes(int sequences, int H, int H_kv, int T, int d) {
-  return check_decode_shape(sequences, H, H_kv, T, d) == FM_OK ? decode_bytes(sequences, H, H_kv, T, d) : 0;
+  DecodeCuts cuts;
+  return check_decode_shape(sequences, H, H_kv, T, d, cuts) == FM_OK ? decode_bytes(cuts, sequences, H, T, d) : 0;
 }
 
 int flashmask_decode(const flashmask_cache* cache, const void* q, const int32_t* lens, const int32_t* lts,
@@ -167,14 +170,15 @@ int flashmask_decode(const flashmask_cache* cache, const void* q, const int32_t*
   const bool bounds = lts || lte || uts || ute;
   if (bounds && (!lts || !lte || !uts || !ute)) return FM_ERR_NULL;
   if (int rc = check_row_type(type, *cache)) return rc;
-  if (int rc = check_decode_shape(cache->sequences, H, cache->heads, T, cache->d)) return rc;
+  DecodeCuts cuts;
+  if (int rc = check_decode_shape(cache->sequences, H, cache->heads, T, cache->d, cuts)) return rc;
   if (bounds && bound_columns <= 0) return FM_ERR_SHAPE;
   if ((long long)cache->sequences * cache->columns * cache->page > 1ll << 34) return FM_ERR_SHAPE;   // groups of 16 keys are added up in 32 bits
   if (!(scale > 0.f) || !(scale < 3.0e38f) || window < 0) return FM_ERR_ARG;
   for (int t = 0; t < 2; ++t)
     if (int rc = check_strides(strides[t], type, cache->sequences, H, T, cache->d)) return rc;
   if (misaligned(q) || misaligned(out)) return FM_ERR_ALIGN;
-  if (bad_workspace(workspace, workspace_bytes, decode_bytes(cache->sequences, H, cache->heads, T, cache->d))) return FM_ERR_WORKSPACE;
+  if (bad_workspace(workspace, workspace_bytes, decode_bytes(cuts, cache->sequences, H, T, cache->d))) return FM_ERR_WORKSPACE;
   char* ws = (char*)workspace;
   FmDecodeArgs a;
   a.q = q; a.out = out; a.lse = lse; a.sq = to_kernel(strides[0]); a.so = to_kernel(strides[1]);
@@ -192,7 +196,7 @@ int flashmask_decode(const flashmask_cache* cache, const void* q, const int32_t*
   // Pages stored token by token have the rows of all heads side by side: a workgroup takes two of less than 256 bytes together.
   const int row = cache->d * element_bytes(cache->type);
   const bool side_by_side = a.k.head < 256 && a.v.head < 256;
-  a.cut = fm_decode_cut(H, cache->heads, T, cache->d, cache->sequences, side_by_side && row < 256 ? 2 : 1, fm_compute_units());
+  a.cut = cuts.of[side_by_side && row < 256];
   const bool split = (long long)cache->columns * cache->page >
                      fm_whole_keys(fm_decode_round_groups(cache->d, cache->type == FM_TYPE_E4M3, a.cut), (long long)cache->sequences * a.cut.workgroups,
                                    a.cut.least, fm_compute_units());

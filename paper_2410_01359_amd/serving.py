@@ -164,9 +164,10 @@ def flashmask_decode(q, k_cache, v_cache, table, lens, scale: float, *, bounds=N
             and (workspace is None or workspace.get_device() == device and workspace.is_contiguous())):
         _refuse((q, "q", tuple(_ROW_TYPE), (B, None, None, d), 1), (lens, "lens", (torch.int32,), (B,), 2),
                 *(() if workspace is None else ((workspace, "workspace", (workspace.dtype,), tuple(workspace.shape), 2),)))
-    if window < 0:
-        raise FlashMaskError(f"window must not be negative, got {window}")
-    window = min(window, 0x7fffffff)    # no table holds as many keys
+    if not 0 <= window < 1 << 31:
+        if window < 0:
+            raise FlashMaskError(f"window must not be negative, got {window}")
+        window = 0    # no table holds as many keys
     H, T = shape[1], shape[2]
     at, columns = (0, 0, 0, 0), 0
     if bounds is not None:
