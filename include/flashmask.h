@@ -330,8 +330,9 @@ enum { FM_ROPE_HALF = 0, FM_ROPE_INTERLEAVED = 1 };
 /*
  * Rotary positions.  Pair i < rot / 2 of a row at position p is turned by the angle p * freqs[i]:
  *     a' = amp (a cos - b sin),   b' = amp (b cos + a sin),
- * elements from `rot` on are copied.  Scaled frequencies and `amp` are how contexts are stretched.  Angles, sines and
- * cosines are computed in 64 bits, the products in 32, with one rounding to the type at the end.
+ * elements from `rot` on are copied.  Scaled frequencies and `amp` are how contexts are stretched.  Angles are products in 64 bits, sines and
+ * cosines of them within 1.2e-10 (up to angles of 2^45, where the product itself is off by more), what is multiplied by them in 32, with
+ * one rounding to the type at the end.
  *   q, q_out       [B,H,N,d], k, k_out [B,H_kv,N,d], of `type` (BF16, F16, F32); strides[4] describe q, k, q_out, k_out in
  *                  elements (multiples of 16 bytes; see flashmask_strides).  An output may be its own input (same strides).
  *   freqs          double [rot / 2]
