@@ -408,6 +408,84 @@ int flashmask_decode(const flashmask_cache* cache, const void* q, const int32_t*
 size_t flashmask_decode_workspace_bytes(int sequences, int H, int H_kv, int T, int d);
 
 /*
+ * flashmask_decode for a tree of drafted tokens, the last T of every sequence: token t, at place lens[b] - T + t, follows token parents[b][t]
+ * where that is one of 0 .. t - 1, and the sequence ahead of the drafted ones where it is anything else.  With depth[t] its number of
+ * ancestors among the drafted ones, its row is i = lens[b] - T + depth[t], which is the position that its query and key are rotated to, and
+ *     of the keys j < lens[b] - T it sees those with                     j > i - window (window > 0),
+ *     of the drafted tokens those that are its ancestors or itself with  depth[u] > depth[t] - window,
+ * and of both no key with LTS[j] <= i < LTE[j] or UTS[j] <= i < UTE[j] (j the key's place).  A token whose place is below 0 is not there.
+ *   parents     int32 [sequences, T];  all else as for flashmask_decode, its workspace, limits and guarantees among it.  (New tokens are
+ *               written to places that are not their positions by flashmask_rope and flashmask_cache_append without freqs.)
+ */
+int flashmask_decode_tree(const flashmask_cache* cache, const void* q, const int32_t* lens, const int32_t* parents, const int32_t* lts,
+                          const int32_t* lte, const int32_t* uts, const int32_t* ute, int bound_columns, int window, float scale,
+                          void* out, float* lse, int type, int H, int T, const flashmask_strides* strides, void* workspace,
+                          size_t workspace_bytes, void* hip_stream);
+
+/*
+ * Takes over the accepted path of a tree of drafted tokens, the last T (1 to 256) of every sequence: with start = lens[b] - T, the token at place
+ * start + path[b][i] moves to place start + i in every pool, in place, and lens_out[b] = start + the path's length.
+ *   path        int32 [sequences, path_columns], path_columns <= T: ascending numbers of drafted tokens.  It ends in front of the first value that
+ *               is not one of 0 .. T - 1 or not above the one before (-1 by custom).
+ *   lens_out    int32 [sequences], not lens itself;  a sequence of fewer than T tokens stays as it is
+ *   pools       HOST array of num_pools device pointers to pages of `type` (BF16, F16 or E4M3), 16-byte aligned, one layout for all: strides as in
+ *               flashmask_cache, `heads` rows of d elements to a token
+ * A place without a page is not written; from a place without one come zeros.  At most 65535 sequences.
+ */
+int flashmask_cache_accept(void* const* pools, int num_pools, const flashmask_strides* strides, int type, int heads, int d, int num_pages,
+                           int page, const int32_t* table, const int32_t* lens, const int32_t* path, int32_t* lens_out, int sequences,
+                           int columns, int T, int path_columns, void* hip_stream);
+
+/*
+ * The attention weight that each key of a prompt gets, from the forward's lse:
+ *     weights[b][hk][j] = sum over the query heads h of K/V head hk, and the rows i >= first_row that see j, of exp(scale * q_i k_j - lse[b][h][i])
+ * What a row does not see has no influence on it; a row with lse = -inf gives nothing.
+ *   q           bf16 [B,H,N,d], k bf16 [B,H_kv,N,d]; strides[2] describe q and k (flashmask_strides); lts..ute int32 [B,N]
+ *   weights     float [B,H_kv,N]
+ *   first_row   0 .. N - 1: rows before it do not count
+ *   workspace   at least flashmask_weights_workspace_bytes(), 256-byte aligned
+ * N at most 2^30, 16384 query heads, and B * H_kv * N below about 2^31.  The same call gives the same bits every time.
+ */
+int flashmask_weights(const void* q, const void* k, const float* lse, const int32_t* lts, const int32_t* lte, const int32_t* uts,
+                      const int32_t* ute, float scale, float* weights, int B, int H, int H_kv, int N, int d, int first_row,
+                      const flashmask_strides* strides, void* workspace, size_t workspace_bytes, void* hip_stream);
+/* Bytes of scratch of that call, 0 for an invalid shape.  Host-only. */
+size_t flashmask_weights_workspace_bytes(int B, int H, int H_kv, int N, int d, int first_row);
+
+/*
+ * The same of the last T (1 to 256) tokens of every sequence over a cache, added to what its keys have: with q, lens, bounds and window as for
+ * flashmask_decode and lse from it,
+ *     weights[b][hk][j] = (j < lens[b] - T ? decay * before[b][hk][j] : 0) + sum of exp(scale * q_i k_j - lse_i)      for places j < lens[b]
+ * that the table and weight_columns have; others stay as they are.  A key without a page gets nothing from the new tokens.
+ *   before      float [sequences, heads, weight_columns], may be weights itself; NULL, or decay = 0: nothing, and not read
+ *   weights     float [sequences, heads, weight_columns];  decay at least 0 and finite;  strides[1] describes q
+ * Limits as for flashmask_decode, and sequences * heads * (places / 1024, rounded up) below about 2^24.
+ */
+int flashmask_cache_weights(const flashmask_cache* cache, const void* q, const int32_t* lens, const int32_t* lts, const int32_t* lte,
+                            const int32_t* uts, const int32_t* ute, int bound_columns, int window, float scale, const float* lse,
+                            const float* before, float decay, float* weights, int weight_columns, int type, int H, int T,
+                            const flashmask_strides* strides, void* hip_stream);
+
+/*
+ * Evicts: a sequence of more than `keep` tokens (that the table has places for) keeps its `first` first ones, its `recent` last ones, and of those between the
+ * keep - first - recent heaviest, in their order, in places 0 .. keep - 1 of the pages new_table[b]; its old pages stay as they are.  A shorter
+ * one stays as it is.
+ *   weights     float [sequences, weight_heads, weight_columns]: with weight_heads = heads every K/V head keeps tokens of its own, with 1 all
+ *               keep the same.  Of equal weights the first token's counts as heavier (0 and -0 are equal), NaN is lighter than any other; places
+ *               from weight_columns on have 0.
+ *   new_table   int32 [sequences, new_columns], new_columns * page and columns * page at least keep: pages for those that are evicted from,
+ *               none of them in use or named twice.  What falls to "no page" is not written.
+ *   table_out   int32 [sequences, columns], lens_out int32 [sequences]: the new pages and -1 behind them, and keep; or the old row and length
+ *   weights_out as weights: those of the tokens in their new places, 0 behind them
+ *  * A kept token whose old place has no page becomes zeros.  Outputs overlap nothing else.  At most 65535 sequences.
+ */
+int flashmask_cache_evict(const flashmask_cache* cache, const int32_t* lens, const float* weights, int weight_heads, int weight_columns,
+                          int keep, int first, int recent, const int32_t* new_table, int new_columns, int32_t* table_out, int32_t* lens_out,
+                          float* weights_out, int32_t* kept, void* workspace, size_t workspace_bytes, void* hip_stream);
+/* Bytes of scratch of that call, 0 for an invalid shape.  Host-only. */
+size_t flashmask_cache_evict_workspace_bytes(int sequences, int weight_heads, int weight_columns);
+
+/*
  * Forks sequences: child r goes on from sequence parents[r], sharing its full pages.
  *   table_out   int32 [children, columns]: the parent's row.  A child with a page of its own (new_pages[r] >= 0) keeps the full
  *               pages lens / page; of a last page that is partly filled it gets a copy, in new_pages[r], in every pool.  Without one

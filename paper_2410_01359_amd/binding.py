@@ -87,6 +87,20 @@ def load_library() -> ctypes.CDLL:
     lib.flashmask_decode.argtypes = [vp, vp, ip, ip, ip, ip, ip, i, i, f, vp, fp, i, i, i, vp, vp, sz, vp]
     lib.flashmask_decode_workspace_bytes.restype = sz
     lib.flashmask_decode_workspace_bytes.argtypes = [i, i, i, i, i]
+    lib.flashmask_decode_tree.restype = i
+    lib.flashmask_decode_tree.argtypes = [vp, vp, ip, ip, ip, ip, ip, ip, i, i, f, vp, fp, i, i, i, vp, vp, sz, vp]
+    lib.flashmask_weights.restype = i
+    lib.flashmask_weights.argtypes = [vp, vp, fp, ip, ip, ip, ip, f, fp, i, i, i, i, i, i, vp, vp, sz, vp]
+    lib.flashmask_weights_workspace_bytes.restype = sz
+    lib.flashmask_weights_workspace_bytes.argtypes = [i, i, i, i, i, i]
+    lib.flashmask_cache_weights.restype = i
+    lib.flashmask_cache_weights.argtypes = [vp, vp, ip, ip, ip, ip, ip, i, i, f, fp, fp, f, fp, i, i, i, i, vp, vp]
+    lib.flashmask_cache_evict.restype = i
+    lib.flashmask_cache_evict.argtypes = [vp, ip, fp, i, i, i, i, i, ip, i, ip, ip, fp, ip, vp, sz, vp]
+    lib.flashmask_cache_evict_workspace_bytes.restype = sz
+    lib.flashmask_cache_evict_workspace_bytes.argtypes = [i, i, i]
+    lib.flashmask_cache_accept.restype = i
+    lib.flashmask_cache_accept.argtypes = [vp, i, vp, i, i, i, i, i, ip, ip, ip, ip, i, i, i, i, vp]
     lib.flashmask_cache_fork.restype = i
     lib.flashmask_cache_fork.argtypes = [vp, i, sz, i, ip, ip, ip, ip, ip, ip, i, i, i, i, vp]
     lib.flashmask_cache_free_list.restype = i

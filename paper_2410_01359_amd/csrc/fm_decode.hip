@@ -15,119 +15,14 @@
 // heads of 128 elements: 94 us, 5.7 TB/s of the 6.4 that a plain reading loop reaches here, and 5 for the join.
 #include <algorithm>
 
+#include "fm_cache_math.h"
 #include "fm_common.h"
 #include "fm_serving.h"
 
 namespace fm {
 
-typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
-typedef __attribute__((ext_vector_type(2))) _Float16 f16x2;
-typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
-typedef __attribute__((ext_vector_type(2))) unsigned short u16x2;
-
-#define FM_CONSTANT __attribute__((address_space(4)))
-
 constexpr int kGroup = FM_KEY_GROUP;
 constexpr int kWaves = 4;
-
-template <bool F16>
-__device__ __forceinline__ f32x4 mfma_keys(u32x4 a, u32x4 b, f32x4 c) {
-  if constexpr (F16) return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
-  else return mfma16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c);
-}
-// Two floats to 16 bits each.
-template <bool F16>
-__device__ __forceinline__ unsigned pack2(float a, float b) {
-  if constexpr (F16) return __builtin_bit_cast(unsigned, f16x2{(_Float16)a, (_Float16)b});
-  else return __builtin_bit_cast(unsigned, bf16x2{(__bf16)a, (__bf16)b});
-}
-// Probabilities enter their product as sums hi + lo of two 16-bit values: cut off and what that left, 16 bits of the
-// value for bf16, 22 for f16.  Neither is negative, and neither is 0 where the probability is a normal number of 32 bits: an infinite
-// value a row sees comes out as itself and not as 0 * inf.  For that each has the type's smallest value at least where the
-// probability is above 0.  f16 ends at 2^-24: probabilities are taken times 2^kShift there, and below 2^-38 count as 2^-37.
-template <bool F16>
-constexpr float kShift = F16 ? 14.f : 0.f;
-template <bool F16>
-constexpr float kUnshift = F16 ? 0x1p-14f : 1.f;
-// Two 16-bit values at least as large as two others, none of them negative: their order is that of their bits.
-__device__ __forceinline__ unsigned at_least(unsigned x, u16x2 least) {
-  return __builtin_bit_cast(unsigned, __builtin_elementwise_max(__builtin_bit_cast(u16x2, x), least));
-}
-template <bool F16>
-__device__ __forceinline__ void split2(float a, float b, unsigned& hi, unsigned& lo) {
-  const unsigned x = __builtin_bit_cast(unsigned, a), y = __builtin_bit_cast(unsigned, b);
-  const unsigned upper = __builtin_amdgcn_perm(y, x, 0x07060302u);   // not 0 from 2^-133 on
-  unsigned ones = 0x00010001u;
-  asm("" : "+s"(ones));   // of a minimum with a known 1 the compiler makes comparisons of the halves one by one
-  const u16x2 least = __builtin_elementwise_min(__builtin_bit_cast(u16x2, upper), __builtin_bit_cast(u16x2, ones));
-  if constexpr (F16) {
-    const auto h = __builtin_amdgcn_cvt_pkrtz(a, b);
-    hi = at_least(__builtin_bit_cast(unsigned, h), least);
-    unsigned rest = pack2<true>(a - (float)h[0], b - (float)h[1]);
-    asm("" : "+v"(rest));   // one conversion of both: the compiler would take it apart
-    lo = at_least(rest, least);
-  } else {
-    hi = upper;
-    lo = at_least(pack2<false>(__builtin_bit_cast(float, x) - __builtin_bit_cast(float, x & 0xffff0000u),
-                               __builtin_bit_cast(float, y) - __builtin_bit_cast(float, y & 0xffff0000u)), least);
-  }
-}
-// Four e4m3 values to 16 bits each (exact in both types).
-template <bool F16>
-__device__ __forceinline__ u32x2 widen4(unsigned x) {
-  if constexpr (F16)
-    return u32x2{__builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)x, 1.f, false)),
-                 __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)x, 1.f, true))};
-  else
-    return u32x2{__builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)x, 1.f, false)),
-                 __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)x, 1.f, true))};
-}
-// The low or the high halves of two words.
-__device__ __forceinline__ unsigned pair_of(unsigned first, unsigned second, int high) {
-  return __builtin_amdgcn_perm(second, first, high ? 0x07060302u : 0x05040100u);
-}
-template <int CTRL>
-__device__ __forceinline__ unsigned dpp_or(unsigned x) {
-  return x | (unsigned)__builtin_amdgcn_update_dpp((int)x, (int)x, CTRL, 0xf, 0xf, false);
-}
-// Bits set in any of the 16 lanes of a DPP row.
-__device__ __forceinline__ unsigned row16_or(unsigned x) { return dpp_or<0x121>(dpp_or<0x122>(dpp_or<0x124>(dpp_or<0x128>(x)))); }
-// Whether a word of cached values has an infinity or NaN: an exponent (e4m3: all bits but the sign) of ones, to which one more bit
-// carries into the sign's place.
-template <bool F16, bool E4M3>
-__device__ __forceinline__ bool odd_word(unsigned x) {
-  constexpr unsigned kOnes = E4M3 ? 0x7f7f7f7fu : F16 ? 0x7c007c00u : 0x7f807f80u;
-  constexpr unsigned kOne = E4M3 ? 0x01010101u : F16 ? 0x04000400u : 0x00800080u, kCarry = E4M3 ? 0x80808080u : 0x80008000u;
-  return (((x & kOnes) + kOne) & kCarry) != 0;
-}
-// Maximum over the four lanes l, l ^ 16, l ^ 32, l ^ 48.
-__device__ __forceinline__ float quad_max(float x) {
-  auto r = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(int, x), __builtin_bit_cast(int, x), false, false);
-  x = fmaxf(__builtin_bit_cast(float, (int)r[0]), __builtin_bit_cast(float, (int)r[1]));
-  r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(int, x), __builtin_bit_cast(int, x), false, false);
-  return fmaxf(__builtin_bit_cast(float, (int)r[0]), __builtin_bit_cast(float, (int)r[1]));
-}
-// Sums over the lanes up to this one, and the last lane's value (uniform).
-template <int CTRL, int ROWS>
-__device__ __forceinline__ int dpp_add(int x) {
-  return x + __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xf, false);
-}
-__device__ __forceinline__ int wave_scan(int x) {
-  x = dpp_add<0x111, 0xf>(x);   // from 1, 2, 4, 8 lanes back in the row of 16
-  x = dpp_add<0x112, 0xf>(x);
-  x = dpp_add<0x114, 0xf>(x);
-  x = dpp_add<0x118, 0xf>(x);
-  x = dpp_add<0x142, 0xa>(x);   // the last lane of rows 0 and 2 to the next row, then of row 1 to rows 2 and 3
-  return dpp_add<0x143, 0xc>(x);
-}
-__device__ __forceinline__ int wave_last(int x) { return __builtin_amdgcn_readlane(x, 63); }
-// Exponents are taken against this: a row that has seen nothing has no maximum.
-__device__ __forceinline__ float reference(float m) { return m == -INFINITY ? 0.f : m; }
-
-// Whether the bounds (LTS, LTE, UTS, UTE) of a key hide it from row i.
-__device__ __forceinline__ bool hides(const i32x4& bound, int i) {
-  return (bound[0] <= i && i < bound[1]) || (bound[2] <= i && i < bound[3]);
-}
 
 template <int D, bool F16, bool E4M3, int NB>
 struct Decode {
@@ -154,14 +49,44 @@ struct Decode {
   };
 };
 
+// A tree of drafted tokens: token t follows token parents[t] < t, or the sequence itself (any other value).  Its row is as many rows behind the first
+// new one as it has ancestors in the tree, and of the drafted tokens it sees those and itself.
+struct Tree {
+  unsigned ancestors[FM_MOST_NEW_TOKENS][FM_MOST_NEW_TOKENS / 32];   // of a token, itself among them
+  int depth[FM_MOST_NEW_TOKENS];
+  __device__ __forceinline__ bool on_path(int t, int u) const { return ancestors[t][u / 32] >> (u % 32) & 1; }
+};
+template <class Args>
+constexpr bool kTree = std::is_same_v<Args, FmTreeArgs>;
+
+// Every token walks up its line; parents come before their children, so that ends.
+__device__ __forceinline__ void plant(Tree& tree, const int* parents, int T) {
+  const int t = threadIdx.x;
+  if (t < T) {
+    const int p = parents[t];
+    tree.depth[t] = p >= 0 && p < t ? p : -1;
+#pragma unroll
+    for (int w = 0; w < FM_MOST_NEW_TOKENS / 32; ++w) tree.ancestors[t][w] = 0;
+  }
+  barrier_nofence();
+  int depth = -1;
+  if (t < T)
+    for (int u = t; u >= 0; u = tree.depth[u], ++depth) tree.ancestors[t][u / 32] |= 1u << (u % 32);
+  barrier_nofence();
+  if (t < T) tree.depth[t] = depth;
+  barrier_nofence();
+}
+
 // TEAMS > 1: the workgroup's waves are teams that go over the same keys together, for blocks of query rows, which find in the caches what
 // the first of them loads, or for heads whose rows lie side by side.
-template <int D, bool F16, bool E4M3, int NB, int TEAMS>
-__global__ __launch_bounds__(64 * kWaves, 2) void decode_kernel(FmDecodeArgs a, int members, FmDivisor inner, FmDivisor row_blocks,
+// FmTreeArgs: the new tokens are a tree.
+template <int D, bool F16, bool E4M3, int NB, int TEAMS, class Args>
+__global__ __launch_bounds__(64 * kWaves, 2) void decode_kernel(Args a, int members, FmDivisor inner, FmDivisor row_blocks,
                                                               FmDivisor tokens, FmDivisor chunks_meant) {
   constexpr int TW = kWaves / TEAMS;   // waves of a team
   using C = Decode<D, F16, E4M3, NB>;
   __shared__ typename C::Shared sh;
+  __shared__ std::conditional_t<kTree<Args>, Tree, char> tree;
   // Barriers here order LDS alone (barrier_nofence): loads stay in flight across them.
   // The launch arguments that come first, read together: left where they are first needed they are six round trips in a row.
   asm volatile("" ::"s"(a.units), "s"(a.plan), "s"(a.lens), "s"(a.B), "s"(a.T), "s"(a.window), "s"(a.columns), "s"(a.page_tokens), "s"(a.cut.least),
@@ -228,6 +153,22 @@ __global__ __launch_bounds__(64 * kWaves, 2) void decode_kernel(FmDecodeArgs a, 
   const int j_begin = range.lo + chunk * size * kGroup;
   const int j_end = (int)std::min<long long>(range.hi, j_begin + (long long)size * kGroup);
   const int first_row = range.len - a.T;   // row of query 0
+  if constexpr (kTree<Args>) plant(tree, a.parents + (size_t)b * a.T, a.T);
+  // Row of query t, and whether it sees key j, bounds apart
+  const auto row_of = [&](int t) {
+    if constexpr (kTree<Args>) return first_row + tree.depth[t];
+    else return first_row + t;
+  };
+  const auto reaches = [&](int j, int t) {
+    const int i = row_of(t);
+    if constexpr (kTree<Args>) {
+      const int u = j - first_row;
+      if (first_row + t < 0) return false;   // not there
+      return u < 0 ? a.window <= 0 || j > i - a.window : u < a.T && tree.on_path(t, u) && (a.window <= 0 || tree.depth[t] - tree.depth[u] < a.window);
+    } else {
+      return j <= i && (a.window <= 0 || j > i - a.window);
+    }
+  };
 
   // Queries
   const int G = a.H / a.Hk, R = G * a.T;
@@ -241,7 +182,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void decode_kernel(FmDecodeArgs a, 
     for (int s = 0; s < C::KSTEPS; ++s) q[nb][s] = u32x4{0, 0, 0, 0};
     if (r < R) {
       const int hq = fm_div(r, tokens), t = r - hq * a.T;
-      column_token[nb] = t;
+      column_token[nb] = kTree<Args> && first_row + t < 0 ? -1 : t;
       const char* p = (const char*)a.q + 2 * ((long long)b * a.sq.b + (long long)(hk * G + hq) * a.sq.h + (long long)t * a.sq.n);
 #pragma unroll
       for (int s = 0; s < C::KSTEPS; ++s)
@@ -313,16 +254,20 @@ __global__ __launch_bounds__(64 * kWaves, 2) void decode_kernel(FmDecodeArgs a, 
     }
   };
 
-  // Which of the lane's keys (bit 4 i + r: key 4 g + r of group i) row `row_i` sees
-  const auto seen_keys = [&](int start, int panel, unsigned pages_there, int row_i) {
+  // Which of the lane's keys (bit 4 i + r: key 4 g + r of group i) query t sees
+  const auto seen_keys = [&](int start, int panel, unsigned pages_there, int t) {
     unsigned seen = 0;
+    const int row_i = row_of(t);
     const int last = min(j_end - 1, row_i), first = a.window > 0 ? row_i - a.window + 1 : 0;
 #pragma unroll 1
     for (int i = 0; i < C::GROUPS; ++i) {
       const int j = start + i * kGroup + 4 * g;
       unsigned four = 0;
 #pragma unroll
-      for (int r = 0; r < 4; ++r) four |= (j + r <= last && j + r >= first ? 1u : 0u) << r;
+      for (int r = 0; r < 4; ++r) {
+        if constexpr (kTree<Args>) four |= (j + r < j_end && reaches(j + r, t) ? 1u : 0u) << r;
+        else four |= (j + r <= last && j + r >= first ? 1u : 0u) << r;
+      }
       if (a.bounds[0]) {
 #pragma unroll
         for (int r = 0; r < 4; ++r)
@@ -367,8 +312,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void decode_kernel(FmDecodeArgs a, 
           sh.bound[j - panel] = bound;
           int flag = 0;
           for (int t = 0; t < a.T; ++t) {
-            const int i = first_row + t;
-            flag |= j <= i && (a.window <= 0 || j > i - a.window) && !hides(bound, i) ? 1 : 2;
+            flag |= reaches(j, t) && !hides(bound, row_of(t)) ? 1 : 2;
           }
           atomicOr(&sh.flag[(j - panel) / C::KEYS], flag);
         }
@@ -400,7 +344,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void decode_kernel(FmDecodeArgs a, 
         for (int s = team_wave; s < steps; s += TW) {
           const int more = (s + TW - steps) >> 31;   // -1: another step follows
           const int start = panel + entry / 4 * C::KEYS;
-          bool masked = (entry & 2) || start + C::KEYS > j_end || start + C::KEYS - 1 > first_row ||
+          bool masked = (entry & 2) || start + C::KEYS > j_end || start + C::KEYS - 1 > first_row - (kTree<Args> ? 1 : 0) ||
                         (a.window > 0 && start <= range.len - 1 - a.window);
 #pragma unroll
           for (int i = 0; i < C::GROUPS; ++i) masked |= now.page(i) < 0;
@@ -442,7 +386,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void decode_kernel(FmDecodeArgs a, 
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb) {
               const bool real = row_token[nb] >= 0;
-              const unsigned seen = real ? seen_keys(start, panel, pages_there, first_row + row_token[nb]) : 0u;
+              const unsigned seen = real ? seen_keys(start, panel, pages_there, row_token[nb]) : 0u;
               any |= row16_or(seen);
               every &= ~row16_or(real ? ~seen : 0u);
 #pragma unroll
@@ -718,14 +662,14 @@ static int round_groups(const FmDecodeCut& cut) {
   return kWaves / cut.teams * (cut.block_rows == 16 ? Decode<D, false, E4M3, 1>::GROUPS : Decode<D, false, E4M3, 2>::GROUPS);
 }
 
-template <int D, bool F16, bool E4M3>
-static void launch(FmDecodeArgs a, hipStream_t stream) {
+template <int D, bool F16, bool E4M3, class Args>
+static void launch(Args a, hipStream_t stream) {
   constexpr int kMost = 1 << 23;   // workgroups of a launch, which has fewer than 2^32 lanes
   const FmDecodeCut& cut = a.cut;
   const int units = a.plan ? fm_listed_units(cut.chunks, a.B) : (a.B + 7) / 8 * 8, workgroups = units * cut.workgroups;
   const FmDivisor di = fm_divisor(cut.workgroups), dr = fm_divisor(cut.row_blocks), dt = fm_divisor(a.T), dc = fm_divisor(cut.chunks);
 #define FM_DECODE(NB, TEAMS)                                                                                                      \
-  hipLaunchKernelGGL((decode_kernel<D, F16, E4M3, NB, TEAMS>), dim3((unsigned)std::min(workgroups - a.first_workgroup, kMost)), \
+  hipLaunchKernelGGL((decode_kernel<D, F16, E4M3, NB, TEAMS, Args>), dim3((unsigned)std::min(workgroups - a.first_workgroup, kMost)), \
                      dim3(64 * kWaves), 0, stream, a, cut.row_blocks * a.Hk, di, dr, dt, dc)
   if (a.units)
     hipLaunchKernelGGL(plan_units_kernel, dim3(1), dim3(kPlanThreads), 0, stream, a, dc,
@@ -784,7 +728,8 @@ int fm_decode_round_groups(int d, bool e4m3, const FmDecodeCut& cut) {
   return e4m3 ? fm::round_groups<128, true>(cut) : fm::round_groups<128, false>(cut);
 }
 
-hipError_t fm_launch_decode(const FmDecodeArgs& a, bool f16, bool e4m3, hipStream_t stream) {
+template <class Args>
+static hipError_t launch_decode(const Args& a, bool f16, bool e4m3, hipStream_t stream) {
   if (a.d == 64) {
     if (f16) e4m3 ? fm::launch<64, true, true>(a, stream) : fm::launch<64, true, false>(a, stream);
     else e4m3 ? fm::launch<64, false, true>(a, stream) : fm::launch<64, false, false>(a, stream);
@@ -794,3 +739,5 @@ hipError_t fm_launch_decode(const FmDecodeArgs& a, bool f16, bool e4m3, hipStrea
   }
   return hipGetLastError();
 }
+hipError_t fm_launch_decode(const FmDecodeArgs& a, bool f16, bool e4m3, hipStream_t stream) { return launch_decode(a, f16, e4m3, stream); }
+hipError_t fm_launch_decode_tree(const FmTreeArgs& a, bool f16, bool e4m3, hipStream_t stream) { return launch_decode(a, f16, e4m3, stream); }

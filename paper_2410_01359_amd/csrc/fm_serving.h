@@ -81,6 +81,72 @@ struct FmDecodeArgs {
 };
 hipError_t fm_launch_decode(const FmDecodeArgs& a, bool f16, bool e4m3, hipStream_t stream);
 
+// Attention over a cache and a tree of drafted tokens.
+struct FmTreeArgs : FmDecodeArgs {
+  const int* parents;     // [B, T]
+};
+hipError_t fm_launch_decode_tree(const FmTreeArgs& a, bool f16, bool e4m3, hipStream_t stream);
+
+// How a call on a prompt is cut: row tiles of a head, blocks of keys, parts that the tiles of a group's heads are cut into, and tiles of a part.
+struct FmWeightsCut {
+  int row_tiles, key_blocks, parts, part_tiles;
+};
+FmWeightsCut fm_weights_cut(int B, int H, int Hk, int N, int first_row, int cus);
+struct FmWeightsArgs {
+  const void *q, *k;
+  const float* lse;
+  const int* bounds[4];
+  float* part;            // [parts, B, Hk, N]
+  FmStride sq, sk;        // elements
+  float scale;
+  int B, H, Hk, N, d, first_row;
+  int row_tiles, parts, part_tiles;
+  FmDivisor slices, by_part, by_head, by_tile;
+};
+// a.part: scratch where there are several parts.
+hipError_t fm_launch_weights(FmWeightsArgs a, float* weights, const FmWeightsCut& cut, hipStream_t stream);
+
+constexpr int FM_WEIGHTS_CHUNK = 1024;   // keys of a workgroup of the call below
+struct FmCacheWeightsArgs {
+  const void* q;
+  const float* lse;       // [B, H, T]
+  FmStride sq;            // elements
+  FmPages k;
+  const float* k_scale;
+  const int *table, *lens;
+  const int* bounds[4];
+  const float* before;    // [B, Hk, weight_columns], NULL: 0
+  float* weights;
+  float scale, decay;
+  int B, H, Hk, T, d, columns, num_pages, bound_columns, window, weight_columns;
+  int places;             // that have a page and a weight
+  FmDivisor page, tokens, chunks, by_head;   // tokens of a page, T, chunks of a sequence, Hk
+};
+hipError_t fm_launch_cache_weights(const FmCacheWeightsArgs& a, bool f16, bool e4m3, hipStream_t stream);
+
+struct FmEvictArgs {
+  FmPages cache[2];       // k, v
+  const int *table, *lens, *new_table;
+  const float* weights;   // [B, weight_heads, weight_columns]
+  float* weights_out;
+  int *kept, *table_out, *lens_out;   // kept [B, weight_heads, keep]
+  int B, Hk, weight_heads, weight_columns, keep, first, recent, columns, new_columns, num_pages, row_bytes;
+  FmDivisor page;
+};
+hipError_t fm_launch_evict(const FmEvictArgs& a, hipStream_t stream);
+
+// Strides in bytes; pools go by their numbers.
+struct FmAcceptArgs {
+  long long page_bytes, head_bytes;
+  unsigned token_bytes;
+  int heads, row_bytes, num_pages;
+  const int *table, *lens, *path;
+  int* lens_out;
+  int B, columns, T, path_columns;
+  FmDivisor page;
+};
+hipError_t fm_launch_accept(void* const* pools, int num_pools, const FmAcceptArgs& a, hipStream_t stream);
+
 constexpr int FM_POOLS = 64;   // pools of one launch
 struct FmPools {
   char* p[FM_POOLS];

@@ -101,6 +101,66 @@ size_t decode_bytes(const DecodeCuts& cuts, int sequences, int H, int T, int d) 
   return std::max(decode_space(cuts.of[0], sequences, H, T, d).total, decode_space(cuts.of[1], sequences, H, T, d).total);
 }
 
+// Checks of a decoding call and its launch arguments.
+int decode_args(const flashmask_cache* cache, const void* q, const int32_t* lens, const int32_t* lts, const int32_t* lte, const int32_t* uts,
+                const int32_t* ute, int bound_columns, int window, float scale, void* out, float* lse, int type, int H, int T,
+                const flashmask_strides* strides, void* workspace, size_t workspace_bytes, FmDecodeArgs& a) {
+  if (int rc = check_cache(cache)) return rc;
+  if (!q || !lens || !out || !lse || !strides) return FM_ERR_NULL;
+  const bool bounds = lts || lte || uts || ute;
+  if (bounds && (!lts || !lte || !uts || !ute)) return FM_ERR_NULL;
+  if (int rc = check_row_type(type, *cache)) return rc;
+  DecodeCuts cuts;
+  if (int rc = check_decode_shape(cache->sequences, H, cache->heads, T, cache->d, cuts)) return rc;
+  if (bounds && bound_columns <= 0) return FM_ERR_SHAPE;
+  if ((long long)cache->sequences * cache->columns * cache->page > 1ll << 34) return FM_ERR_SHAPE;   // groups of 16 keys are added up in 32 bits
+  if (!(scale > 0.f) || !(scale < 3.0e38f) || window < 0) return FM_ERR_ARG;
+  for (int t = 0; t < 2; ++t)
+    if (int rc = check_strides(strides[t], type, cache->sequences, H, T, cache->d)) return rc;
+  if (misaligned(q) || misaligned(out)) return FM_ERR_ALIGN;
+  if (bad_workspace(workspace, workspace_bytes, decode_bytes(cuts, cache->sequences, H, T, cache->d))) return FM_ERR_WORKSPACE;
+  char* ws = (char*)workspace;
+  a.q = q; a.out = out; a.lse = lse; a.sq = to_kernel(strides[0]); a.so = to_kernel(strides[1]);
+  a.k = pages(cache->k, cache->sk, cache->type);
+  a.v = pages(cache->v, cache->sv, cache->type);
+  a.k_scale = cache->k_scale; a.v_scale = cache->v_scale;
+  a.table = cache->table; a.lens = lens;
+  a.bounds[0] = lts; a.bounds[1] = lte; a.bounds[2] = uts; a.bounds[3] = ute;
+  a.scale = scale;
+  a.B = cache->sequences; a.H = H; a.Hk = cache->heads; a.T = T; a.d = cache->d;
+  a.columns = cache->columns; a.num_pages = cache->num_pages; a.page_tokens = cache->page;
+  a.bound_columns = bounds ? bound_columns : 0;
+  a.window = window < (1 << 30) ? window : 0;   // no table holds more keys
+  a.page = fm_divisor(cache->page);
+  // Pages stored token by token have the rows of all heads side by side: a workgroup takes two of less than 256 bytes together.
+  const int row = cache->d * element_bytes(cache->type);
+  const bool side_by_side = a.k.head < 256 && a.v.head < 256;
+  a.cut = cuts.of[side_by_side && row < 256];
+  const bool split = (long long)cache->columns * cache->page >
+                     fm_whole_keys(fm_decode_round_groups(cache->d, cache->type == FM_TYPE_E4M3, a.cut), (long long)cache->sequences * a.cut.workgroups,
+                                   a.cut.least, fm_compute_units());
+  const DecodeSpace space = decode_space(a.cut, cache->sequences, H, T, cache->d);
+  const bool listed = split && a.cut.listed;
+  a.plan = split ? (int2*)ws : nullptr;
+  a.units = listed ? (int4*)(ws + space.units) : nullptr;
+  a.split = listed ? (int*)(ws + space.split) : nullptr;
+  a.stat = (float2*)(ws + space.stat);
+  a.part = (float*)(ws + space.part);
+  return FM_OK;
+}
+
+// Of a call on a prompt's weights: launches have fewer than 2^32 lanes.
+int check_weights_shape(int B, int H, int Hk, int N, int d, int first_row, FmWeightsCut& cut) {
+  if (B <= 0 || H <= 0 || H > FM_MOST_HEADS || Hk <= 0 || H % Hk || N <= 0 || N > (1 << 30) || bad_head_dim(d) || first_row < 0 || first_row >= N)
+    return FM_ERR_SHAPE;
+  if ((long long)B * Hk > 1 << 22 || (long long)H / Hk * ((N - first_row + 63) / 64) > 1 << 30) return FM_ERR_SHAPE;
+  cut = fm_weights_cut(B, H, Hk, N, first_row, fm_compute_units());
+  return (long long)B * Hk * cut.key_blocks * cut.parts < 1 << 24 ? FM_OK : FM_ERR_SHAPE;
+}
+size_t weights_bytes(const FmWeightsCut& cut, int B, int Hk, int N) {
+  return cut.parts == 1 ? 256 : (size_t)cut.parts * B * Hk * N * sizeof(float);
+}
+
 int check_pools(void* const* pools, int num_pools, size_t page_bytes, int num_pages) {
   if (num_pools < 0 || num_pages <= 0) return FM_ERR_SHAPE;
   if (num_pools == 0) return FM_OK;
@@ -165,49 +225,135 @@ int flashmask_decode(const flashmask_cache* cache, const void* q, const int32_t*
                      const int32_t* lte, const int32_t* uts, const int32_t* ute, int bound_columns, int window, float scale,
                      void* out, float* lse, int type, int H, int T, const flashmask_strides* strides, void* workspace,
                      size_t workspace_bytes, void* hip_stream) {
+  FmDecodeArgs a;
+  if (int rc = decode_args(cache, q, lens, lts, lte, uts, ute, bound_columns, window, scale, out, lse, type, H, T, strides, workspace,
+                           workspace_bytes, a)) return rc;
+  return done(fm_launch_decode(a, type == FM_TYPE_F16, cache->type == FM_TYPE_E4M3, (hipStream_t)hip_stream));
+}
+
+int flashmask_decode_tree(const flashmask_cache* cache, const void* q, const int32_t* lens, const int32_t* parents, const int32_t* lts,
+                          const int32_t* lte, const int32_t* uts, const int32_t* ute, int bound_columns, int window, float scale,
+                          void* out, float* lse, int type, int H, int T, const flashmask_strides* strides, void* workspace,
+                          size_t workspace_bytes, void* hip_stream) {
+  if (!parents) return FM_ERR_NULL;
+  FmTreeArgs a;
+  if (int rc = decode_args(cache, q, lens, lts, lte, uts, ute, bound_columns, window, scale, out, lse, type, H, T, strides, workspace,
+                           workspace_bytes, a)) return rc;
+  a.parents = parents;
+  return done(fm_launch_decode_tree(a, type == FM_TYPE_F16, cache->type == FM_TYPE_E4M3, (hipStream_t)hip_stream));
+}
+
+size_t flashmask_weights_workspace_bytes(int B, int H, int H_kv, int N, int d, int first_row) {
+  FmWeightsCut cut;
+  return check_weights_shape(B, H, H_kv, N, d, first_row, cut) == FM_OK ? weights_bytes(cut, B, H_kv, N) : 0;
+}
+
+int flashmask_weights(const void* q, const void* k, const float* lse, const int32_t* lts, const int32_t* lte, const int32_t* uts,
+                      const int32_t* ute, float scale, float* weights, int B, int H, int H_kv, int N, int d, int first_row,
+                      const flashmask_strides* strides, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  if (!q || !k || !lse || !lts || !lte || !uts || !ute || !weights || !strides) return FM_ERR_NULL;
+  FmWeightsCut cut;
+  if (int rc = check_weights_shape(B, H, H_kv, N, d, first_row, cut)) return rc;
+  if (!(scale > 0.f) || !(scale < 3.0e38f)) return FM_ERR_ARG;
+  for (int t = 0; t < 2; ++t)
+    if (int rc = check_strides(strides[t], FM_TYPE_BF16, B, t ? H_kv : H, N, d)) return rc;
+  if (misaligned(q) || misaligned(k)) return FM_ERR_ALIGN;
+  if (bad_workspace(workspace, workspace_bytes, weights_bytes(cut, B, H_kv, N))) return FM_ERR_WORKSPACE;
+  FmWeightsArgs a;
+  a.q = q; a.k = k; a.lse = lse; a.part = (float*)workspace;
+  a.bounds[0] = lts; a.bounds[1] = lte; a.bounds[2] = uts; a.bounds[3] = ute;
+  a.sq = to_kernel(strides[0]); a.sk = to_kernel(strides[1]);
+  a.scale = scale;
+  a.B = B; a.H = H; a.Hk = H_kv; a.N = N; a.d = d; a.first_row = first_row;
+  return done(fm_launch_weights(a, weights, cut, (hipStream_t)hip_stream));
+}
+
+int flashmask_cache_weights(const flashmask_cache* cache, const void* q, const int32_t* lens, const int32_t* lts, const int32_t* lte,
+                            const int32_t* uts, const int32_t* ute, int bound_columns, int window, float scale, const float* lse,
+                            const float* before, float decay, float* weights, int weight_columns, int type, int H, int T,
+                            const flashmask_strides* strides, void* hip_stream) {
   if (int rc = check_cache(cache)) return rc;
-  if (!q || !lens || !out || !lse || !strides) return FM_ERR_NULL;
+  if (!q || !lens || !lse || !weights || !strides) return FM_ERR_NULL;
   const bool bounds = lts || lte || uts || ute;
   if (bounds && (!lts || !lte || !uts || !ute)) return FM_ERR_NULL;
   if (int rc = check_row_type(type, *cache)) return rc;
-  DecodeCuts cuts;
-  if (int rc = check_decode_shape(cache->sequences, H, cache->heads, T, cache->d, cuts)) return rc;
-  if (bounds && bound_columns <= 0) return FM_ERR_SHAPE;
-  if ((long long)cache->sequences * cache->columns * cache->page > 1ll << 34) return FM_ERR_SHAPE;   // groups of 16 keys are added up in 32 bits
-  if (!(scale > 0.f) || !(scale < 3.0e38f) || window < 0) return FM_ERR_ARG;
-  for (int t = 0; t < 2; ++t)
-    if (int rc = check_strides(strides[t], type, cache->sequences, H, T, cache->d)) return rc;
-  if (misaligned(q) || misaligned(out)) return FM_ERR_ALIGN;
-  if (bad_workspace(workspace, workspace_bytes, decode_bytes(cuts, cache->sequences, H, T, cache->d))) return FM_ERR_WORKSPACE;
-  char* ws = (char*)workspace;
-  FmDecodeArgs a;
-  a.q = q; a.out = out; a.lse = lse; a.sq = to_kernel(strides[0]); a.so = to_kernel(strides[1]);
+  const int B = cache->sequences, Hk = cache->heads;
+  if (H <= 0 || H > FM_MOST_HEADS || H % Hk || T <= 0 || T > FM_MOST_NEW_TOKENS || B > 65535 || (long long)H * T > (1 << 24) ||
+      (long long)H * T * B > (1ll << 30) || weight_columns <= 0 || weight_columns > (1 << 30) || (bounds && bound_columns <= 0))
+    return FM_ERR_SHAPE;
+  if (!(scale > 0.f) || !(scale < 3.0e38f) || window < 0 || !(decay >= 0.f) || !(decay < 3.0e38f)) return FM_ERR_ARG;
+  if (int rc = check_strides(strides[0], type, B, H, T, cache->d)) return rc;
+  if (misaligned(q)) return FM_ERR_ALIGN;
+  FmCacheWeightsArgs a;
+  a.places = (int)std::min<long long>((long long)cache->columns * cache->page, weight_columns);
+  const int chunks = (a.places + FM_WEIGHTS_CHUNK - 1) / FM_WEIGHTS_CHUNK;
+  if (((long long)B * chunks + 8) * Hk >= 1 << 24) return FM_ERR_SHAPE;   // workgroups of a launch, which has fewer than 2^32 lanes
+  a.q = q; a.lse = lse; a.sq = to_kernel(strides[0]);
   a.k = pages(cache->k, cache->sk, cache->type);
-  a.v = pages(cache->v, cache->sv, cache->type);
-  a.k_scale = cache->k_scale; a.v_scale = cache->v_scale;
+  a.k_scale = cache->k_scale;
   a.table = cache->table; a.lens = lens;
   a.bounds[0] = lts; a.bounds[1] = lte; a.bounds[2] = uts; a.bounds[3] = ute;
-  a.scale = scale;
-  a.B = cache->sequences; a.H = H; a.Hk = cache->heads; a.T = T; a.d = cache->d;
-  a.columns = cache->columns; a.num_pages = cache->num_pages; a.page_tokens = cache->page;
+  a.before = decay > 0.f ? before : nullptr;
+  a.weights = weights;
+  a.scale = scale; a.decay = decay;
+  a.B = B; a.H = H; a.Hk = Hk; a.T = T; a.d = cache->d; a.columns = cache->columns; a.num_pages = cache->num_pages;
   a.bound_columns = bounds ? bound_columns : 0;
   a.window = window < (1 << 30) ? window : 0;   // no table holds more keys
+  a.weight_columns = weight_columns;
+  a.page = fm_divisor(cache->page); a.tokens = fm_divisor(T); a.chunks = fm_divisor(chunks); a.by_head = fm_divisor(Hk);
+  return done(fm_launch_cache_weights(a, type == FM_TYPE_F16, cache->type == FM_TYPE_E4M3, (hipStream_t)hip_stream));
+}
+
+size_t flashmask_cache_evict_workspace_bytes(int sequences, int weight_heads, int weight_columns) {
+  if (sequences <= 0 || sequences > 65535 || weight_heads <= 0 || weight_heads > FM_MOST_HEADS || weight_columns <= 0 || weight_columns > (1 << 30)) return 0;
+  return 256;
+}
+
+int flashmask_cache_evict(const flashmask_cache* cache, const int32_t* lens, const float* weights, int weight_heads, int weight_columns,
+                          int keep, int first, int recent, const int32_t* new_table, int new_columns, int32_t* table_out, int32_t* lens_out,
+                          float* weights_out, int32_t* kept, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  if (int rc = check_cache(cache)) return rc;
+  if (!lens || !weights || !new_table || !table_out || !lens_out || !weights_out || !kept) return FM_ERR_NULL;
+  if (weight_columns <= 0 || weight_columns > (1 << 30) || (weight_heads != 1 && weight_heads != cache->heads) || cache->sequences > 65535 ||
+      keep <= 0 || keep > (1 << 30) || first < 0 || recent < 0 || (long long)first + recent > keep || new_columns <= 0)
+    return FM_ERR_SHAPE;
+  const int pages_kept = (keep + cache->page - 1) / cache->page;
+  if (new_columns < pages_kept || cache->columns < pages_kept) return FM_ERR_SHAPE;
+  if (bad_workspace(workspace, workspace_bytes, flashmask_cache_evict_workspace_bytes(cache->sequences, weight_heads, weight_columns))) return FM_ERR_WORKSPACE;
+  FmEvictArgs a;
+  a.cache[0] = pages(cache->k, cache->sk, cache->type);
+  a.cache[1] = pages(cache->v, cache->sv, cache->type);
+  a.table = cache->table; a.lens = lens; a.new_table = new_table; a.weights = weights; a.weights_out = weights_out;
+  a.kept = kept; a.table_out = table_out; a.lens_out = lens_out;
+  a.B = cache->sequences; a.Hk = cache->heads; a.weight_heads = weight_heads; a.weight_columns = weight_columns;
+  a.keep = keep; a.first = first; a.recent = recent; a.columns = cache->columns; a.new_columns = new_columns; a.num_pages = cache->num_pages;
+  a.row_bytes = cache->d * element_bytes(cache->type);
   a.page = fm_divisor(cache->page);
-  // Pages stored token by token have the rows of all heads side by side: a workgroup takes two of less than 256 bytes together.
-  const int row = cache->d * element_bytes(cache->type);
-  const bool side_by_side = a.k.head < 256 && a.v.head < 256;
-  a.cut = cuts.of[side_by_side && row < 256];
-  const bool split = (long long)cache->columns * cache->page >
-                     fm_whole_keys(fm_decode_round_groups(cache->d, cache->type == FM_TYPE_E4M3, a.cut), (long long)cache->sequences * a.cut.workgroups,
-                                   a.cut.least, fm_compute_units());
-  const DecodeSpace space = decode_space(a.cut, cache->sequences, H, T, cache->d);
-  const bool listed = split && a.cut.listed;
-  a.plan = split ? (int2*)ws : nullptr;
-  a.units = listed ? (int4*)(ws + space.units) : nullptr;
-  a.split = listed ? (int*)(ws + space.split) : nullptr;
-  a.stat = (float2*)(ws + space.stat);
-  a.part = (float*)(ws + space.part);
-  return done(fm_launch_decode(a, type == FM_TYPE_F16, cache->type == FM_TYPE_E4M3, (hipStream_t)hip_stream));
+  return done(fm_launch_evict(a, (hipStream_t)hip_stream));
+}
+
+int flashmask_cache_accept(void* const* pools, int num_pools, const flashmask_strides* strides, int type, int heads, int d, int num_pages,
+                           int page, const int32_t* table, const int32_t* lens, const int32_t* path, int32_t* lens_out, int sequences,
+                           int columns, int T, int path_columns, void* hip_stream) {
+  if (!pools || !strides || !table || !lens || !path || !lens_out) return FM_ERR_NULL;
+  if (type != FM_TYPE_BF16 && type != FM_TYPE_F16 && type != FM_TYPE_E4M3) return FM_ERR_ARG;
+  if (num_pools <= 0 || heads <= 0 || heads > FM_MOST_HEADS || bad_head_dim(d) || num_pages <= 0 || page <= 0 || page % 16 || page > (1 << 20) ||
+      sequences <= 0 || sequences > 65535 || columns <= 0 || (long long)columns * page > (1 << 30) || T <= 0 || T > FM_MOST_NEW_TOKENS ||
+      path_columns <= 0 || path_columns > T)
+    return FM_ERR_SHAPE;
+  if (int rc = check_strides(*strides, type, num_pages, heads, page, d)) return rc;
+  for (int i = 0; i < num_pools; ++i) {
+    if (!pools[i]) return FM_ERR_NULL;
+    if (misaligned(pools[i])) return FM_ERR_ALIGN;
+  }
+  const int bytes = element_bytes(type);
+  FmAcceptArgs a;
+  a.page_bytes = strides->batch * bytes; a.head_bytes = strides->head * bytes; a.token_bytes = (unsigned)(strides->row * bytes);
+  a.heads = heads; a.row_bytes = d * bytes; a.num_pages = num_pages;
+  a.table = table; a.lens = lens; a.path = path; a.lens_out = lens_out;
+  a.B = sequences; a.columns = columns; a.T = T; a.path_columns = path_columns;
+  a.page = fm_divisor(page);
+  return done(fm_launch_accept(pools, num_pools, a, (hipStream_t)hip_stream));
 }
 
 int flashmask_cache_fork(void* const* pools, int num_pools, size_t page_bytes, int num_pages, const int32_t* table,

@@ -1,4 +1,4 @@
-"""Rotary positions, the paged key-value cache and attention of new tokens over it (see include/flashmask.h for the contract).
+"""Rotary positions, the paged key-value cache, attention of new tokens over it, and the weight of its keys (see include/flashmask.h for the contract).
 
 Argument marshalling only, as in binding.py: every step runs in the HIP kernels, and nothing falls back.  A cache is a pair of
 tensors indexed [pages, heads, tokens of a page, d] (any strides, d contiguous), a page table int32 [sequences, columns] with -1
@@ -19,7 +19,7 @@ _ROW_TYPE = {torch.bfloat16: 0, torch.float16: 1}
 _CACHE_TYPE = {torch.bfloat16: 0, torch.float16: 1, torch.float8_e4m3fn: 3}
 # flashmask_cache, and records of flashmask_strides one behind the other.  Packed by hand: a ctypes.Structure takes twice the time.
 _CACHE = struct.Struct("@PP6qPPP7i")
-_TWO, _FOUR = struct.Struct("@6q"), struct.Struct("@12q")
+_ONE, _TWO, _FOUR = struct.Struct("@3q"), struct.Struct("@6q"), struct.Struct("@12q")
 
 
 # A call of few tokens takes the host longer than the GPU, so a call's checks are one expression, and what exactly is wrong is only
@@ -188,6 +188,182 @@ def flashmask_decode(q, k_cache, v_cache, table, lens, scale: float, *, bounds=N
                                 _TWO.pack(sq[0], sq[1], sq[2], so[0], so[1], so[2]), workspace.data_ptr(),
                                 workspace.numel() * workspace.element_size(), _stream()), "flashmask_decode")
     return out, lse
+
+
+def _window(window):
+    if not 0 <= window < 1 << 31:
+        if window < 0:
+            raise FlashMaskError(f"window must not be negative, got {window}")
+        window = 0    # no table holds as many keys
+    return window
+
+
+def _bounds(bounds, B: int, device: int):
+    """Addresses of (lts, lte, uts, ute) and their columns."""
+    if bounds is None:
+        return (0, 0, 0, 0), 0
+    if len(bounds) != 4:
+        raise FlashMaskError("bounds must be (lts, lte, uts, ute), int32 [sequences, columns]")
+    columns = bounds[0].shape[-1] if bounds[0].dim() else 0
+    for x in bounds:
+        if not (x.dtype is torch.int32 and x.shape == (B, columns) and columns > 0 and x.is_contiguous() and x.get_device() == device):
+            _refuse(*((y, n, (torch.int32,), (B, columns), 2) for y, n in zip(bounds, ("lts", "lte", "uts", "ute"))))
+    return [x.data_ptr() for x in bounds], columns
+
+
+def flashmask_decode_tree(q, k_cache, v_cache, table, lens, parents, scale: float, *, bounds=None, window: int = 0, k_scale=None, v_scale=None,
+                          workspace: torch.Tensor | None = None):
+    """flashmask_decode where the last T tokens of a sequence are a tree of drafted ones: token t follows token parents[b, t] < t of them
+    (int32 [sequences, T]; -1: the sequence ahead of them) and sees what is ahead of all of them, its ancestors and itself.  Its row, and its
+    position, is lens[b] - T + the number of its ancestors."""
+    dtype, shape, device, sq = q.dtype, q.shape, q.get_device(), q.stride()
+    type_id = _ROW_TYPE.get(dtype)
+    cache, heads, d, B = _cache(k_cache, v_cache, table, k_scale, v_scale, device)
+    if not (type_id is not None and len(shape) == 4 and shape[0] == B and shape[3] == d and sq[3] == 1 and lens.dtype is torch.int32
+            and lens.shape == (B,) and lens.is_contiguous() and parents.dtype is torch.int32 and parents.shape == (B, shape[2])
+            and parents.is_contiguous() and device == lens.get_device() == parents.get_device()
+            and (workspace is None or workspace.get_device() == device and workspace.is_contiguous())):
+        _refuse((q, "q", tuple(_ROW_TYPE), (B, None, None, d), 1), (lens, "lens", (torch.int32,), (B,), 2),
+                (parents, "parents", (torch.int32,), (B, shape[2] if len(shape) == 4 else None), 2),
+                *(() if workspace is None else ((workspace, "workspace", (workspace.dtype,), tuple(workspace.shape), 2),)))
+    window = _window(window)
+    H, T = shape[1], shape[2]
+    at, columns = _bounds(bounds, B, device)
+    out = torch.empty_like(q)
+    so = out.stride()
+    lse = torch.empty(B, H, T, dtype=torch.float32, device=q.device)
+    lib = load_library()
+    if workspace is None:
+        workspace = torch.empty(max(int(lib.flashmask_decode_workspace_bytes(B, H, heads, T, d)), 256), dtype=torch.uint8, device=q.device)
+    _check(lib.flashmask_decode_tree(cache, q.data_ptr(), lens.data_ptr(), parents.data_ptr(), *at, columns, window, scale, out.data_ptr(),
+                                     lse.data_ptr(), type_id, H, T, _TWO.pack(sq[0], sq[1], sq[2], so[0], so[1], so[2]), workspace.data_ptr(),
+                                     workspace.numel() * workspace.element_size(), _stream()), "flashmask_decode_tree")
+    return out, lse
+
+
+def flashmask_cache_accept(pools, table, lens, T: int, path):
+    """Take over the accepted path of every sequence's tree of T drafted tokens, its last ones: token path[b, i] (int32 [sequences, n], ascending,
+    -1 behind the last) moves to the i-th place behind the sequence ahead of them, in every pool (tensors [pages, heads, page, d] of one layout).
+    Returns the new lengths."""
+    if not pools:
+        raise FlashMaskError("no pools")
+    first = pools[0]
+    shape, strides, dtype, device = first.shape, first.stride(), first.dtype, first.get_device()
+    entries, ints = table.shape, torch.int32
+    B = entries[0] if len(entries) == 2 else -1
+    type_id = _CACHE_TYPE.get(dtype)
+    if not (type_id is not None and len(shape) == 4 and strides[3] == 1 and table.dtype is ints and lens.dtype is ints
+            and path.dtype is ints and lens.shape == (B,) and path.dim() == 2 and path.shape[0] == B and table.is_contiguous()
+            and lens.is_contiguous() and path.is_contiguous()
+            and 0 <= device == table.get_device() == lens.get_device() == path.get_device() == torch._C._cuda_getDevice()):
+        _refuse((first, "pools", tuple(_CACHE_TYPE), (None,) * 4, 1), (table, "table", (ints,), (None, None), 2), (lens, "lens", (ints,), (B,), 2),
+                (path, "path", (ints,), (B, None), 2))
+    for p in pools:
+        if not (p.dtype is dtype and p.shape == shape and p.stride() == strides and p.get_device() == device):
+            raise FlashMaskError("the pools must have one shape, layout and type, on one GPU")
+    if not _fits(T):
+        raise FlashMaskError(f"T is out of range: {T}")
+    pages, heads, page, d = shape
+    lens_out = torch.empty_like(lens)
+    _check(load_library().flashmask_cache_accept(struct.pack(f"@{len(pools)}P", *[p.data_ptr() for p in pools]), len(pools), _ONE.pack(*strides[:3]),
+                                                 type_id, heads, d, pages, page, table.data_ptr(), lens.data_ptr(), path.data_ptr(),
+                                                 lens_out.data_ptr(), B, entries[1], T, path.shape[1], _stream()), "flashmask_cache_accept")
+    return lens_out
+
+
+def flashmask_weights_workspace_bytes(B: int, H: int, H_kv: int, N: int, d: int, first_row: int = 0) -> int:
+    return int(load_library().flashmask_weights_workspace_bytes(B, H, H_kv, N, d, first_row)) if _fits(B, H, H_kv, N, d, first_row) else 0
+
+
+def flashmask_weights(q, k, lse, lts, lte, uts, ute, scale: float, *, first_row: int = 0, workspace: torch.Tensor | None = None):
+    """The attention weight that each key of a prompt gets: fp32 [B,H_kv,N], sums of exp(scale q k - lse) over the rows from first_row on that see
+    the key and the query heads of its K/V head.  q [B,H,N,d], k [B,H_kv,N,d] (bf16, any strides, d contiguous) and the bounds as for
+    flashmask_fwd_ex, lse [B,H,N] from it."""
+    shape, device, sq, sk = q.shape, q.get_device(), q.stride(), k.stride()
+    bounds, ints, f32, half = (lts, lte, uts, ute), torch.int32, torch.float32, torch.bfloat16
+    if not (len(shape) == 4 and q.dtype is half and k.dtype is half and sq[3] == 1 and len(sk) == 4 and sk[3] == 1
+            and k.shape == (shape[0], k.shape[1], shape[2], shape[3]) and lse.dtype is f32 and lse.shape == shape[:3] and lse.is_contiguous()
+            and 0 <= device == k.get_device() == lse.get_device() == torch._C._cuda_getDevice()
+            and all(x.dtype is ints and x.shape == (shape[0], shape[2]) and x.is_contiguous() and x.get_device() == device for x in bounds)
+            and (workspace is None or workspace.get_device() == device and workspace.is_contiguous())):
+        like = (*shape, None, None, None, None)
+        _refuse((q, "q", (half,), (None,) * 4, 1), (k, "k", (half,), (like[0], None, like[2], like[3]), 1), (lse, "lse", (f32,), like[:3], 2),
+                *((x, n, (ints,), (like[0], like[2]), 2) for x, n in zip(bounds, ("lts", "lte", "uts", "ute"))),
+                *(() if workspace is None else ((workspace, "workspace", (workspace.dtype,), tuple(workspace.shape), 2),)))
+    B, H, N, d = shape
+    heads = k.shape[1]
+    if not _fits(first_row):
+        raise FlashMaskError(f"first_row is out of range: {first_row}")
+    lib = load_library()
+    weights = torch.empty(B, heads, N, dtype=f32, device=q.device)
+    if workspace is None:
+        workspace = torch.empty(max(int(lib.flashmask_weights_workspace_bytes(B, H, heads, N, d, first_row)), 256), dtype=torch.uint8, device=q.device)
+    _check(lib.flashmask_weights(q.data_ptr(), k.data_ptr(), lse.data_ptr(), *[x.data_ptr() for x in bounds], scale, weights.data_ptr(), B, H, heads,
+                                 N, d, first_row, _TWO.pack(sq[0], sq[1], sq[2], sk[0], sk[1], sk[2]), workspace.data_ptr(),
+                                 workspace.numel() * workspace.element_size(), _stream()), "flashmask_weights")
+    return weights
+
+
+def flashmask_cache_weights(q, k_cache, v_cache, table, lens, lse, scale: float, before=None, *, out=None, decay: float = 1.0, bounds=None,
+                            window: int = 0, k_scale=None, v_scale=None):
+    """Add the attention weight that the last T tokens of every sequence, q [sequences, H, T, d], give the cached keys: with lse, bounds and window of
+    their flashmask_decode, out = decay * before + sums of exp(scale q k - lse) for the places of each sequence (those of its last T tokens:
+    the sums alone); others stay as they are.  before, out: fp32 [sequences, H_kv, places]; without out it is before, and without both a
+    new tensor of zeros for all places of the table.  Returns out."""
+    dtype, shape, device, sq = q.dtype, q.shape, q.get_device(), q.stride()
+    type_id, f32 = _ROW_TYPE.get(dtype), torch.float32
+    cache, heads, d, B = _cache(k_cache, v_cache, table, k_scale, v_scale, device)
+    if out is None:
+        out = before if before is not None else torch.zeros(B, heads, table.shape[1] * k_cache.shape[2], dtype=f32, device=q.device)
+    columns = out.shape[-1] if out.dim() else 0
+    if not (type_id is not None and len(shape) == 4 and shape[0] == B and shape[3] == d and sq[3] == 1 and lens.dtype is torch.int32
+            and lens.shape == (B,) and lens.is_contiguous() and lse.dtype is f32 and lse.shape == shape[:3] and lse.is_contiguous()
+            and out.dtype is f32 and out.shape == (B, heads, columns) and out.is_contiguous()
+            and device == lens.get_device() == lse.get_device() == out.get_device()
+            and (before is None or before.dtype is f32 and before.shape == out.shape and before.is_contiguous() and before.get_device() == device)):
+        _refuse((q, "q", tuple(_ROW_TYPE), (B, None, None, d), 1), (lens, "lens", (torch.int32,), (B,), 2), (lse, "lse", (f32,), tuple(shape[:3]), 2),
+                (out, "out", (f32,), (B, heads, None), 2), (before, "before", (f32,), tuple(out.shape), 2))
+    window = _window(window)
+    at, bound_columns = _bounds(bounds, B, device)
+    _check(load_library().flashmask_cache_weights(cache, q.data_ptr(), lens.data_ptr(), *at, bound_columns, window, scale, lse.data_ptr(),
+                                                  0 if before is None else before.data_ptr(), decay, out.data_ptr(), columns, type_id, shape[1],
+                                                  shape[2], _ONE.pack(sq[0], sq[1], sq[2]), _stream()), "flashmask_cache_weights")
+    return out
+
+
+def flashmask_cache_evict_workspace_bytes(sequences: int, weight_heads: int, weight_columns: int) -> int:
+    return int(load_library().flashmask_cache_evict_workspace_bytes(sequences, weight_heads, weight_columns)) \
+        if _fits(sequences, weight_heads, weight_columns) else 0
+
+
+def flashmask_cache_evict(k_cache, v_cache, table, lens, weights, new_table, keep: int, *, first: int = 0, recent: int = 0, k_scale=None,
+                          v_scale=None, workspace: torch.Tensor | None = None):
+    """Sequences of more than `keep` tokens keep their `first` first, their `recent` last and the heaviest of the tokens between, in their order, in
+    the pages new_table[b] (int32 [sequences, at least keep / page]).  weights fp32 [sequences, H_kv or 1, places]: a selection for each K/V head or
+    one for all; equally heavy tokens: the first ones stay.  Returns table, lens, weights (of the tokens in their new places, 0 behind
+    them) and the places that they come from (int32 [sequences, H_kv or 1, keep], -1 behind the last)."""
+    device, ints, f32 = k_cache.get_device(), torch.int32, torch.float32
+    cache, heads, d, B = _cache(k_cache, v_cache, table, k_scale, v_scale, device)
+    which, columns = weights.shape[1:] if weights.dim() == 3 else (heads, 0)
+    if not (lens.dtype is ints and lens.shape == (B,) and lens.is_contiguous() and weights.dtype is f32 and weights.shape == (B, which, columns)
+            and (which == heads or which == 1) and weights.is_contiguous() and new_table.dtype is ints and new_table.dim() == 2
+            and new_table.shape[0] == B and new_table.is_contiguous() and device == lens.get_device() == weights.get_device() == new_table.get_device()
+            and (workspace is None or workspace.get_device() == device and workspace.is_contiguous())):
+        _refuse((lens, "lens", (ints,), (B,), 2), (weights, "weights", (f32,), (B, which if which in (heads, 1) else heads, None), 2),
+                (new_table, "new_table", (ints,), (B, None), 2),
+                *(() if workspace is None else ((workspace, "workspace", (workspace.dtype,), tuple(workspace.shape), 2),)))
+    if not _fits(keep, first, recent):
+        raise FlashMaskError(f"keep, first or recent is out of range: {keep}, {first}, {recent}")
+    if not 0 < keep <= table.shape[1] * k_cache.shape[2]:
+        raise FlashMaskError(f"keep must be positive and within the table's places, got {keep}")
+    lib = load_library()
+    if workspace is None:
+        workspace = torch.empty(max(int(lib.flashmask_cache_evict_workspace_bytes(B, which, columns)), 256), dtype=torch.uint8, device=weights.device)
+    table_out, lens_out, weights_out, kept = torch.empty_like(table), torch.empty_like(lens), torch.empty_like(weights), _ints(table, B, which, keep)
+    _check(lib.flashmask_cache_evict(cache, lens.data_ptr(), weights.data_ptr(), which, columns, keep, first, recent, new_table.data_ptr(),
+                                     new_table.shape[1], table_out.data_ptr(), lens_out.data_ptr(), weights_out.data_ptr(), kept.data_ptr(),
+                                     workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream()), "flashmask_cache_evict")
+    return table_out, lens_out, weights_out, kept
 
 
 def _ints(like, *shape):
