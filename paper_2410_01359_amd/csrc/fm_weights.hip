@@ -24,8 +24,8 @@ constexpr int kKeys = 256, kTile = 64;
 
 template <int D>
 struct WeightsShared {
-  char q[2][kTile * TileLayout<D>::RS];
-  float lse[2][kTile];
+  alignas(16) char q[2][kTile * TileLayout<D>::RS];
+  alignas(16) float lse[2][kTile];
   int minmax[4][8];
 };
 
@@ -144,35 +144,50 @@ __global__ __launch_bounds__(256, 2) void weights_kernel(FmWeightsArgs a) {
 
     const int cls = classify_tile(now.row, min(now.row + kTile, a.N), mine);
     if (cls == T_FULLY) continue;
-    const bool masked = cls != T_UNMASKED || now.row + kTile > a.N;
-#pragma unroll
-    for (int m = 0; m < 2; ++m) {
-      f32x16 s[2] = {};
+    const auto scores = [&](int m, f32x16 (&s)[2]) {
+      s[0] = s[1] = f32x16{};
 #pragma unroll
       for (int step = 0; step < STEPS; ++step) {
         const bf16x8 rows = *(const bf16x8*)(sh.q[buffer] + L::add_col(row_part, 32 * step) + 32 * m * L::RS);
         s[0] = mfma32(rows, k[0][step], s[0]);
         s[1] = mfma32(rows, k[1][step], s[1]);
       }
+    };
+    // a tile's sums first: partial sums of 32 rows keep the error of long ones down
+    const auto add = [&](int m, const f32x16 (&s)[2]) {
       float tile[2] = {0.f, 0.f};
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
         const f32x4 lse = *(const f32x4*)&sh.lse[buffer][32 * m + 8 * q + 4 * half];
-        const int row = now.row + 32 * m + 8 * q + 4 * half;
 #pragma unroll
         for (int n = 0; n < 2; ++n)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            float x = fmaf(s[n][4 * q + r], scale, lse[r]);
-            if (masked) {
-              const int i = row + r;
-              if (i >= a.N || (bound[n][0] <= i && i < bound[n][1]) || (bound[n][2] <= i && i < bound[n][3])) x = -INFINITY;
-            }
-            tile[n] += fast_exp2(x);
-          }
+          for (int r = 0; r < 4; ++r) tile[n] += fast_exp2(fmaf(s[n][4 * q + r], scale, lse[r]));
       }
       sum[0] += tile[0];
       sum[1] += tile[1];
+    };
+    if (cls == T_UNMASKED && now.row + kTile <= a.N) {
+      f32x16 s[2][2];
+      scores(0, s[0]);
+      scores(1, s[1]);
+      add(0, s[0]);
+      add(1, s[1]);
+    } else {
+#pragma unroll
+      for (int m = 0; m < 2; ++m) {
+        f32x16 s[2];
+        scores(m, s);
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
+            hide4(s[n], 4 * q, [&](int r) {
+              const int i = now.row + 32 * m + 8 * q + 4 * half + r;
+              return (i >= a.N) | ((bound[n][0] <= i) & (i < bound[n][1])) | ((bound[n][2] <= i) & (i < bound[n][3]));
+            });
+        add(m, s);
+      }
     }
   }
 #pragma unroll
