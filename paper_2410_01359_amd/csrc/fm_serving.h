@@ -87,9 +87,9 @@ struct FmTreeArgs : FmDecodeArgs {
 };
 hipError_t fm_launch_decode_tree(const FmTreeArgs& a, bool f16, bool e4m3, hipStream_t stream);
 
-// How a call on a prompt is cut: row tiles of a head, blocks of keys, parts that the tiles of a group's heads are cut into, and tiles of a part.
+// How a call on a prompt is cut: row tiles of a head, blocks of keys, parts that the tiles of a block and a group's heads are cut into.
 struct FmWeightsCut {
-  int row_tiles, key_blocks, parts, part_tiles;
+  int row_tiles, key_blocks, parts;
 };
 FmWeightsCut fm_weights_cut(int B, int H, int Hk, int N, int first_row, int cus);
 struct FmWeightsArgs {
@@ -100,8 +100,8 @@ struct FmWeightsArgs {
   FmStride sq, sk;        // elements
   float scale;
   int B, H, Hk, N, d, first_row;
-  int row_tiles, parts, part_tiles;
-  FmDivisor slices, by_part, by_head, by_tile;
+  int row_tiles, parts;
+  FmDivisor slices, by_part, by_head;
 };
 // a.part: scratch where there are several parts.
 hipError_t fm_launch_weights(FmWeightsArgs a, float* weights, const FmWeightsCut& cut, hipStream_t stream);

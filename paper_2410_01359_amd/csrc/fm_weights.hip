@@ -20,13 +20,14 @@ __device__ __forceinline__ float minus_lse(float lse) { return lse == -INFINITY 
 // a time come through LDS, two buffers, their loads in flight over the tile before.  Row tiles of all query heads of the group, one behind
 // the other, are cut into `parts`; Equation 4 tells for the workgroup's and for the wave's keys which are skipped and which
 // take the element mask.
-constexpr int kKeys = 256, kTile = 64;
+constexpr int kKeys = 256, kTile = 64, kPanel = 2048;   // kPanel: row tiles that are listed together
 
 template <int D>
 struct WeightsShared {
   alignas(16) char q[2][kTile * TileLayout<D>::RS];
-  alignas(16) float lse[2][kTile];
+  alignas(16) float lse[3][kTile];   // one more: a wave may still be at the rows before the last
   int minmax[4][8];
+  int list[kPanel], wave_count[4];   // row tiles that some key of the workgroup's sees: tile | class for wave w << (16 + 2 w)
 };
 
 // Maximum, minimum over the 32 lanes of a wave's half (all halves alike).
@@ -76,119 +77,172 @@ __global__ __launch_bounds__(256, 2) void weights_kernel(FmWeightsArgs a) {
 #pragma unroll
     for (int w = 0; w < 8; ++w) sh.minmax[wave][w] = mine.v[w];
   }
-  __syncthreads();
+  barrier_nofence();
 #pragma unroll
   for (int w = 0; w < 8; ++w) {
     int x = sh.minmax[0][w];
 #pragma unroll
     for (int i = 1; i < 4; ++i) x = w % 2 ? min(x, sh.minmax[i][w]) : max(x, sh.minmax[i][w]);
-    all.v[w] = __builtin_amdgcn_readfirstlane(x);
+    all.v[w] = x;
   }
-
-  // Tiles of this part: head h, tile t of its rows
-  struct Tile {
-    int at, h, row;
-  };
-  const int last = min((part + 1) * a.part_tiles, G * a.row_tiles);
-  const auto live = [&](Tile t) {   // the first live one from t on
-    while (t.at < last && classify_tile(t.row, min(t.row + kTile, a.N), all) == T_FULLY) {
-      ++t.at;
-      t.row += kTile;
-      if (t.row >= a.N) {
-        t.row = a.first_row;
-        ++t.h;
-      }
-    }
-    return t;
-  };
-  const auto behind = [&](Tile t) {
-    ++t.at;
-    t.row += kTile;
-    if (t.row >= a.N) {
-      t.row = a.first_row;
-      ++t.h;
-    }
-    return live(t);
-  };
   u32x4 staged[LOADS];
   float staged_lse = 0.f;
-  const auto load = [&](const Tile& t) {
-    const char* rows = (const char*)a.q + 2 * ((long long)b * a.sq.b + (long long)(hk * G + t.h) * a.sq.h);
+  const auto load = [&](int h, int first) {
+    const char* rows = (const char*)a.q + 2 * ((long long)b * a.sq.b + (long long)(hk * G + h) * a.sq.h);
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
-      const int piece = i * 256 + threadIdx.x, row = min(t.row + piece / PIECES, a.N - 1);
+      const int piece = i * 256 + threadIdx.x, row = min(first + piece / PIECES, a.N - 1);
       staged[i] = ldg16(rows + 2 * ((long long)row * a.sq.n + piece % PIECES * 8));
     }
-    if (threadIdx.x < kTile) staged_lse = a.lse[((size_t)b * a.H + hk * G + t.h) * a.N + min(t.row + (int)threadIdx.x, a.N - 1)];
+    if (threadIdx.x < kTile) staged_lse = a.lse[((size_t)b * a.H + hk * G + h) * a.N + min(first + (int)threadIdx.x, a.N - 1)];
   };
 
   const float scale = a.scale * kLog2e;
   float sum[2] = {0.f, 0.f};
-  Tile t;
-  t.at = part * a.part_tiles;
-  t.h = fm_div(t.at, a.by_tile);
-  t.row = a.first_row + (t.at - t.h * a.row_tiles) * kTile;
-  t = live(t);
-  if (t.at < last) load(t);
-  for (int buffer = 0; t.at < last; buffer ^= 1) {
+  // Products of half m of a tile with the keys, and (OLD) beside them the exponentials of the 32 rows before: two elements (d = 64: four) to a
+  // product, each a multiply-add, an exponential and, a product later each, an addition.
+  // Sums of 32 rows first keep the error of long sums down.
+  const auto scores = [&](auto with_old, int m, const char* rows, f32x16 (&s)[2], const f32x16 (&old)[2], const float* old_lse) {
+    constexpr bool OLD = decltype(with_old)::value;
+    constexpr int RING = 3, EACH = 16 / STEPS;   // elements to a product; element e: row e / 2 of the lane's 16, key e % 2
+    bf16x8 ring[RING];
+    f32x4 lse[4];
+    float x[2][EACH], tile[2] = {0.f, 0.f};
+    const auto fetch = [&](int step) { ring[step % RING] = *(const bf16x8*)(rows + L::add_col(row_part, 32 * step) + 32 * m * L::RS); };
+    fetch(0);
+    fetch(1);
+    if constexpr (OLD) {
 #pragma unroll
-    for (int i = 0; i < LOADS; ++i) {
-      const int piece = i * 256 + threadIdx.x;
-      *(u32x4*)(sh.q[buffer] + L::off(piece / PIECES, piece % PIECES * 16)) = staged[i];
+      for (int q = 0; q < 4; ++q) lse[q] = *(const f32x4*)(old_lse + 8 * q + 4 * half);
     }
-    if (threadIdx.x < kTile) sh.lse[buffer][threadIdx.x] = minus_lse(staged_lse);
-    const Tile now = t;
-    t = behind(t);
-    if (t.at < last) load(t);
-    barrier_nofence();   // the next tile's loads stay in flight
-
-    const int cls = classify_tile(now.row, min(now.row + kTile, a.N), mine);
-    if (cls == T_FULLY) continue;
-    const auto scores = [&](int m, f32x16 (&s)[2]) {
-      s[0] = s[1] = f32x16{};
+    s[0] = s[1] = f32x16{};
 #pragma unroll
-      for (int step = 0; step < STEPS; ++step) {
-        const bf16x8 rows = *(const bf16x8*)(sh.q[buffer] + L::add_col(row_part, 32 * step) + 32 * m * L::RS);
-        s[0] = mfma32(rows, k[0][step], s[0]);
-        s[1] = mfma32(rows, k[1][step], s[1]);
+    for (int i = 0; i < 2 * STEPS + 2; ++i) {
+      if (i < 2 * STEPS) {
+        if (i % 2 == 0 && i / 2 + 2 < STEPS) fetch(i / 2 + 2);
+        s[i % 2] = mfma32(ring[i / 2 % RING], k[i % 2][i / 2], s[i % 2]);
       }
-    };
-    // a tile's sums first: partial sums of 32 rows keep the error of long ones down
-    const auto add = [&](int m, const f32x16 (&s)[2]) {
-      float tile[2] = {0.f, 0.f};
+      if constexpr (OLD) {
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const f32x4 lse = *(const f32x4*)&sh.lse[buffer][32 * m + 8 * q + 4 * half];
-#pragma unroll
-        for (int n = 0; n < 2; ++n)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) tile[n] += fast_exp2(fmaf(s[n][4 * q + r], scale, lse[r]));
+        for (int e = 0; e < EACH; ++e) {
+          if (i > 1) tile[e % 2] += x[i % 2][e];
+          if (i < 2 * STEPS) {
+            const int at = i * EACH + e, row = at / 2;
+            x[i % 2][e] = fmaf(old[at % 2][row], scale, lse[row / 4][row % 4]);
+          }
+          if (i > 0 && i < 2 * STEPS + 1) x[(i - 1) % 2][e] = fast_exp2(x[(i - 1) % 2][e]);
+        }
       }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    if constexpr (OLD) {
       sum[0] += tile[0];
       sum[1] += tile[1];
-    };
-    if (cls == T_UNMASKED && now.row + kTile <= a.N) {
-      f32x16 s[2][2];
-      scores(0, s[0]);
-      scores(1, s[1]);
-      add(0, s[0]);
-      add(1, s[1]);
-    } else {
+    }
+  };
+  constexpr std::true_type with_old;
+  constexpr std::false_type alone;
+  // The same exponentials by themselves; hides(n, r): rows r that do not see key n.
+  const auto add = [&](const f32x16 (&s)[2], const float* lses, const auto& hides) {
+    float tile[2] = {0.f, 0.f};
 #pragma unroll
-      for (int m = 0; m < 2; ++m) {
-        f32x16 s[2];
-        scores(m, s);
+    for (int q = 0; q < 4; ++q) {
+      const f32x4 lse = *(const f32x4*)(lses + 8 * q + 4 * half);
 #pragma unroll
-        for (int n = 0; n < 2; ++n)
+      for (int n = 0; n < 2; ++n) {
+        f32x4 x;
 #pragma unroll
-          for (int q = 0; q < 4; ++q)
-            hide4(s[n], 4 * q, [&](int r) {
-              const int i = now.row + 32 * m + 8 * q + 4 * half + r;
-              return (i >= a.N) | ((bound[n][0] <= i) & (i < bound[n][1])) | ((bound[n][2] <= i) & (i < bound[n][3]));
-            });
-        add(m, s);
+        for (int r = 0; r < 4; ++r) x[r] = fmaf(s[n][4 * q + r], scale, lse[r]);
+        hides(x, n, 8 * q + 4 * half);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) tile[n] += fast_exp2(x[r]);
       }
     }
+    sum[0] += tile[0];
+    sum[1] += tile[1];
+  };
+  const auto none = [](f32x4&, int, int) {};
+
+  f32x16 upper[2], lower[2];   // scores of a tile's halves; those of `lower` wait for the next products
+  const float* waiting = nullptr;   // their rows' lse
+  int buffer = 0, turn = 0;
+  for (int panel = 0; panel < a.row_tiles; panel += kPanel) {
+    const int panel_row = a.first_row + panel * kTile, tiles = min(kPanel, a.row_tiles - panel);
+    int listed = 0;
+    barrier_nofence();   // the list before has been read
+    for (int base = 0; base < tiles; base += 256) {
+      const int tile = base + threadIdx.x, r0 = panel_row + tile * kTile, r1 = min(r0 + kTile, a.N);
+      int entry = tile;
+      bool live = false;
+      if (tile < tiles && classify_tile(r0, r1, all) != T_FULLY) {
+        live = true;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          MinMax8 x;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) x.v[i] = sh.minmax[w][i];
+          entry |= (classify_tile(r0, r1, x) & 3) << (16 + 2 * w);
+        }
+      }
+      append_live(live, entry, sh.list, sh.wave_count, listed);
+    }
+    // this part's share of the heads' tiles
+    const long long items = (long long)G * listed;
+    int left = (int)(items * (part + 1) / a.parts - items * part / a.parts);
+    if (left == 0) continue;
+    const long long first = items * part / a.parts;
+    int h = (int)(first / listed), at = (int)(first - (long long)h * listed);
+    int entry = __builtin_amdgcn_readfirstlane(sh.list[at]);
+    load(h, panel_row + (entry & 0xffff) * kTile);
+    for (; left > 0; --left) {
+      const char* rows = sh.q[buffer];
+      float* lses = sh.lse[turn];
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i) {
+        const int piece = i * 256 + threadIdx.x;
+        *(u32x4*)(sh.q[buffer] + L::off(piece / PIECES, piece % PIECES * 16)) = staged[i];
+      }
+      if (threadIdx.x < kTile) lses[threadIdx.x] = minus_lse(staged_lse);
+      const int row = panel_row + (entry & 0xffff) * kTile, cls = entry >> (16 + 2 * wave) & 3;
+      if (left > 1) {
+        if (++at == listed) {
+          at = 0;
+          ++h;
+        }
+        entry = __builtin_amdgcn_readfirstlane(sh.list[at]);
+        load(h, panel_row + (entry & 0xffff) * kTile);
+      }
+      buffer ^= 1;
+      turn = turn == 2 ? 0 : turn + 1;
+      barrier_nofence();   // the next tile's loads stay in flight
+
+      if (cls == T_FULLY) {   // what waits does not wait longer than a tile
+        if (waiting) add(lower, waiting, none);
+        waiting = nullptr;
+        continue;
+      }
+      if (waiting) scores(with_old, 0, rows, upper, lower, waiting);
+      else scores(alone, 0, rows, upper, upper, lses);
+      if (cls == T_UNMASKED && row + kTile <= a.N) {
+        scores(with_old, 1, rows, lower, upper, lses);
+        waiting = lses + 32;
+        continue;
+      }
+      const auto masked = [&](int m) {
+        return [&, m](f32x4& x, int n, int r0) {
+          hide4(x, 0, [&](int r) {
+            const int i = row + 32 * m + r0 + r;
+            return (i >= a.N) | ((bound[n][0] <= i) & (i < bound[n][1])) | ((bound[n][2] <= i) & (i < bound[n][3]));
+          });
+        };
+      };
+      add(upper, lses, masked(0));
+      scores(alone, 1, rows, lower, lower, lses);
+      add(lower, lses + 32, masked(1));
+      waiting = nullptr;
+    }
+    if (waiting) add(lower, waiting, none);
+    waiting = nullptr;
   }
 #pragma unroll
   for (int n = 0; n < 2; ++n) sum[n] += partner32(sum[n]);
@@ -386,25 +440,20 @@ static void launch(const FmCacheWeightsArgs& a, unsigned workgroups, hipStream_t
 
 FmWeightsCut fm_weights_cut(int B, int H, int Hk, int N, int first_row, int cus) {
   FmWeightsCut cut;
-  const int tiles = (N - first_row + fm::kTile - 1) / fm::kTile, all = H / Hk * tiles;
-  cut.row_tiles = tiles;
+  cut.row_tiles = (N - first_row + fm::kTile - 1) / fm::kTile;
   cut.key_blocks = (N + fm::kKeys - 1) / fm::kKeys;
   // eight rounds of the places that the chip has, parts of 16 tiles at least
-  const long long units = (long long)B * Hk * cut.key_blocks, wanted = 16ll * (cus > 0 ? cus : 256);
-  long long parts = std::max<long long>(1, std::min<long long>((wanted + units - 1) / units, all / 16));
-  cut.part_tiles = (int)((all + parts - 1) / parts);
-  cut.parts = (all + cut.part_tiles - 1) / cut.part_tiles;
+  const long long units = (long long)B * Hk * cut.key_blocks, wanted = 16ll * (cus > 0 ? cus : 256), all = (long long)H / Hk * cut.row_tiles;
+  cut.parts = (int)std::max<long long>(1, std::min<long long>((wanted + units - 1) / units, all / 16));
   return cut;
 }
 
 hipError_t fm_launch_weights(FmWeightsArgs a, float* weights, const FmWeightsCut& cut, hipStream_t stream) {
   a.row_tiles = cut.row_tiles;
   a.parts = cut.parts;
-  a.part_tiles = cut.part_tiles;
   a.slices = fm_divisor(a.B * a.Hk);
   a.by_part = fm_divisor(cut.parts);
   a.by_head = fm_divisor(a.Hk);
-  a.by_tile = fm_divisor(cut.row_tiles);
   float* parts = a.part;
   if (cut.parts == 1) a.part = weights;
   const unsigned workgroups = (unsigned)a.B * a.Hk * cut.key_blocks * cut.parts;
