@@ -442,9 +442,10 @@ FmWeightsCut fm_weights_cut(int B, int H, int Hk, int N, int first_row, int cus)
   FmWeightsCut cut;
   cut.row_tiles = (N - first_row + fm::kTile - 1) / fm::kTile;
   cut.key_blocks = (N + fm::kKeys - 1) / fm::kKeys;
-  // eight rounds of the places that the chip has, parts of 16 tiles at least
-  const long long units = (long long)B * Hk * cut.key_blocks, wanted = 16ll * (cus > 0 ? cus : 256), all = (long long)H / Hk * cut.row_tiles;
-  cut.parts = (int)std::max<long long>(1, std::min<long long>((wanted + units - 1) / units, all / 16));
+  // Eight rounds of the places that the chip has, with parts of 16 tiles at least; where that leaves places empty, parts of 2 tiles.
+  const long long units = (long long)B * Hk * cut.key_blocks, places = 2ll * (cus > 0 ? cus : 256), all = (long long)H / Hk * cut.row_tiles;
+  const long long rounds = std::min((8 * places + units - 1) / units, all / 16), once = std::min((places + units - 1) / units, (all + 1) / 2);
+  cut.parts = (int)std::max({rounds, once, 1ll});
   return cut;
 }
 
