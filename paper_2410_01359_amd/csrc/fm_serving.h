@@ -124,15 +124,19 @@ struct FmCacheWeightsArgs {
 };
 hipError_t fm_launch_cache_weights(const FmCacheWeightsArgs& a, bool f16, bool e4m3, hipStream_t stream);
 
+constexpr int FM_EVICT_PARTS = 16;   // workgroups that a long row is split over
 struct FmEvictArgs {
   FmPages cache[2];       // k, v
   const int *table, *lens, *new_table;
   const float* weights;   // [B, weight_heads, weight_columns]
   float* weights_out;
   int *kept, *table_out, *lens_out;   // kept [B, weight_heads, keep]
+  unsigned* scratch;
   int B, Hk, weight_heads, weight_columns, keep, first, recent, columns, new_columns, num_pages, row_bytes;
   FmDivisor page;
 };
+// Scratch, 0 where no row is split.
+size_t fm_evict_bytes(int sequences, int weight_heads, int weight_columns);
 hipError_t fm_launch_evict(const FmEvictArgs& a, hipStream_t stream);
 
 // Strides in bytes; pools go by their numbers.

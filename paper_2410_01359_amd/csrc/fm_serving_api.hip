@@ -306,7 +306,7 @@ int flashmask_cache_weights(const flashmask_cache* cache, const void* q, const i
 
 size_t flashmask_cache_evict_workspace_bytes(int sequences, int weight_heads, int weight_columns) {
   if (sequences <= 0 || sequences > 65535 || weight_heads <= 0 || weight_heads > FM_MOST_HEADS || weight_columns <= 0 || weight_columns > (1 << 30)) return 0;
-  return 256;
+  return std::max<size_t>(fm_evict_bytes(sequences, weight_heads, weight_columns), 256);
 }
 
 int flashmask_cache_evict(const flashmask_cache* cache, const int32_t* lens, const float* weights, int weight_heads, int weight_columns,
@@ -324,7 +324,7 @@ int flashmask_cache_evict(const flashmask_cache* cache, const int32_t* lens, con
   a.cache[0] = pages(cache->k, cache->sk, cache->type);
   a.cache[1] = pages(cache->v, cache->sv, cache->type);
   a.table = cache->table; a.lens = lens; a.new_table = new_table; a.weights = weights; a.weights_out = weights_out;
-  a.kept = kept; a.table_out = table_out; a.lens_out = lens_out;
+  a.kept = kept; a.table_out = table_out; a.lens_out = lens_out; a.scratch = (unsigned*)workspace;
   a.B = cache->sequences; a.Hk = cache->heads; a.weight_heads = weight_heads; a.weight_columns = weight_columns;
   a.keep = keep; a.first = first; a.recent = recent; a.columns = cache->columns; a.new_columns = new_columns; a.num_pages = cache->num_pages;
   a.row_bytes = cache->d * element_bytes(cache->type);

@@ -82,6 +82,32 @@ def test_equal_and_odd_weights(case, kind):
     _check(p, _weights(kind, B, heads, p["table"].shape[1] * page, case), _new_table(p, keep), keep, first, recent)
 
 
+@pytest.mark.parametrize("kind", ["plain", "few", "odd", "same"])
+@pytest.mark.parametrize("lens,heads,keep,first,recent", [([40000, 100, 17001], 2, 9000, 4, 500), ([16500, 16640], 1, 16400, 0, 0), ([30000], 1, 700, 300, 400),
+                                                          ([140000], 1, 20000, 1, 1), ([20000, 5], 1, 1, 0, 0)])
+def test_long_rows(lens, heads, keep, first, recent, kind):
+    """Rows that several workgroups share."""
+    B = len(lens)
+    p = paged(40, lens, heads, 256, 64, "e4m3", spare=B * -(-keep // 256))
+    p["k_scale"], p["v_scale"] = (torch.ones(heads, device="cuda") for _ in range(2))
+    _check(p, _weights(kind, B, heads, p["table"].shape[1] * 256, len(lens)), _new_table(p, keep), keep, first, recent)
+
+
+def test_a_long_row_with_fewer_weights_than_places():
+    p = paged(41, [40000], 1, 256, 64, "e4m3", spare=80)
+    weights = _weights("plain", 1, 1, 17000, 6)
+    weights[0, 0, ::3] *= -1
+    _check(p, weights, _new_table(p, 20000), 20000, 0, 10)
+
+
+@pytest.mark.parametrize("heads,B", [(129, 1), (1, 130)])
+def test_many_long_rows(heads, B):
+    """More than are shared."""
+    lens = [16500] + [20] * (B - 1)
+    p = paged(42, lens, heads, 4096, 64, "e4m3", spare=2 * B)
+    _check(p, _weights("plain", B, heads, 20480, 7), _new_table(p, 5000), 5000, 3, 30)
+
+
 @pytest.mark.parametrize("columns", [1, 30, 64, 90, 500])
 def test_more_or_fewer_weights_than_places(columns):
     """Places without a weight have 0, and a negative weight is lighter."""
@@ -114,11 +140,13 @@ def test_twice():
     _check(again, got[2].cpu().numpy(), pages[12:].reshape(2, 3), 48, 4, 20)
 
 
-def test_on_a_stream_of_its_own_and_in_a_graph():
+@pytest.mark.parametrize("long", [3000, 17000])
+def test_on_a_stream_of_its_own_and_in_a_graph(long):
     import paper_2410_01359_amd as fm
-    p = paged(34, [3000, 500, 20], 2, 32, 64, "bf16", spare=3 * 8)
-    weights, fresh = torch.tensor(_weights("plain", 3, 2, 3008, 5), device="cuda"), ints(_new_table(p, 256))
-    ws = torch.empty(fm.flashmask_cache_evict_workspace_bytes(3, 2, 3008), dtype=torch.uint8, device="cuda")
+    p = paged(34, [long, 500, 20], 2, 32, 64, "bf16", spare=3 * 8)
+    places = p["table"].shape[1] * 32
+    weights, fresh = torch.tensor(_weights("plain", 3, 2, places, 5), device="cuda"), ints(_new_table(p, 256))
+    ws = torch.empty(fm.flashmask_cache_evict_workspace_bytes(3, 2, places), dtype=torch.uint8, device="cuda")
 
     def call():
         return fm.flashmask_cache_evict(p["k_cache"], p["v_cache"], p["table"], p["lens"], weights, fresh, 256, first=4, recent=64, workspace=ws)
