@@ -459,7 +459,7 @@ size_t flashmask_weights_workspace_bytes(int B, int H, int H_kv, int N, int d, i
  * that the table and weight_columns have; others stay as they are.  A key without a page gets nothing from the new tokens.
  *   before      float [sequences, heads, weight_columns], may be weights itself; NULL, or decay = 0: nothing, and not read
  *   weights     float [sequences, heads, weight_columns];  decay at least 0 and finite;  strides[1] describes q
- * Limits as for flashmask_decode, and sequences * heads * (places / 1024, rounded up) below about 2^24.
+ * Limits as for flashmask_decode; with more than 512 sequences also sequences * heads * (places / 8192, rounded up) below about 2^24.
  */
 int flashmask_cache_weights(const flashmask_cache* cache, const void* q, const int32_t* lens, const int32_t* lts, const int32_t* lte,
                             const int32_t* uts, const int32_t* ute, int bound_columns, int window, float scale, const float* lse,

@@ -106,7 +106,6 @@ struct FmWeightsArgs {
 // a.part: scratch where there are several parts.
 hipError_t fm_launch_weights(FmWeightsArgs a, float* weights, const FmWeightsCut& cut, hipStream_t stream);
 
-constexpr int FM_WEIGHTS_CHUNK = 1024;   // keys of a workgroup of the call below
 struct FmCacheWeightsArgs {
   const void* q;
   const float* lse;       // [B, H, T]
@@ -120,8 +119,13 @@ struct FmCacheWeightsArgs {
   float scale, decay;
   int B, H, Hk, T, d, columns, num_pages, bound_columns, window, weight_columns;
   int places;             // that have a page and a weight
-  FmDivisor page, tokens, chunks, by_head;   // tokens of a page, T, chunks of a sequence, Hk
+  FmDivisor page, tokens, by_head;   // tokens of a page, T, Hk
+  bool dealt;             // all sequences' keys into `chunks` pieces, by their lengths; else each sequence's places into `chunks` of chunk_keys
+  FmDivisor chunks;
+  int chunk_keys;
 };
+// Cuts a call's work for `cus` compute units; false: too many workgroups.
+bool fm_cut_cache_weights(FmCacheWeightsArgs& a, int cus);
 hipError_t fm_launch_cache_weights(const FmCacheWeightsArgs& a, bool f16, bool e4m3, hipStream_t stream);
 
 constexpr int FM_EVICT_PARTS = 16;   // workgroups that a long row is split over

@@ -286,8 +286,7 @@ int flashmask_cache_weights(const flashmask_cache* cache, const void* q, const i
   if (misaligned(q)) return FM_ERR_ALIGN;
   FmCacheWeightsArgs a;
   a.places = (int)std::min<long long>((long long)cache->columns * cache->page, weight_columns);
-  const int chunks = (a.places + FM_WEIGHTS_CHUNK - 1) / FM_WEIGHTS_CHUNK;
-  if (((long long)B * chunks + 8) * Hk >= 1 << 24) return FM_ERR_SHAPE;   // workgroups of a launch, which has fewer than 2^32 lanes
+  if ((long long)B * a.places > 1ll << 34) return FM_ERR_SHAPE;   // groups of 16 keys are added up in 32 bits
   a.q = q; a.lse = lse; a.sq = to_kernel(strides[0]);
   a.k = pages(cache->k, cache->sk, cache->type);
   a.k_scale = cache->k_scale;
@@ -300,7 +299,8 @@ int flashmask_cache_weights(const flashmask_cache* cache, const void* q, const i
   a.bound_columns = bounds ? bound_columns : 0;
   a.window = window < (1 << 30) ? window : 0;   // no table holds more keys
   a.weight_columns = weight_columns;
-  a.page = fm_divisor(cache->page); a.tokens = fm_divisor(T); a.chunks = fm_divisor(chunks); a.by_head = fm_divisor(Hk);
+  a.page = fm_divisor(cache->page); a.tokens = fm_divisor(T); a.by_head = fm_divisor(Hk);
+  if (!fm_cut_cache_weights(a, fm_compute_units())) return FM_ERR_SHAPE;
   return done(fm_launch_cache_weights(a, type == FM_TYPE_F16, cache->type == FM_TYPE_E4M3, (hipStream_t)hip_stream));
 }
 

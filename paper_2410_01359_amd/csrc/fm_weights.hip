@@ -261,10 +261,12 @@ __global__ __launch_bounds__(256) void join_weights_kernel(const float* __restri
 
 // --- a cache ---------------------------------------------------------------------------------------------------
 // Keys in steps of 64 to a wave, four groups of 16 (B operands of 16x16x32 products: a lane has a key of each group); 16 query rows are the A operand,
-// so that a lane's results are four rows of its keys.  A workgroup has a chunk of a sequence's keys of one K/V head.  First every lane works
-// out for its own key how many of the T rows see it: steps that none sees are not read, and only steps of keys that some
-// rows do not see take the element mask.
-constexpr int kStep = 64, kGroups = kStep / FM_KEY_GROUP, kWaves = 4;
+// so that a lane's results are four rows of its keys.  A wave has the next step's keys in flight.  Of up to 16 rows to a K/V head the
+// operand stays in registers and reading the keys is what takes the time; of more, 256 at a time lie in LDS.
+// Chunks of keys are dealt as in attention over the cache: all sequences' keys in as many pieces as the chip has places, each sequence in whole ones.
+// With bounds every lane first works out for its own key how many of the T rows see it: steps that none sees are not read, and only steps with keys that
+// some rows do not see take the element mask.
+constexpr int kStep = 64, kGroups = kStep / FM_KEY_GROUP, kWaves = 4, kSteps = 64, kRows = 256;   // kSteps: of a panel, whose flags lie together
 
 // Rows of [lo, hi) that an interval pair leaves.
 __device__ __forceinline__ int rows_left(int lo, int hi, const i32x4& bound) {
@@ -273,20 +275,64 @@ __device__ __forceinline__ int rows_left(int lo, int hi, const i32x4& bound) {
   return hi - lo - max(b0 - a0, 0) - max(b1 - a1, 0) + max(min(b0, b1) - max(a0, a1), 0);
 }
 
-// ONE: the rows of a K/V head are 16 at most and stay in registers.
+template <int D, bool ONE>
+struct CacheWeightsShared {
+  int flag[kSteps];
+  alignas(16) char q[ONE ? 16 : kRows * TileLayout<D>::RS];
+  alignas(16) float lse[ONE ? 4 : kRows];
+};
+
+// ONE: the rows of a K/V head are 16 at most.
 template <int D, bool F16, bool E4M3, bool ONE>
 __global__ __launch_bounds__(64 * kWaves, 2) void cache_weights_kernel(FmCacheWeightsArgs a) {
+  using L = TileLayout<D>;
   constexpr int BYTES = E4M3 ? 1 : 2, STEPS = D / 32, LOADS = D * BYTES / 64;
-  __shared__ int flags[FM_WEIGHTS_CHUNK / kStep];
+  __shared__ CacheWeightsShared<D, ONE> sh;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int g = lane >> 4, c = lane & 15;
   // all heads of a chunk on one XCD: they share table entries and bounds, and cache lines where heads lie side by side
   const int turn = fm_div(blockIdx.x >> 3, a.by_head), hk = (blockIdx.x >> 3) - turn * a.Hk, unit = turn * 8 + (blockIdx.x & 7);
-  const int b = fm_div(unit, a.chunks), chunk = unit - b * (int)a.chunks.n;
-  if (b >= a.B) return;
-  const int len = max(a.lens[b], 0), end = min(len, a.places), j0 = chunk * FM_WEIGHTS_CHUNK, j1 = min(j0 + FM_WEIGHTS_CHUNK, end);
-  if (j0 >= j1) return;
-  const int first_row = len - a.T, steps = (j1 - j0 + kStep - 1) / kStep;
+  int b, len, begin, end;
+  if (a.dealt) {
+    int lane_len = lane < a.B ? a.lens[lane] : 0;
+    const auto lane_groups = [&](int base) {
+      if (a.B > 64) lane_len = base + lane < a.B ? a.lens[base + lane] : 0;
+      return (min(max(lane_len, 0), a.places) + FM_KEY_GROUP - 1) / FM_KEY_GROUP;
+    };
+    unsigned total = 0;
+    for (int base = 0; base < a.B; base += 64) total += wave_last(wave_scan(lane_groups(base)));
+    const int size = fm_chunk_groups(total, a.chunks, kWaves * kGroups, kWaves * kGroups);
+    int chunk = 0, chunks = 1, groups = 0;
+    for (int units = 0, base = 0;;) {
+      const int mine = lane_groups(base), n = base + lane < a.B ? fm_chunks_of(mine, size) : 0, upto = wave_scan(n);
+      const unsigned long long behind = __ballot(units + upto > unit);
+      if (behind) {
+        const int at = __builtin_ctzll(behind);
+        b = base + at;
+        chunks = __builtin_amdgcn_readlane(n, at);
+        chunk = unit - (units + __builtin_amdgcn_readlane(upto, at) - chunks);
+        groups = __builtin_amdgcn_readlane(mine, at);
+        len = __builtin_amdgcn_readlane(lane_len, at);
+        break;
+      }
+      units += wave_last(upto);
+      base += 64;
+      if (base >= a.B) return;
+    }
+    const int keys = fm_even_chunk(groups, chunks, kGroups) * FM_KEY_GROUP;
+    begin = chunk * keys;
+    end = begin + keys;
+  } else {
+    b = fm_div(unit, a.chunks);
+    if (b >= a.B) return;
+    len = a.lens[b];
+    begin = (unit - b * (int)a.chunks.n) * a.chunk_keys;
+    end = begin + a.chunk_keys;
+  }
+  len = max(len, 0);
+  end = min(end, min(len, a.places));
+  if (begin >= end) return;
+  const int first_row = len - a.T;
   const FM_CONSTANT int* table = (const FM_CONSTANT int*)(a.table + (size_t)b * a.columns);
   const size_t row_of_weights = ((size_t)b * a.Hk + hk) * a.weight_columns;
   const auto old = [&](int j) { return a.before && j < first_row ? a.decay * a.before[row_of_weights + j] : 0.f; };
@@ -298,54 +344,36 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache_weights_kernel(FmCacheWe
     }
     return x;
   };
-  const auto last_row = [&](int j) { return a.window > 0 ? (int)std::min<long long>(len, (long long)j + a.window) : len; };   // that sees j, and one
-
-  for (int s = wave; s < steps; s += kWaves) {
-    const int j = j0 + s * kStep + lane;
-    int seen = 0;
-    if (j < j1 && fm_known_page(a.table[(size_t)b * a.columns + fm_div(j, a.page)], a.num_pages) >= 0)
-      seen = rows_left(max(first_row, j), last_row(j), a.bound_columns ? bound_of(j) : i32x4{0, 0, 0, 0});
-    const bool some = __any(seen > 0), all = __all(seen == a.T);
-    if (lane == 0) flags[s] = some ? all ? 1 : 2 : 0;
-    if (!some && j < j1) a.weights[row_of_weights + j] = old(j);
-  }
-  __syncthreads();
-  const int flag = lane < steps ? flags[lane] : 0;
-  unsigned long long left = __ballot(flag != 0);
-  const unsigned long long partly = __ballot(flag == 2);
-  const auto skip = [&](int n) {
-    for (int i = 0; i < n; ++i) left &= left - 1;
-  };
-  skip(wave);
-  if (!left) return;
+  const auto rows_end = [&](int j) { return a.window > 0 ? (int)std::min<long long>(len, (long long)j + a.window) : len; };   // behind the last that sees j
 
   // Queries: rows hq * T + t of the K/V head, 16 at a time; rows past the last are copies that give nothing
-  const int G = a.H / a.Hk, R = G * a.T, blocks = ONE ? 1 : (R + 15) / 16;
-  const auto load_rows = [&](int block, u32x4 (&q)[STEPS], f32x4& lse) {
-    const int r = min(block * 16 + c, R - 1), hq = fm_div(r, a.tokens);
-    const char* p = (const char*)a.q + 2 * ((long long)b * a.sq.b + (long long)(hk * G + hq) * a.sq.h + (long long)(r - hq * a.T) * a.sq.n);
+  const int G = a.H / a.Hk, R = G * a.T;
+  const auto query = [&](int r) {
+    const int hq = fm_div(r, a.tokens);
+    return (const char*)a.q + 2 * ((long long)b * a.sq.b + (long long)(hk * G + hq) * a.sq.h + (long long)(r - hq * a.T) * a.sq.n);
+  };
+  const auto lse_of = [&](int r) { return r < R ? minus_lse(a.lse[((size_t)b * a.H + hk * G) * a.T + r]) : -INFINITY; };   // [b, head, t] is contiguous
+  u32x4 q[STEPS];
+  f32x4 lse;
+  if constexpr (ONE) {
+    const char* p = query(min(c, R - 1));
 #pragma unroll
     for (int s = 0; s < STEPS; ++s) q[s] = ldg16(p + 2 * (E4M3 ? 64 * (s / 2) + 16 * g + 8 * (s % 2) : 32 * s + 8 * g));
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int at = block * 16 + 4 * g + i;   // [b, head, t] is contiguous
-      lse[i] = a.lse[((size_t)b * a.H + hk * G) * a.T + min(at, R - 1)];
-      if (at >= R) lse[i] = -INFINITY;
-    }
-  };
-  u32x4 q[STEPS];
-  f32x4 lse;
-  load_rows(0, q, lse);
+    for (int r = 0; r < 4; ++r) lse[r] = lse_of(4 * g + r);
+  }
 
   const char* k_head = a.k.base + (long long)hk * a.k.head;
   u32x4 kraw[kGroups][LOADS];
-  const auto load_keys = [&](int step) {
+  unsigned there = 0;   // groups that have a page, of the step that was loaded last
+  const auto load_keys = [&](int start) {
+    there = 0;
 #pragma unroll
     for (int i = 0; i < kGroups; ++i) {
-      const int j = j0 + step * kStep + i * FM_KEY_GROUP, at = min(j, j1 - 1), column = fm_div(at, a.page), slot = at - column * (int)a.page.n;
-      const int page = j < j1 ? fm_known_page(table[column], a.num_pages) : -1;
-      // slot: of the group's first key, a multiple of 16
-      const char* base = k_head + std::max(page, 0) * a.k.page + (unsigned)(slot & ~(FM_KEY_GROUP - 1)) * (unsigned long long)a.k.token;
+      const int j = start + i * FM_KEY_GROUP, at = j < end ? j : start, column = fm_div(at, a.page);
+      const int page = j < end ? fm_known_page(table[column], a.num_pages) : -1;
+      const char* base = k_head + std::max(page, 0) * a.k.page + (unsigned)(at - column * (int)a.page.n) * (unsigned long long)a.k.token;
+      there |= (page >= 0 ? 1u : 0u) << i;
       // a descriptor of no bytes where there is no page: such loads give 0 and touch no memory
       const auto rows = __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, __builtin_amdgcn_readfirstlane(page < 0 ? 0 : -1), 0x00020000);
 #pragma unroll
@@ -355,78 +383,137 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache_weights_kernel(FmCacheWe
   };
   const float scale = a.scale * kLog2e * (E4M3 ? a.k_scale[hk] : 1.f);
 
-  int step = __builtin_ctzll(left);
-  load_keys(step);
-  while (left) {
-    const bool masked = partly >> step & 1;
-    const int start = j0 + step * kStep;
-    u32x4 keys[kGroups][STEPS];
-#pragma unroll
-    for (int i = 0; i < kGroups; ++i)
-#pragma unroll
-      for (int s = 0; s < STEPS; ++s) {
-        if constexpr (E4M3) {
-          const u32x4 raw = kraw[i][s / 2];
-          const u32x2 x = widen4<F16>(raw[s % 2 * 2]), y = widen4<F16>(raw[s % 2 * 2 + 1]);
-          keys[i][s] = u32x4{x[0], x[1], y[0], y[1]};
-        } else {
-          keys[i][s] = kraw[i][s];
+  for (int row0 = 0; row0 < R; row0 += ONE ? 16 : kRows) {
+    const int blocks = ONE ? 1 : (min(R - row0, kRows) + 15) / 16;
+    if constexpr (!ONE) {
+      constexpr int PIECES = D / 8;
+      __syncthreads();   // the rows before have been read
+      for (int i = threadIdx.x; i < blocks * 16 * PIECES; i += 64 * kWaves) {
+        const int r = i / PIECES, to = i % PIECES;
+        // e4m3: which elements of d a product takes together follows the order of the keys' bytes
+        const int from = E4M3 ? 8 * (to / 8) + 2 * (to % 4) + to / 4 % 2 : to;
+        *(u32x4*)(sh.q + L::off(r, 16 * to)) = ldg16(query(min(row0 + r, R - 1)) + 16 * from);
+      }
+      if ((int)threadIdx.x < blocks * 16) sh.lse[threadIdx.x] = lse_of(row0 + threadIdx.x);
+      __syncthreads();
+    }
+    for (int panel = begin; panel < end; panel += kSteps * kStep) {
+      const int panel_end = min(end, panel + kSteps * kStep), steps = (panel_end - panel + kStep - 1) / kStep;
+      unsigned long long left, partly;
+      if (a.bound_columns) {
+        __syncthreads();   // the flags before have been read
+        for (int s = wave; s < steps; s += kWaves) {
+          const int j = panel + s * kStep + lane;
+          const int seen = j < panel_end ? rows_left(max(first_row, j), rows_end(j), bound_of(j)) : 0;
+          const bool some = __any(seen > 0), all = __all(seen == a.T);
+          if (lane == 0) sh.flag[s] = some ? all ? 1 : 2 : 0;
         }
+        __syncthreads();
+        const int flag = lane < steps ? sh.flag[lane] : 0;
+        left = __ballot(flag != 0);
+        partly = __ballot(flag == 2);
+      } else {
+        const int start = panel + lane * kStep, first = a.window > 0 ? first_row - a.window + 1 : 0;
+        left = __ballot(lane < steps && start + kStep > first);
+        partly = __ballot(start + kStep > panel_end || start + kStep - 1 > first_row || (a.window > 0 && start <= len - 1 - a.window));
       }
-    const int j = start + lane;
-    const float before = j < j1 ? old(j) : 0.f;
-    skip(kWaves);
-    if (left) {
-      step = __builtin_ctzll(left);
-      load_keys(step);
-    }
-    i32x4 bound[kGroups];
-    bool there[kGroups];
-    if (masked) {
+      // what no row sees has its old weight alone
+      if (row0 == 0)
+        for (unsigned long long none = ~left & (steps < 64 ? (1ull << steps) - 1ull : ~0ull); none; none &= none - 1) {
+          const int s = __builtin_ctzll(none), j = panel + s * kStep + lane;
+          if (s % kWaves == wave && j < panel_end) a.weights[row_of_weights + j] = old(j);
+        }
+      // the wave takes every fourth of the others
+      for (int i = 0; i < wave; ++i) left &= left - 1;
+      if (!left) continue;
+      int step = __builtin_ctzll(left);
+      load_keys(panel + step * kStep);
+      while (left) {
+        const int start = panel + step * kStep, j = start + lane;
+        const unsigned pages = there;
+        const bool masked = (partly >> step & 1) || pages != (1u << kGroups) - 1u;
+        u32x4 keys[kGroups][STEPS];
 #pragma unroll
-      for (int i = 0; i < kGroups; ++i) {
-        const int key = start + i * FM_KEY_GROUP + c;
-        bound[i] = a.bound_columns ? bound_of(key) : i32x4{0, 0, 0, 0};
-        there[i] = key < j1 && fm_known_page(a.table[(size_t)b * a.columns + fm_div(min(key, j1 - 1), a.page)], a.num_pages) >= 0;
-      }
-    }
-    float sum[kGroups] = {};
-    for (int block = 0; block < blocks; ++block) {
-      if constexpr (!ONE) load_rows(block, q, lse);
-      f32x4 score[kGroups];
+        for (int i = 0; i < kGroups; ++i)
 #pragma unroll
-      for (int i = 0; i < kGroups; ++i) score[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+          for (int s = 0; s < STEPS; ++s) {
+            if constexpr (E4M3) {
+              const u32x4 raw = kraw[i][s / 2];
+              const u32x2 x = widen4<F16>(raw[s % 2 * 2]), y = widen4<F16>(raw[s % 2 * 2 + 1]);
+              keys[i][s] = u32x4{x[0], x[1], y[0], y[1]};
+            } else {
+              keys[i][s] = kraw[i][s];
+            }
+          }
+        const float before = j >= panel_end ? 0.f : row0 == 0 ? old(j) : a.weights[row_of_weights + j];
+        for (int i = 0; i < kWaves; ++i) left &= left - 1;
+        if (left) {
+          step = __builtin_ctzll(left);
+          load_keys(panel + step * kStep);
+        }
+        float sum[kGroups] = {};
+        const auto block = [&](int r0, const u32x4 (&q)[STEPS], const f32x4& lse, const auto& mask) {
+          f32x4 score[kGroups];
 #pragma unroll
-      for (int s = 0; s < STEPS; ++s)
+          for (int i = 0; i < kGroups; ++i) score[i] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int i = 0; i < kGroups; ++i) score[i] = mfma_keys<F16>(q[s], keys[i][s], score[i]);
+          for (int s = 0; s < STEPS; ++s)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const float minus = minus_lse(lse[r]);
-        int row = 0;
+            for (int i = 0; i < kGroups; ++i) score[i] = mfma_keys<F16>(q[s], keys[i][s], score[i]);
+#pragma unroll
+          for (int i = 0; i < kGroups; ++i) {
+            f32x4 x;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) x[r] = fmaf(score[i][r], scale, lse[r]);
+            mask(x, i, r0);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) x[r] = fast_exp2(x[r]);
+            sum[i] += (x[0] + x[1]) + (x[2] + x[3]);
+          }
+        };
+        const auto all_blocks = [&](const auto& mask) {
+          if constexpr (ONE) {
+            block(0, q, lse, mask);
+          } else {
+            for (int n = 0; n < blocks; ++n) {
+              u32x4 rows[STEPS];
+#pragma unroll
+              for (int s = 0; s < STEPS; ++s) rows[s] = *(const u32x4*)(sh.q + L::off(c, 16 * g) + n * 16 * L::RS + s * 1024);
+              block(row0 + n * 16, rows, *(const f32x4*)&sh.lse[n * 16 + 4 * g], mask);
+            }
+          }
+        };
         if (masked) {
-          const int at = min(block * 16 + 4 * g + r, R - 1);
-          row = first_row + at - fm_div(at, a.tokens) * a.T;
+          i32x4 bound[kGroups];
+          int key[kGroups], behind[kGroups];   // rows from key on and before `behind` see it, bounds apart
+#pragma unroll
+          for (int i = 0; i < kGroups; ++i) {
+            const int at = start + i * FM_KEY_GROUP + c;
+            const bool real = at < panel_end && (pages >> i & 1);
+            bound[i] = a.bound_columns ? bound_of(at) : i32x4{0, 0, 0, 0};
+            key[i] = at;
+            behind[i] = real ? rows_end(at) : 0;
+          }
+          all_blocks([&](f32x4& x, int i, int r0) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              const int at = min(r0 + 4 * g + r, R - 1), row = first_row + at - fm_div(at, a.tokens) * a.T;
+              const bool gone = (row < key[i]) | (row >= behind[i]) | ((bound[i][0] <= row) & (row < bound[i][1])) | ((bound[i][2] <= row) & (row < bound[i][3]));
+              x[r] = gone ? -INFINITY : x[r];
+            }
+          });
+        } else {
+          all_blocks([](f32x4&, int, int) {});
         }
+        float mine = 0.f;
 #pragma unroll
         for (int i = 0; i < kGroups; ++i) {
-          float x = fmaf(score[i][r], scale, minus);
-          if (masked) {
-            const int key = start + i * FM_KEY_GROUP + c;
-            const bool sees = there[i] && key <= row && row < last_row(key) && !hides(bound[i], row);
-            if (!sees) x = -INFINITY;
-          }
-          sum[i] += fast_exp2(x);
+          const float x = quad_sum(sum[i]);
+          if (i == g) mine = x;
         }
+        if (j < panel_end) a.weights[row_of_weights + j] = before + mine;
       }
     }
-    float mine = 0.f;
-#pragma unroll
-    for (int i = 0; i < kGroups; ++i) {
-      const float x = quad_sum(sum[i]);
-      if (i == g) mine = x;
-    }
-    if (j < j1) a.weights[row_of_weights + j] = before + mine;
   }
 }
 
@@ -467,8 +554,19 @@ hipError_t fm_launch_weights(FmWeightsArgs a, float* weights, const FmWeightsCut
   return hipGetLastError();
 }
 
+bool fm_cut_cache_weights(FmCacheWeightsArgs& a, int cus) {
+  // Every workgroup goes over all lengths, 64 at a time and about 1 us each; more sequences fill the chip by themselves.
+  a.dealt = a.B <= 512;
+  a.chunk_keys = std::min(a.places, 8192);
+  const int places = 2 * (cus > 0 ? cus : 256);
+  a.chunks = fm_divisor(a.dealt ? std::max(1, places / a.Hk) : (a.places + a.chunk_keys - 1) / a.chunk_keys);
+  const long long units = a.dealt ? fm_most_units((int)a.chunks.n, a.B) : (long long)a.B * a.chunks.n;
+  return (units + 8) * a.Hk < 1 << 24;   // a launch has fewer than 2^32 lanes
+}
+
 hipError_t fm_launch_cache_weights(const FmCacheWeightsArgs& a, bool f16, bool e4m3, hipStream_t stream) {
-  const unsigned workgroups = (unsigned)(((long long)a.B * a.chunks.n + 7) / 8 * 8 * a.Hk);
+  const long long units = a.dealt ? fm_most_units((int)a.chunks.n, a.B) : (long long)a.B * a.chunks.n;
+  const unsigned workgroups = (unsigned)((units + 7) / 8 * 8 * a.Hk);
   if (a.d == 64) {
     if (f16) e4m3 ? fm::launch<64, true, true>(a, workgroups, stream) : fm::launch<64, true, false>(a, workgroups, stream);
     else e4m3 ? fm::launch<64, false, true>(a, workgroups, stream) : fm::launch<64, false, false>(a, workgroups, stream);

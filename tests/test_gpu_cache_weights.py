@@ -172,3 +172,27 @@ def test_on_a_stream_of_its_own_and_in_a_graph():
         torch.cuda.synchronize()
         assert torch.equal(out, want), n
     assert raw(p["k_cache"]).shape[0] > 0
+
+
+@pytest.mark.parametrize("B,long", [(64, 900), (65, 1300), (130, 1100), (512, 300), (520, 700)])
+@pytest.mark.parametrize("mask", ["none", "window"])
+def test_more_sequences_than_lanes(B, long, mask):
+    """Lengths are added up 64 sequences at a time, up to 512; of more, every sequence has its own chunks."""
+    rng = np.random.default_rng(B)
+    lens = rng.integers(0, 40, B)
+    lens[0], lens[B // 2], lens[-1] = long, 64, long // 2
+    _run(_problem(B, lens, 2, 1, 1, 64, 16, "bf16", "bf16", mask=mask, hide=False), 0.5)
+
+
+def test_many_long_sequences():
+    """More chunks than one to a sequence beyond 512 sequences: 10000 keys are two of 8192."""
+    lens = np.full(513, 3)
+    lens[7] = 10000
+    _run(_problem(20, lens, 1, 1, 1, 64, 2048, "bf16", "bf16", hide=False), 0.5)
+
+
+@pytest.mark.parametrize("type,cache", [("bf16", "bf16"), ("f16", "e4m3")])
+def test_more_rows_than_lie_in_lds(type, cache):
+    """300 and 2048 query rows to a K/V head."""
+    _run(_problem(21, [400, 33], 12, 1, 25, 128, 64, type, cache, mask="bounds"), 0.5)
+    _run(_problem(22, [300], 8, 1, 256, 64, 16, type, cache, hide=False), 0.5)
