@@ -414,13 +414,17 @@ size_t flashmask_decode_workspace_bytes(int sequences, int H, int H_kv, int T, i
  *     of the keys j < lens[b] - T it sees those with                     j > i - window (window > 0),
  *     of the drafted tokens those that are its ancestors or itself with  depth[u] > depth[t] - window,
  * and of both no key with LTS[j] <= i < LTE[j] or UTS[j] <= i < UTE[j] (j the key's place).  A token whose place is below 0 is not there.
- *   parents     int32 [sequences, T];  all else as for flashmask_decode, its workspace, limits and guarantees among it.  (New tokens are
- *               written to places that are not their positions by flashmask_rope and flashmask_cache_append without freqs.)
+ *   parents     int32 [sequences, T]
+ *   workspace   at least flashmask_decode_tree_workspace_bytes(), 256-byte aligned
+ * All else is as for flashmask_decode, its limits and guarantees among it.  (New tokens are written to places that are not their positions by
+ * flashmask_rope and flashmask_cache_append without freqs.)
  */
 int flashmask_decode_tree(const flashmask_cache* cache, const void* q, const int32_t* lens, const int32_t* parents, const int32_t* lts,
                           const int32_t* lte, const int32_t* uts, const int32_t* ute, int bound_columns, int window, float scale,
                           void* out, float* lse, int type, int H, int T, const flashmask_strides* strides, void* workspace,
                           size_t workspace_bytes, void* hip_stream);
+/* Bytes of scratch of a call on `sequences` sequences, 0 for an invalid shape.  Host-only. */
+size_t flashmask_decode_tree_workspace_bytes(int sequences, int H, int H_kv, int T, int d);
 
 /*
  * Takes over the accepted path of a tree of drafted tokens, the last T (1 to 256) of every sequence: with start = lens[b] - T, the token at place

@@ -10,6 +10,6 @@ from .binding import (  # noqa: F401
 from .serving import (  # noqa: F401
     FM_ROPE_HALF, FM_ROPE_INTERLEAVED, flashmask_cache_accept, flashmask_cache_append, flashmask_cache_compact, flashmask_cache_evict,
     flashmask_cache_evict_workspace_bytes, flashmask_cache_fork, flashmask_cache_free_list, flashmask_cache_plan_bytes, flashmask_cache_weights,
-    flashmask_decode, flashmask_decode_tree, flashmask_decode_workspace_bytes, flashmask_rope, flashmask_rope_bwd, flashmask_weights,
-    flashmask_weights_workspace_bytes,
+    flashmask_decode, flashmask_decode_tree, flashmask_decode_tree_workspace_bytes, flashmask_decode_workspace_bytes, flashmask_rope,
+    flashmask_rope_bwd, flashmask_weights, flashmask_weights_workspace_bytes,
 )

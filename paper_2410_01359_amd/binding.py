@@ -89,6 +89,8 @@ def load_library() -> ctypes.CDLL:
     lib.flashmask_decode_workspace_bytes.argtypes = [i, i, i, i, i]
     lib.flashmask_decode_tree.restype = i
     lib.flashmask_decode_tree.argtypes = [vp, vp, ip, ip, ip, ip, ip, ip, i, i, f, vp, fp, i, i, i, vp, vp, sz, vp]
+    lib.flashmask_decode_tree_workspace_bytes.restype = sz
+    lib.flashmask_decode_tree_workspace_bytes.argtypes = [i, i, i, i, i]
     lib.flashmask_weights.restype = i
     lib.flashmask_weights.argtypes = [vp, vp, fp, ip, ip, ip, ip, f, fp, i, i, i, i, i, i, vp, vp, sz, vp]
     lib.flashmask_weights_workspace_bytes.restype = sz

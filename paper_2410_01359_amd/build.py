@@ -9,7 +9,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB_PATH = os.path.join(HERE, "libflashmask.so")
 SOURCES = ["fm_api.hip", "fm_preprocess.hip", "fm_fwd.hip", "fm_bwd.hip", "fm_probe.hip",
-           "fm_rope.hip", "fm_decode.hip", "fm_pages.hip", "fm_weights.hip", "fm_evict.hip", "fm_serving_api.hip"]
+           "fm_rope.hip", "fm_decode.hip", "fm_pages.hip", "fm_tree.hip", "fm_weights.hip", "fm_evict.hip", "fm_serving_api.hip"]
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

@@ -82,6 +82,18 @@ __device__ __forceinline__ bool odd_word(unsigned x) {
   constexpr unsigned kOne = E4M3 ? 0x01010101u : F16 ? 0x04000400u : 0x00800080u, kCarry = E4M3 ? 0x80808080u : 0x80008000u;
   return (((x & kOnes) + kOne) & kCarry) != 0;
 }
+// Whether any of eight 16-bit values is an infinity or NaN, and the values with 0 for those.
+template <bool F16>
+__device__ __forceinline__ bool odd_words(u32x4 x) {
+  return odd_word<F16, false>(x[0]) | odd_word<F16, false>(x[1]) | odd_word<F16, false>(x[2]) | odd_word<F16, false>(x[3]);
+}
+template <bool F16>
+__device__ __forceinline__ u32x4 without_odd(u32x4 x) {
+  constexpr unsigned kOnes = F16 ? 0x7c00u : 0x7f80u;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) x[w] &= ((x[w] & kOnes) == kOnes ? 0u : 0xffffu) | ((x[w] >> 16 & kOnes) == kOnes ? 0u : 0xffff0000u);
+  return x;
+}
 // Maximum over the four lanes l, l ^ 16, l ^ 32, l ^ 48.
 __device__ __forceinline__ float quad_max(float x) {
   auto r = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(int, x), __builtin_bit_cast(int, x), false, false);
@@ -109,6 +121,14 @@ __device__ __forceinline__ float reference(float m) { return m == -INFINITY ? 0.
 // Whether the bounds (LTS, LTE, UTS, UTE) of a key hide it from row i.
 __device__ __forceinline__ bool hides(const i32x4& bound, int i) {
   return (bound[0] <= i && i < bound[1]) || (bound[2] <= i && i < bound[3]);
+}
+
+
+// Rows of [lo, hi) that the bounds of a key leave.
+__device__ __forceinline__ int rows_left(int lo, int hi, const i32x4& bound) {
+  if (lo >= hi) return 0;
+  const int a0 = max(bound[0], lo), b0 = min(bound[1], hi), a1 = max(bound[2], lo), b1 = min(bound[3], hi);
+  return hi - lo - max(b0 - a0, 0) - max(b1 - a1, 0) + max(min(b0, b1) - max(a0, a1), 0);
 }
 
 }  // namespace fm

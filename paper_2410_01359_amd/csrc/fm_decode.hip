@@ -18,6 +18,7 @@
 #include "fm_cache_math.h"
 #include "fm_common.h"
 #include "fm_serving.h"
+#include "fm_tree.h"
 
 namespace fm {
 
@@ -49,33 +50,8 @@ struct Decode {
   };
 };
 
-// A tree of drafted tokens: token t follows token parents[t] < t, or the sequence itself (any other value).  Its row is as many rows behind the first
-// new one as it has ancestors in the tree, and of the drafted tokens it sees those and itself.
-struct Tree {
-  unsigned ancestors[FM_MOST_NEW_TOKENS][FM_MOST_NEW_TOKENS / 32];   // of a token, itself among them
-  int depth[FM_MOST_NEW_TOKENS];
-  __device__ __forceinline__ bool on_path(int t, int u) const { return ancestors[t][u / 32] >> (u % 32) & 1; }
-};
 template <class Args>
 constexpr bool kTree = std::is_same_v<Args, FmTreeArgs>;
-
-// Every token walks up its line; parents come before their children, so that ends.
-__device__ __forceinline__ void plant(Tree& tree, const int* parents, int T) {
-  const int t = threadIdx.x;
-  if (t < T) {
-    const int p = parents[t];
-    tree.depth[t] = p >= 0 && p < t ? p : -1;
-#pragma unroll
-    for (int w = 0; w < FM_MOST_NEW_TOKENS / 32; ++w) tree.ancestors[t][w] = 0;
-  }
-  barrier_nofence();
-  int depth = -1;
-  if (t < T)
-    for (int u = t; u >= 0; u = tree.depth[u], ++depth) tree.ancestors[t][u / 32] |= 1u << (u % 32);
-  barrier_nofence();
-  if (t < T) tree.depth[t] = depth;
-  barrier_nofence();
-}
 
 // TEAMS > 1: the workgroup's waves are teams that go over the same keys together, for blocks of query rows, which find in the caches what
 // the first of them loads, or for heads whose rows lie side by side.
@@ -657,6 +633,17 @@ __global__ __launch_bounds__(256) void join_kernel(FmDecodeArgs a, FmDivisor row
   if (lane == 0) a.lse[((size_t)b * a.H + h) * a.T + t] = total == 0.f ? -INFINITY : (top + fast_log2(total * kUnshift<F16>)) * kLn2;
 }
 
+static void launch_list(const FmDecodeArgs& a, int round, hipStream_t stream) {
+  hipLaunchKernelGGL(plan_units_kernel, dim3(1), dim3(kPlanThreads), 0, stream, a, fm_divisor(a.cut.chunks), round,
+                     fm_listed_units(a.cut.chunks, a.B), fm_most_splits(a.cut.chunks, a.B));
+}
+template <int D, bool F16>
+static void launch_join(const FmDecodeArgs& a, hipStream_t stream) {
+  const int R = a.H / a.Hk * a.T;
+  hipLaunchKernelGGL((join_kernel<D, F16>), dim3(a.Hk * R, a.split ? fm_most_splits(a.cut.chunks, a.B) : a.B), dim3(256), 0, stream, a, fm_divisor(R),
+                     fm_divisor(a.T));
+}
+
 template <int D, bool E4M3>
 static int round_groups(const FmDecodeCut& cut) {
   return kWaves / cut.teams * (cut.block_rows == 16 ? Decode<D, false, E4M3, 1>::GROUPS : Decode<D, false, E4M3, 2>::GROUPS);
@@ -671,9 +658,7 @@ static void launch(Args a, hipStream_t stream) {
 #define FM_DECODE(NB, TEAMS)                                                                                                      \
   hipLaunchKernelGGL((decode_kernel<D, F16, E4M3, NB, TEAMS, Args>), dim3((unsigned)std::min(workgroups - a.first_workgroup, kMost)), \
                      dim3(64 * kWaves), 0, stream, a, cut.row_blocks * a.Hk, di, dr, dt, dc)
-  if (a.units)
-    hipLaunchKernelGGL(plan_units_kernel, dim3(1), dim3(kPlanThreads), 0, stream, a, dc,
-                       round_groups<D, E4M3>(cut), units, fm_most_splits(cut.chunks, a.B));
+  if (a.units) launch_list(a, round_groups<D, E4M3>(cut), stream);
   for (a.first_workgroup = 0; a.first_workgroup < workgroups; a.first_workgroup += kMost) {
     if (cut.block_rows == 16) {
       if constexpr (E4M3 || D == 64) {   // rows of less than 256 bytes, which may go together
@@ -688,10 +673,7 @@ static void launch(Args a, hipStream_t stream) {
     }
   }
 #undef FM_DECODE
-  if (a.plan) {
-    const int R = a.H / a.Hk * a.T;
-    hipLaunchKernelGGL((join_kernel<D, F16>), dim3(a.Hk * R, a.split ? fm_most_splits(cut.chunks, a.B) : a.B), dim3(256), 0, stream, a, fm_divisor(R), dt);
-  }
+  if (a.plan) launch_join<D, F16>(a, stream);
 }
 
 }  // namespace fm
@@ -741,3 +723,8 @@ static hipError_t launch_decode(const Args& a, bool f16, bool e4m3, hipStream_t 
 }
 hipError_t fm_launch_decode(const FmDecodeArgs& a, bool f16, bool e4m3, hipStream_t stream) { return launch_decode(a, f16, e4m3, stream); }
 hipError_t fm_launch_decode_tree(const FmTreeArgs& a, bool f16, bool e4m3, hipStream_t stream) { return launch_decode(a, f16, e4m3, stream); }
+void fm_launch_decode_list(const FmDecodeArgs& a, int round, hipStream_t stream) { fm::launch_list(a, round, stream); }
+void fm_launch_decode_join(const FmDecodeArgs& a, bool f16, hipStream_t stream) {
+  if (a.d == 64) f16 ? fm::launch_join<64, true>(a, stream) : fm::launch_join<64, false>(a, stream);
+  else f16 ? fm::launch_join<128, true>(a, stream) : fm::launch_join<128, false>(a, stream);
+}

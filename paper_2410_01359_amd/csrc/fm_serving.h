@@ -86,6 +86,14 @@ struct FmTreeArgs : FmDecodeArgs {
   const int* parents;     // [B, T]
 };
 hipError_t fm_launch_decode_tree(const FmTreeArgs& a, bool f16, bool e4m3, hipStream_t stream);
+// Many query rows to a K/V head go through a kernel of their own, cut by fm_tree_cut in multiples of FM_TREE_ROUND groups of keys.
+inline bool fm_tree_is_wide(int H, int Hk, int T) { return H / Hk * T > 64; }
+constexpr int FM_TREE_ROUND = 4;
+FmDecodeCut fm_tree_cut(int H, int Hk, int T, int d, int B, int cus);
+hipError_t fm_launch_tree_wide(const FmTreeArgs& a, bool f16, bool e4m3, hipStream_t stream);
+// What split calls launch before and behind their loop: the list of chunks, cut in multiples of `round` groups, where there is one, and the join.
+void fm_launch_decode_list(const FmDecodeArgs& a, int round, hipStream_t stream);
+void fm_launch_decode_join(const FmDecodeArgs& a, bool f16, hipStream_t stream);
 
 // How a call on a prompt is cut: row tiles of a head, blocks of keys, parts that the tiles of a block and a group's heads are cut into.
 struct FmWeightsCut {

@@ -101,8 +101,16 @@ size_t decode_bytes(const DecodeCuts& cuts, int sequences, int H, int T, int d) 
   return std::max(decode_space(cuts.of[0], sequences, H, T, d).total, decode_space(cuts.of[1], sequences, H, T, d).total);
 }
 
+// Of a tree's call: that of many query rows to a K/V head has a cut of its own.
+int check_tree_shape(int sequences, int H, int Hk, int T, int d, DecodeCuts& cuts, FmDecodeCut& wide) {
+  if (int rc = check_decode_shape(sequences, H, Hk, T, d, cuts)) return rc;
+  if (!fm_tree_is_wide(H, Hk, T)) return FM_OK;
+  wide = fm_tree_cut(H, Hk, T, d, sequences, fm_compute_units());
+  return (fm_most_units(wide.chunks, sequences) + 8ll) * wide.workgroups < 1 << 24 ? FM_OK : FM_ERR_SHAPE;
+}
+
 // Checks of a decoding call and its launch arguments.
-int decode_args(const flashmask_cache* cache, const void* q, const int32_t* lens, const int32_t* lts, const int32_t* lte, const int32_t* uts,
+int decode_args(bool tree, const flashmask_cache* cache, const void* q, const int32_t* lens, const int32_t* lts, const int32_t* lte, const int32_t* uts,
                 const int32_t* ute, int bound_columns, int window, float scale, void* out, float* lse, int type, int H, int T,
                 const flashmask_strides* strides, void* workspace, size_t workspace_bytes, FmDecodeArgs& a) {
   if (int rc = check_cache(cache)) return rc;
@@ -111,14 +119,17 @@ int decode_args(const flashmask_cache* cache, const void* q, const int32_t* lens
   if (bounds && (!lts || !lte || !uts || !ute)) return FM_ERR_NULL;
   if (int rc = check_row_type(type, *cache)) return rc;
   DecodeCuts cuts;
-  if (int rc = check_decode_shape(cache->sequences, H, cache->heads, T, cache->d, cuts)) return rc;
+  const bool wide = tree && fm_tree_is_wide(H, cache->heads, T);
+  if (int rc = tree ? check_tree_shape(cache->sequences, H, cache->heads, T, cache->d, cuts, a.cut)
+                    : check_decode_shape(cache->sequences, H, cache->heads, T, cache->d, cuts)) return rc;
   if (bounds && bound_columns <= 0) return FM_ERR_SHAPE;
   if ((long long)cache->sequences * cache->columns * cache->page > 1ll << 34) return FM_ERR_SHAPE;   // groups of 16 keys are added up in 32 bits
   if (!(scale > 0.f) || !(scale < 3.0e38f) || window < 0) return FM_ERR_ARG;
   for (int t = 0; t < 2; ++t)
     if (int rc = check_strides(strides[t], type, cache->sequences, H, T, cache->d)) return rc;
   if (misaligned(q) || misaligned(out)) return FM_ERR_ALIGN;
-  if (bad_workspace(workspace, workspace_bytes, decode_bytes(cuts, cache->sequences, H, T, cache->d))) return FM_ERR_WORKSPACE;
+  if (bad_workspace(workspace, workspace_bytes, wide ? decode_space(a.cut, cache->sequences, H, T, cache->d).total
+                                                     : decode_bytes(cuts, cache->sequences, H, T, cache->d))) return FM_ERR_WORKSPACE;
   char* ws = (char*)workspace;
   a.q = q; a.out = out; a.lse = lse; a.sq = to_kernel(strides[0]); a.so = to_kernel(strides[1]);
   a.k = pages(cache->k, cache->sk, cache->type);
@@ -135,9 +146,10 @@ int decode_args(const flashmask_cache* cache, const void* q, const int32_t* lens
   // Pages stored token by token have the rows of all heads side by side: a workgroup takes two of less than 256 bytes together.
   const int row = cache->d * element_bytes(cache->type);
   const bool side_by_side = a.k.head < 256 && a.v.head < 256;
-  a.cut = cuts.of[side_by_side && row < 256];
+  if (!wide) a.cut = cuts.of[side_by_side && row < 256];
+  const int round = wide ? FM_TREE_ROUND : fm_decode_round_groups(cache->d, cache->type == FM_TYPE_E4M3, a.cut);
   const bool split = (long long)cache->columns * cache->page >
-                     fm_whole_keys(fm_decode_round_groups(cache->d, cache->type == FM_TYPE_E4M3, a.cut), (long long)cache->sequences * a.cut.workgroups,
+                     fm_whole_keys(round, (long long)cache->sequences * a.cut.workgroups,
                                    a.cut.least, fm_compute_units());
   const DecodeSpace space = decode_space(a.cut, cache->sequences, H, T, cache->d);
   const bool listed = split && a.cut.listed;
@@ -226,9 +238,16 @@ int flashmask_decode(const flashmask_cache* cache, const void* q, const int32_t*
                      void* out, float* lse, int type, int H, int T, const flashmask_strides* strides, void* workspace,
                      size_t workspace_bytes, void* hip_stream) {
   FmDecodeArgs a;
-  if (int rc = decode_args(cache, q, lens, lts, lte, uts, ute, bound_columns, window, scale, out, lse, type, H, T, strides, workspace,
+  if (int rc = decode_args(false, cache, q, lens, lts, lte, uts, ute, bound_columns, window, scale, out, lse, type, H, T, strides, workspace,
                            workspace_bytes, a)) return rc;
   return done(fm_launch_decode(a, type == FM_TYPE_F16, cache->type == FM_TYPE_E4M3, (hipStream_t)hip_stream));
+}
+
+size_t flashmask_decode_tree_workspace_bytes(int sequences, int H, int H_kv, int T, int d) {
+  DecodeCuts cuts;
+  FmDecodeCut wide;
+  if (check_tree_shape(sequences, H, H_kv, T, d, cuts, wide) != FM_OK) return 0;
+  return fm_tree_is_wide(H, H_kv, T) ? decode_space(wide, sequences, H, T, d).total : decode_bytes(cuts, sequences, H, T, d);
 }
 
 int flashmask_decode_tree(const flashmask_cache* cache, const void* q, const int32_t* lens, const int32_t* parents, const int32_t* lts,
@@ -237,10 +256,10 @@ int flashmask_decode_tree(const flashmask_cache* cache, const void* q, const int
                           size_t workspace_bytes, void* hip_stream) {
   if (!parents) return FM_ERR_NULL;
   FmTreeArgs a;
-  if (int rc = decode_args(cache, q, lens, lts, lte, uts, ute, bound_columns, window, scale, out, lse, type, H, T, strides, workspace,
+  if (int rc = decode_args(true, cache, q, lens, lts, lte, uts, ute, bound_columns, window, scale, out, lse, type, H, T, strides, workspace,
                            workspace_bytes, a)) return rc;
   a.parents = parents;
-  return done(fm_launch_decode_tree(a, type == FM_TYPE_F16, cache->type == FM_TYPE_E4M3, (hipStream_t)hip_stream));
+  return done((fm_tree_is_wide(H, cache->heads, T) ? fm_launch_tree_wide : fm_launch_decode_tree)(a, type == FM_TYPE_F16, cache->type == FM_TYPE_E4M3, (hipStream_t)hip_stream));
 }
 
 size_t flashmask_weights_workspace_bytes(int B, int H, int H_kv, int N, int d, int first_row) {

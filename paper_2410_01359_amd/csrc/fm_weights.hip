@@ -9,6 +9,7 @@
 #include "fm_cache_math.h"
 #include "fm_common.h"
 #include "fm_serving.h"
+#include "fm_tree.h"
 
 namespace fm {
 
@@ -268,13 +269,6 @@ __global__ __launch_bounds__(256) void join_weights_kernel(const float* __restri
 // some rows do not see take the element mask.
 constexpr int kStep = 64, kGroups = kStep / FM_KEY_GROUP, kWaves = 4, kSteps = 64, kRows = 256;   // kSteps: of a panel, whose flags lie together
 
-// Rows of [lo, hi) that an interval pair leaves.
-__device__ __forceinline__ int rows_left(int lo, int hi, const i32x4& bound) {
-  if (lo >= hi) return 0;
-  const int a0 = max(bound[0], lo), b0 = min(bound[1], hi), a1 = max(bound[2], lo), b1 = min(bound[3], hi);
-  return hi - lo - max(b0 - a0, 0) - max(b1 - a1, 0) + max(min(b0, b1) - max(a0, a1), 0);
-}
-
 template <int D, bool ONE>
 struct CacheWeightsShared {
   int flag[kSteps];
@@ -294,33 +288,13 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache_weights_kernel(FmCacheWe
   const int turn = fm_div(blockIdx.x >> 3, a.by_head), hk = (blockIdx.x >> 3) - turn * a.Hk, unit = turn * 8 + (blockIdx.x & 7);
   int b, len, begin, end;
   if (a.dealt) {
-    int lane_len = lane < a.B ? a.lens[lane] : 0;
-    const auto lane_groups = [&](int base) {
-      if (a.B > 64) lane_len = base + lane < a.B ? a.lens[base + lane] : 0;
-      return (min(max(lane_len, 0), a.places) + FM_KEY_GROUP - 1) / FM_KEY_GROUP;
-    };
-    unsigned total = 0;
-    for (int base = 0; base < a.B; base += 64) total += wave_last(wave_scan(lane_groups(base)));
-    const int size = fm_chunk_groups(total, a.chunks, kWaves * kGroups, kWaves * kGroups);
-    int chunk = 0, chunks = 1, groups = 0;
-    for (int units = 0, base = 0;;) {
-      const int mine = lane_groups(base), n = base + lane < a.B ? fm_chunks_of(mine, size) : 0, upto = wave_scan(n);
-      const unsigned long long behind = __ballot(units + upto > unit);
-      if (behind) {
-        const int at = __builtin_ctzll(behind);
-        b = base + at;
-        chunks = __builtin_amdgcn_readlane(n, at);
-        chunk = unit - (units + __builtin_amdgcn_readlane(upto, at) - chunks);
-        groups = __builtin_amdgcn_readlane(mine, at);
-        len = __builtin_amdgcn_readlane(lane_len, at);
-        break;
-      }
-      units += wave_last(upto);
-      base += 64;
-      if (base >= a.B) return;
-    }
-    const int keys = fm_even_chunk(groups, chunks, kGroups) * FM_KEY_GROUP;
-    begin = chunk * keys;
+    const auto groups_of = [&](int n) { return (min(max(n, 0), a.places) + FM_KEY_GROUP - 1) / FM_KEY_GROUP; };
+    Chunk chunk;
+    if (!find_chunk(a.lens, a.B, a.chunks, kWaves * kGroups, kWaves * kGroups, unit, groups_of, chunk)) return;
+    b = chunk.b;
+    len = chunk.len;
+    const int keys = fm_even_chunk(groups_of(len), chunk.of, kGroups) * FM_KEY_GROUP;
+    begin = chunk.number * keys;
     end = begin + keys;
   } else {
     b = fm_div(unit, a.chunks);
@@ -558,8 +532,10 @@ bool fm_cut_cache_weights(FmCacheWeightsArgs& a, int cus) {
   // Every workgroup goes over all lengths, 64 at a time and about 1 us each; more sequences fill the chip by themselves.
   a.dealt = a.B <= 512;
   a.chunk_keys = std::min(a.places, 8192);
-  const int places = 2 * (cus > 0 ? cus : 256);
-  a.chunks = fm_divisor(a.dealt ? std::max(1, places / a.Hk) : (a.places + a.chunk_keys - 1) / a.chunk_keys);
+  // Four rounds of the two workgroups that a compute unit holds: there is nothing to join, and 64 ragged sequences take 82 us, with one, two, three
+  // and eight rounds 90, 87, 83 and 85.
+  const int workgroups = 8 * (cus > 0 ? cus : 256);
+  a.chunks = fm_divisor(a.dealt ? std::max(1, workgroups / a.Hk) : (a.places + a.chunk_keys - 1) / a.chunk_keys);
   const long long units = a.dealt ? fm_most_units((int)a.chunks.n, a.B) : (long long)a.B * a.chunks.n;
   return (units + 8) * a.Hk < 1 << 24;   // a launch has fewer than 2^32 lanes
 }

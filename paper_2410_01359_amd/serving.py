@@ -211,6 +211,10 @@ def _bounds(bounds, B: int, device: int):
     return [x.data_ptr() for x in bounds], columns
 
 
+def flashmask_decode_tree_workspace_bytes(sequences: int, H: int, H_kv: int, T: int, d: int) -> int:
+    return int(load_library().flashmask_decode_tree_workspace_bytes(sequences, H, H_kv, T, d)) if _fits(sequences, H, H_kv, T, d) else 0
+
+
 def flashmask_decode_tree(q, k_cache, v_cache, table, lens, parents, scale: float, *, bounds=None, window: int = 0, k_scale=None, v_scale=None,
                           workspace: torch.Tensor | None = None):
     """flashmask_decode where the last T tokens of a sequence are a tree of drafted ones: token t follows token parents[b, t] < t of them
@@ -234,7 +238,7 @@ def flashmask_decode_tree(q, k_cache, v_cache, table, lens, parents, scale: floa
     lse = torch.empty(B, H, T, dtype=torch.float32, device=q.device)
     lib = load_library()
     if workspace is None:
-        workspace = torch.empty(max(int(lib.flashmask_decode_workspace_bytes(B, H, heads, T, d)), 256), dtype=torch.uint8, device=q.device)
+        workspace = torch.empty(max(int(lib.flashmask_decode_tree_workspace_bytes(B, H, heads, T, d)), 256), dtype=torch.uint8, device=q.device)
     _check(lib.flashmask_decode_tree(cache, q.data_ptr(), lens.data_ptr(), parents.data_ptr(), *at, columns, window, scale, out.data_ptr(),
                                      lse.data_ptr(), type_id, H, T, _TWO.pack(sq[0], sq[1], sq[2], so[0], so[1], so[2]), workspace.data_ptr(),
                                      workspace.numel() * workspace.element_size(), _stream()), "flashmask_decode_tree")

@@ -146,7 +146,7 @@ def test_on_a_stream_of_its_own_and_in_a_graph():
     import paper_2410_01359_amd as fm
     p = _problem(8, [2000, 700, 40], 8, 2, 20, 64, 16, "bf16", "bf16")
     p["parents"] = ints(p["parents"])
-    ws = torch.empty(fm.flashmask_decode_workspace_bytes(3, 8, 2, 20, 64), dtype=torch.uint8, device="cuda")
+    ws = torch.empty(fm.flashmask_decode_tree_workspace_bytes(3, 8, 2, 20, 64), dtype=torch.uint8, device="cuda")
 
     def call():
         return fm.flashmask_decode_tree(p["q"], p["k_cache"], p["v_cache"], p["table"], p["lens"], p["parents"], p["scale"], workspace=ws)

@@ -124,6 +124,14 @@ def test_sizes_of_scratch():
         assert of_weights(*bad) == 0
     for bad in ((0, 8, 10), (1, 0, 10), (1, 8, 0), (70000, 8, 10)):
         assert of_evict(*bad) == 0
+    of_tree = fm.flashmask_decode_tree_workspace_bytes
+    assert of_tree(2, 8, 2, 5, 64) > 0 and 0 < of_tree(2, 32, 8, 256, 128) <= 1 << 28
+    for bad in ((0, 8, 8, 1, 128), (1, 0, 1, 1, 128), (1, 8, 3, 1, 128), (1, 8, 0, 1, 128), (1, 8, 8, 0, 128), (1, 8, 8, 257, 128), (1, 8, 8, 1, 96)):
+        assert of_tree(*bad) == 0
+    for at in range(5):
+        shape = [2, 8, 2, 5, 64]
+        shape[at] += BEYOND
+        assert of_tree(*shape) == 0
     for at in range(6):
         shape = [1, 8, 2, 100, 64, 5]
         shape[at] += BEYOND
