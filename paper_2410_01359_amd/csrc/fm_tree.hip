@@ -259,14 +259,14 @@ __global__ __launch_bounds__(kThreads, 2) void tree_kernel(FmTreeArgs a, FmDivis
       }
     l += sum;
     {
-      constexpr int RING = 3;
+      constexpr int RING = 4;
       u32x4 ring[RING], hi, lo;
       const auto fetch = [&](int i) {
         const char* rows = sh.v[buffer] + i / NDB * 16 * L::RS;
         ring[i % RING] = __builtin_bit_cast(u32x4, cat4(lds_read_tr16(rows + L::add_col(v_off[0], i % NDB * 64)), lds_read_tr16(rows + L::add_col(v_off[1], i % NDB * 64))));
       };
-#pragma unroll
-      for (int i = 0; i < RING - 1; ++i) fetch(i);
+      fetch(0);
+      fetch(1);
 #pragma unroll
       for (int i = 0; i < 4 * NDB; ++i) {
         const int n = i / NDB;   // of 16 keys
@@ -279,10 +279,14 @@ __global__ __launch_bounds__(kThreads, 2) void tree_kernel(FmTreeArgs a, FmDivis
             lo[w] = y;
           }
         }
-        if (i + RING - 1 < 4 * NDB) fetch(i + RING - 1);
-        acc[i % NDB] = mfma_rows<F16>(ring[i % RING], lo, acc[i % NDB]);
-        acc[i % NDB] = mfma_rows<F16>(ring[i % RING], hi, acc[i % NDB]);
-        __builtin_amdgcn_sched_barrier(0);
+        if (i + 2 < 4 * NDB) fetch(i + 2);
+        if (i % 2 == 1) {   // two results in turn
+          acc[i % NDB - 1] = mfma_rows<F16>(ring[(i - 1) % RING], lo, acc[i % NDB - 1]);
+          acc[i % NDB] = mfma_rows<F16>(ring[i % RING], lo, acc[i % NDB]);
+          acc[i % NDB - 1] = mfma_rows<F16>(ring[(i - 1) % RING], hi, acc[i % NDB - 1]);
+          acc[i % NDB] = mfma_rows<F16>(ring[i % RING], hi, acc[i % NDB]);
+          __builtin_amdgcn_sched_barrier(0);
+        }
       }
     }
     if constexpr (MASKED) {
@@ -442,11 +446,12 @@ FmDecodeCut fm_tree_cut(int H, int Hk, int T, int d, int B, int cus) {
   cut.row_blocks = (R + fm::kBlockRows - 1) / fm::kBlockRows;
   cut.teams = 1;
   cut.workgroups = cut.row_blocks * Hk;
-  // As attention of few rows is cut (fm_decode_cut).
+  // Chunks that give every compute unit its two workgroups once, for more sequences than that twice, as where few rows are (fm_decode_cut); two tiles
+  // at least, and partial results in 96 MiB.
   const long long at_once = std::max(1, 2 * (cus > 0 ? cus : 256) / cut.workgroups), wanted = B <= at_once ? at_once : 2 * at_once;
-  const long long bytes = (long long)Hk * R * (d + 2) * 4, room = (96ll << 20) / (2 * bytes);
-  cut.chunks = (int)std::max<long long>(1, std::min({wanted, room, 256ll}));
-  cut.least = std::max(128, 4 * R) / FM_KEY_GROUP;
+  const long long room = (96ll << 20) / ((long long)Hk * R * (d + 2) * 4), most = room / 2 < B ? room / 2 : room - B;   // see fm_most_slots
+  cut.chunks = (int)std::max<long long>(1, std::min({wanted, most, 256ll}));
+  cut.least = 2 * FM_TREE_ROUND;
   cut.slots = fm_most_slots(cut.chunks, B);
   cut.listed = (B + 63) / 64 * (long long)B * cut.workgroups > 4 * 2ll * (cus > 0 ? cus : 256);
   return cut;
