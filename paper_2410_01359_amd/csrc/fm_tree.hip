@@ -63,16 +63,6 @@ __global__ __launch_bounds__(kThreads, 2) void tree_kernel(FmTreeArgs a, FmDivis
   if (a.plan && !a.units && chunk.number == 0 && member == 0 && threadIdx.x == 0) a.plan[chunk.b] = int2{chunk.slot, chunk.of};
   const int b = __builtin_amdgcn_readfirstlane(chunk.b), first_row = __builtin_amdgcn_readfirstlane(range.len - a.T);
 
-  plant(sh.tree, a.parents + (size_t)b * a.T, a.T);
-  if (threadIdx.x < 64) {   // every depth up to the largest occurs: a token's ancestors have the smaller ones
-    int depth = 0;
-    for (int t = lane; t < a.T; t += 64) depth = max(depth, sh.tree.depth[t]);
-#pragma unroll
-    for (int k = 1; k < 64; k *= 2) depth = max(depth, __shfl_xor(depth, k));
-    if (lane == 0) sh.deepest = depth;
-  }
-  if (threadIdx.x < 6) sh.odd[threadIdx.x / 2][threadIdx.x % 2] = 0;
-
   // Queries
   const int G = a.H / a.Hk, R = G * a.T, r = rb * kBlockRows + wave * kWaveRows + c;
   const bool real = r < R;
@@ -85,9 +75,6 @@ __global__ __launch_bounds__(kThreads, 2) void tree_kernel(FmTreeArgs a, FmDivis
     for (int s = 0; s < STEPS; ++s) q[s] = ldg16(p + 2 * (16 * s + 8 * half));
   }
   const float scale = a.scale * kLog2e * (E4M3 ? a.k_scale[hk] : 1.f);
-  barrier_nofence();
-  const int row_i = first_row + sh.tree.depth[t];
-  const int rows_end = first_row + __builtin_amdgcn_readfirstlane(sh.deepest) + 1;   // rows are [first_row, rows_end)
 
   const char* k_head = a.k.base + (long long)hk * a.k.head;
   const char* v_head = a.v.base + (long long)hk * a.v.head;
@@ -180,6 +167,8 @@ __global__ __launch_bounds__(kThreads, 2) void tree_kernel(FmTreeArgs a, FmDivis
 #pragma unroll
   for (int hi = 0; hi < 2; ++hi) v_off[hi] = L::off(4 * half + ((lane & 15) >> 2) + 8 * hi, (16 * ((lane >> 4) & 1) + 4 * (lane & 3)) * 2);
 
+  // The lane's row, and where all of them are, [first_row, rows_end): for chunks that need it (plant_tree)
+  int row_i = 0, rows_end = 0;
   // Which of the lane's keys of a tile (bit 16 n + 4 q + e: key 32 n + 8 q + 4 half + e) its query sees
   const auto seen_keys = [&](int buffer, int start, int tile) {
     unsigned seen = 0;
@@ -321,11 +310,24 @@ __global__ __launch_bounds__(kThreads, 2) void tree_kernel(FmTreeArgs a, FmDivis
     }
   };
 
+  const auto plant_tree = [&] {
+    plant(sh.tree, a.parents + (size_t)b * a.T, a.T);
+    if (threadIdx.x < 64) {   // every depth up to the largest occurs: a token's ancestors have the smaller ones
+      int depth = 0;
+      for (int u = lane; u < a.T; u += 64) depth = max(depth, sh.tree.depth[u]);
+#pragma unroll
+      for (int k = 1; k < 64; k *= 2) depth = max(depth, __shfl_xor(depth, k));
+      if (lane == 0) sh.deepest = depth;
+    }
+    if (threadIdx.x < 6) sh.odd[threadIdx.x / 2][threadIdx.x % 2] = 0;
+    barrier_nofence();
+    row_i = first_row + sh.tree.depth[t];
+    rows_end = first_row + __builtin_amdgcn_readfirstlane(sh.deepest) + 1;
+  };
   // Tiles of a panel: the next one's copies are in flight while one is worked on.
   int buffer = 0, turn = 0;
   const auto run = [&](auto with_mask, int panel, unsigned long long tiles) {
     constexpr bool MASKED = decltype(with_mask)::value;
-    if (!tiles) return;
     int tile = __builtin_ctzll(tiles);
     tiles &= tiles - 1;
     load(buffer, panel, tile);
@@ -355,6 +357,7 @@ __global__ __launch_bounds__(kThreads, 2) void tree_kernel(FmTreeArgs a, FmDivis
       if (!more) break;
     }
   };
+  if (a.bounds[0] || a.window > 0) plant_tree();
   for (int panel = begin; panel < end; panel += kPanelTiles * kTile) {
     const int panel_end = min(end, panel + kPanelTiles * kTile), tiles = (panel_end - panel + kTile - 1) / kTile;
     bool hole = false;
@@ -396,22 +399,38 @@ __global__ __launch_bounds__(kThreads, 2) void tree_kernel(FmTreeArgs a, FmDivis
       live = __ballot(lane < tiles);
       partly = __ballot(hole || start + kTile > panel_end || start + kTile > first_row || (a.window > 0 && start <= rows_end - 1 - a.window));
     }
-    run(std::false_type(), panel, live & ~partly);
-    run(std::true_type(), panel, live & partly);
+    if (live & ~partly) run(std::false_type(), panel, live & ~partly);
+    if (live & partly) {
+      if (!a.bounds[0] && a.window <= 0) plant_tree();
+      run(std::true_type(), panel, live & partly);
+    }
   }
 
   // Results: a lane has elements 32 db + 8 q + 4 half + 0..3 of its row
   const float total = l + partner32(l);
-  if (!real) return;
   if (chunk.of > 1) {
-    const size_t at = ((size_t)(chunk.slot + chunk.number) * a.Hk + hk) * R + r;
+    // Rows of d floats to a wave's piece of LDS, 16-byte pieces of a row in an order that spreads them over the banks, and from there whole rows to memory
+    constexpr int ROW_PIECES = D / 4;
+    char* stage = (wave < 2 ? sh.k[wave] : sh.v[wave - 2]);
+    static_assert(kWaveRows * D * 4 <= sizeof(sh.k[0]));
+    if (!idle) {
 #pragma unroll
-    for (int db = 0; db < NDB; ++db)
+      for (int db = 0; db < NDB; ++db)
 #pragma unroll
-      for (int x = 0; x < 4; ++x)
-        *(f32x4*)(a.part + at * D + 32 * db + 8 * x + 4 * half) = f32x4{acc[db][4 * x], acc[db][4 * x + 1], acc[db][4 * x + 2], acc[db][4 * x + 3]};
-    if (half == 0) a.stat[at] = float2{m, total};
-  } else {
+        for (int x = 0; x < 4; ++x)
+          *(f32x4*)(stage + (c * ROW_PIECES + ((8 * db + 2 * x + half) ^ c % ROW_PIECES)) * 16) =
+              f32x4{acc[db][4 * x], acc[db][4 * x + 1], acc[db][4 * x + 2], acc[db][4 * x + 3]};
+      const size_t at = ((size_t)(chunk.slot + chunk.number) * a.Hk + hk) * R;
+      const int first = rb * kBlockRows + wave * kWaveRows;
+#pragma unroll
+      for (int i = 0; i < kWaveRows * ROW_PIECES / 64; ++i) {
+        const int row = (i * 64 + lane) / ROW_PIECES, piece = lane % ROW_PIECES;
+        const f32x4 x = *(const f32x4*)(stage + (row * ROW_PIECES + (piece ^ row % ROW_PIECES)) * 16);
+        if (first + row < R) *(f32x4*)(a.part + (at + first + row) * D + 4 * piece) = x;
+      }
+      if (half == 0 && real) a.stat[at + r] = float2{m, total};
+    }
+  } else if (real) {
     const int h = hk * G + hq;
     const float factor = total == 0.f ? 0.f : (E4M3 ? a.v_scale[hk] : 1.f) / total;
     char* o = (char*)a.out + 2 * ((long long)b * a.so.b + (long long)h * a.so.h + (long long)t * a.so.n);
