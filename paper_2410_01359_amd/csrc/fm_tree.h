@@ -38,7 +38,8 @@ struct Chunk {
   int len, begin, end;       // tokens of the sequence; keys
 };
 // Unit `unit` of such a cut; false: there are fewer.  groups_of(len): groups of a sequence; every wave works this out for itself, 64 sequences at a time.
-template <class Groups>
+// ONCE: up to 64 sequences in `meant` pieces at most, where pieces of up to twice the size allow that: as many as run at once.
+template <bool ONCE, class Groups>
 __device__ __forceinline__ bool find_chunk(const int* lens, int B, const FmDivisor& meant, int least, int round, int unit, const Groups& groups_of,
                                            Chunk& chunk) {
   const int lane = threadIdx.x & 63;
@@ -49,7 +50,20 @@ __device__ __forceinline__ bool find_chunk(const int* lens, int B, const FmDivis
   };
   unsigned total = 0;
   for (int base = 0; base < B; base += 64) total += wave_last(wave_scan(lane_groups(base)));
-  const int size = fm_chunk_groups(total, meant, least, round);
+  int size = fm_chunk_groups(total, meant, least, round);
+  if (ONCE && B <= 64) {
+    const int groups = lane < B ? lane_groups(0) : 0;
+    const auto pieces = [&](int size) { return wave_last(wave_scan(lane < B ? fm_chunks_of(groups, size) : 0)); };
+    if (pieces(size) > (int)meant.n && pieces(2 * size) <= (int)meant.n) {
+      int low = size, high = 2 * size;   // too many, few enough
+      while (high - low > round) {
+        const int middle = low + (high - low) / (2 * round) * round;
+        if (pieces(middle) > (int)meant.n) low = middle;
+        else high = middle;
+      }
+      size = high;
+    }
+  }
   for (int units = 0, slots = 0, base = 0; base < B; base += 64) {
     const int n = base + lane < B ? fm_chunks_of(lane_groups(base), size) : 0;
     const int upto = wave_scan(n), upto_slots = wave_scan(n > 1 ? n : 0);

@@ -51,7 +51,7 @@ __global__ __launch_bounds__(kThreads, 2) void tree_kernel(FmTreeArgs a, FmDivis
     chunk = Chunk{entry[0], entry[2] & 0xffff, entry[2] >> 16, entry[3], entry[1], 0, 0};
     if (chunk.b < 0) return;
   } else if (a.plan) {
-    if (!find_chunk(a.lens, a.B, chunks_meant, a.cut.least, ROUND, unit, [&](int n) { return fm_key_groups(range_of(n)); }, chunk)) return;
+    if (!find_chunk<true>(a.lens, a.B, chunks_meant, a.cut.least, ROUND, unit, [&](int n) { return fm_key_groups(range_of(n)); }, chunk)) return;
   } else {
     if (unit >= a.B) return;
     chunk.len = a.lens[unit];
@@ -444,6 +444,50 @@ __global__ __launch_bounds__(kThreads, 2) void tree_kernel(FmTreeArgs a, FmDivis
   }
 }
 
+// Joins the chunks of split sequences where they are few and rows many: D / 4 lanes to a row, four chunks at a time.  (join_kernel, which has a workgroup for
+// every row, takes 22 us where this takes ??.)
+template <int D, bool F16>
+__global__ __launch_bounds__(kThreads) void tree_join_kernel(FmTreeArgs a, FmDivisor rows, FmDivisor tokens) {
+  constexpr int LANES = D / 4, BATCH = 4;
+  const int G = a.H / a.Hk, R = G * a.T, b = blockIdx.y, lane = threadIdx.x % LANES, row = blockIdx.x * (kThreads / LANES) + threadIdx.x / LANES;
+  const int2 plan = a.plan[b];
+  if (plan.y <= 1 || row >= a.Hk * R) return;
+  const int hk = fm_div(row, rows), r = row - hk * R;
+  const size_t first = ((size_t)plan.x * a.Hk + hk) * R + r, step = (size_t)a.Hk * R;
+  float m = -INFINITY, l = 0.f;
+  f32x4 x = {0.f, 0.f, 0.f, 0.f};
+  for (int base = 0; base < plan.y; base += BATCH) {
+    f32x4 v[BATCH];
+    float2 s[BATCH];
+#pragma unroll
+    for (int i = 0; i < BATCH; ++i) {
+      const size_t at = first + std::min(base + i, plan.y - 1) * step;
+      s[i] = a.stat[at];
+      v[i] = *(const f32x4*)(a.part + at * D + 4 * lane);
+      if (base + i >= plan.y) s[i] = float2{-INFINITY, 0.f};
+    }
+    float top = m;
+#pragma unroll
+    for (int i = 0; i < BATCH; ++i) top = fmaxf(top, s[i].x);
+    const float alpha = fast_exp2(m - reference(top));
+    m = top;
+    l *= alpha;
+    x *= alpha;
+#pragma unroll
+    for (int i = 0; i < BATCH; ++i) {
+      if (base + i >= plan.y) continue;
+      const float w = fast_exp2(s[i].x - reference(top));
+      l += w * s[i].y;
+      x += w * v[i];
+    }
+  }
+  const int hq = fm_div(r, tokens), t = r - hq * a.T, h = hk * G + hq;
+  const float factor = l == 0.f ? 0.f : (a.v_scale ? a.v_scale[hk] : 1.f) / l;
+  char* o = (char*)a.out + 2 * ((long long)b * a.so.b + (long long)h * a.so.h + (long long)t * a.so.n + 4 * lane);
+  *(u32x2*)o = u32x2{pack2<F16>(x[0] * factor, x[1] * factor), pack2<F16>(x[2] * factor, x[3] * factor)};
+  if (lane == 0) a.lse[((size_t)b * a.H + h) * a.T + t] = l == 0.f ? -INFINITY : (m + fast_log2(l * kUnshift<F16>)) * kLn2;
+}
+
 template <int D, bool F16, bool E4M3>
 static void launch(FmTreeArgs a, hipStream_t stream) {
   constexpr int kMost = 1 << 23;   // workgroups of a launch, which has fewer than 2^32 lanes
@@ -453,7 +497,12 @@ static void launch(FmTreeArgs a, hipStream_t stream) {
   for (a.first_workgroup = 0; a.first_workgroup < workgroups; a.first_workgroup += kMost)
     hipLaunchKernelGGL((tree_kernel<D, F16, E4M3>), dim3((unsigned)std::min(workgroups - a.first_workgroup, kMost)), dim3(kThreads), 0, stream, a,
                        fm_divisor(cut.workgroups), fm_divisor(cut.row_blocks), fm_divisor(a.T), fm_divisor(cut.chunks));
-  if (a.plan) fm_launch_decode_join(a, F16, stream);
+  if (a.plan && cut.chunks <= 32 && !a.split) {
+    const int R = a.H / a.Hk * a.T, each = kThreads / (D / 4);
+    hipLaunchKernelGGL((tree_join_kernel<D, F16>), dim3((a.Hk * R + each - 1) / each, a.B), dim3(kThreads), 0, stream, a, fm_divisor(R), fm_divisor(a.T));
+  } else if (a.plan) {
+    fm_launch_decode_join(a, F16, stream);
+  }
 }
 
 }  // namespace fm

@@ -290,7 +290,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache_weights_kernel(FmCacheWe
   if (a.dealt) {
     const auto groups_of = [&](int n) { return (min(max(n, 0), a.places) + FM_KEY_GROUP - 1) / FM_KEY_GROUP; };
     Chunk chunk;
-    if (!find_chunk(a.lens, a.B, a.chunks, kWaves * kGroups, kWaves * kGroups, unit, groups_of, chunk)) return;
+    if (!find_chunk<false>(a.lens, a.B, a.chunks, kWaves * kGroups, kWaves * kGroups, unit, groups_of, chunk)) return;
     b = chunk.b;
     len = chunk.len;
     const int keys = fm_even_chunk(groups_of(len), chunk.of, kGroups) * FM_KEY_GROUP;
