@@ -169,24 +169,42 @@ __global__ __launch_bounds__(kThreads, 2) void tree_kernel(FmTreeArgs a, FmDivis
 
   // The lane's row, and where all of them are, [first_row, rows_end): for chunks that need it (plant_tree)
   int row_i = 0, rows_end = 0;
-  // Which of the lane's keys of a tile (bit 16 n + 4 q + e: key 32 n + 8 q + 4 half + e) its query sees
+  // Which of the lane's keys of a tile (bit 16 n + 4 q + e: key 32 n + 8 q + 4 half + e) its query sees.  Drafted tokens lie in the order of the bits that
+  // their tree has of them: a tile's 64 are a shift of three words, ahead of them everything is seen.
   const auto seen_keys = [&](int buffer, int start, int tile) {
-    unsigned seen = 0;
-    if (!real || first_row + t < 0) return seen;
-#pragma unroll 1
-    for (int n = 0; n < 8; ++n) {
+    if (!real || first_row + t < 0) return 0u;
+    const int ahead = first_row - start, left = end - start;   // keys that are not drafted ones, and keys
+    const int word = -ahead >> 5, shift = -ahead & 31;
+    unsigned x[3];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int key = 8 * n + 4 * half + e, j = start + key, u = j - first_row;
-        bool sees = j < end;
-        if (u < 0) {
-          sees &= a.window <= 0 || j > row_i - a.window;
-        } else {
-          const int at = min(u, a.T - 1);
-          sees &= sh.tree.on_path(t, at) && (a.window <= 0 || sh.tree.depth[t] - sh.tree.depth[at] < a.window);
+    for (int w = 0; w < 3; ++w) {
+      const int at = word + w;
+      x[w] = at >= 0 && at < FM_MOST_NEW_TOKENS / 32 ? sh.tree.ancestors[t][at] : 0u;
+    }
+    unsigned long long keys = (unsigned long long)__builtin_amdgcn_alignbit(x[2], x[1], shift) << 32 | __builtin_amdgcn_alignbit(x[1], x[0], shift);
+    const auto below = [](int n) { return n >= 64 ? ~0ull : n <= 0 ? 0ull : (1ull << n) - 1ull; };
+    unsigned long long prefix = below(ahead);
+    if (a.window > 0) prefix &= ~below(row_i - a.window + 1 - start);
+    keys = (keys | prefix) & below(left);
+    // nibbles of this half, of each 32
+    unsigned seen = 0;
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+      unsigned y = (unsigned)(keys >> (32 * n + 4 * half)) & 0x0f0f0f0fu;
+      y = (y | y >> 4) & 0x00ff00ffu;
+      seen |= ((y | y >> 8) & 0xffffu) << (16 * n);
+    }
+    // bounds, and windows that end inside the tree
+    if (a.bounds[0] || (a.window > 0 && first_row + a.window < rows_end)) {
+#pragma unroll 1
+      for (int n = 0; n < 8; ++n) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int key = 8 * n + 4 * half + e, u = start + key - first_row, at = min(max(u, 0), a.T - 1);
+          bool sees = a.window <= 0 || u < 0 || sh.tree.depth[t] - sh.tree.depth[at] < a.window;
+          if (a.bounds[0]) sees &= !hides(sh.bound[key], row_i);
+          if (!sees) seen &= ~(1u << (4 * n + e));
         }
-        if (a.bounds[0]) sees &= !hides(sh.bound[key], row_i);
-        seen |= (sees ? 1u : 0u) << (4 * n + e);
       }
     }
     // keys without a page: their values are 0, and so are their scores
