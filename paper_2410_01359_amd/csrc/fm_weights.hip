@@ -46,7 +46,7 @@ __device__ __forceinline__ int half_min(int x) {
 template <int D>
 __global__ __launch_bounds__(256, 2) void weights_kernel(FmWeightsArgs a) {
   using L = TileLayout<D>;
-  constexpr int STEPS = D / 16, PIECES = D / 8, LOADS = kTile * PIECES / 256;
+  constexpr int STEPS = D / 16;
   __shared__ WeightsShared<D> sh;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = lane & 31, half = lane >> 5;
@@ -64,7 +64,7 @@ __global__ __launch_bounds__(256, 2) void weights_kernel(FmWeightsArgs a) {
   for (int n = 0; n < 2; ++n) {
     const int key = min(key0 + 32 * n + c, a.N - 1);   // a lane past the last key works on a copy of it
 #pragma unroll
-    for (int w = 0; w < 4; ++w) bound[n][w] = a.bounds[w][(size_t)b * a.N + key];
+    for (int w = 0; w < 4; ++w) bound[n][w] = min(max(a.bounds[w][(size_t)b * a.N + key], 0), a.N);
 #pragma unroll
     for (int s = 0; s < STEPS; ++s) k[n][s] = __builtin_bit_cast(bf16x8, ldg16(k_rows + 2 * (key * a.sk.n + 16 * s + 8 * half)));
   }
@@ -86,16 +86,15 @@ __global__ __launch_bounds__(256, 2) void weights_kernel(FmWeightsArgs a) {
     for (int i = 1; i < 4; ++i) x = w % 2 ? min(x, sh.minmax[i][w]) : max(x, sh.minmax[i][w]);
     all.v[w] = x;
   }
-  u32x4 staged[LOADS];
+  CopyLanes<D> lanes;
+  lanes.init(lane, 2 * (int)a.sq.n);
   float staged_lse = 0.f;
-  const auto load = [&](int h, int first) {
+  // To LDS, by each wave 16 rows; a tile's rows past the last are copies of it.  (Through registers: ??.)
+  const auto load = [&](int h, int first, int buffer) {
     const char* rows = (const char*)a.q + 2 * ((long long)b * a.sq.b + (long long)(hk * G + h) * a.sq.h);
-#pragma unroll
-    for (int i = 0; i < LOADS; ++i) {
-      const int piece = i * 256 + threadIdx.x, row = min(first + piece / PIECES, a.N - 1);
-      staged[i] = ldg16(rows + 2 * ((long long)row * a.sq.n + piece % PIECES * 8));
-    }
-    if (threadIdx.x < kTile) staged_lse = a.lse[((size_t)b * a.H + hk * G + h) * a.N + min(first + (int)threadIdx.x, a.N - 1)];
+    if (wave == 0) staged_lse = a.lse[((size_t)b * a.H + hk * G + h) * a.N + min(first + lane, a.N - 1)];
+    if (first + kTile <= a.N) tile_load_async<D>(CopyLanes<D>::wave_base(rows, wave, 2 * (int)a.sq.n) + 2 * first * a.sq.n, lanes, sh.q[buffer], wave);
+    else tile_load_async_clamped<D>((const __bf16*)rows, first, a.N, sh.q[buffer], wave, lane, 2 * (int)a.sq.n);
   };
 
   const float scale = a.scale * kLog2e;
@@ -143,7 +142,7 @@ __global__ __launch_bounds__(256, 2) void weights_kernel(FmWeightsArgs a) {
   };
   constexpr std::true_type with_old;
   constexpr std::false_type alone;
-  // The same exponentials by themselves; hides(n, r): rows r that do not see key n.
+  // The same exponentials by themselves; hides(x, n, q) puts -inf where rows 8 q + 4 half + (0..3) do not see key n.
   const auto add = [&](const f32x16 (&s)[2], const float* lses, const auto& hides) {
     float tile[2] = {0.f, 0.f};
 #pragma unroll
@@ -154,7 +153,7 @@ __global__ __launch_bounds__(256, 2) void weights_kernel(FmWeightsArgs a) {
         f32x4 x;
 #pragma unroll
         for (int r = 0; r < 4; ++r) x[r] = fmaf(s[n][4 * q + r], scale, lse[r]);
-        hides(x, n, 8 * q + 4 * half);
+        hides(x, n, q);
 #pragma unroll
         for (int r = 0; r < 4; ++r) tile[n] += fast_exp2(x[r]);
       }
@@ -194,16 +193,13 @@ __global__ __launch_bounds__(256, 2) void weights_kernel(FmWeightsArgs a) {
     const long long first = items * part / a.parts;
     int h = (int)(first / listed), at = (int)(first - (long long)h * listed);
     int entry = __builtin_amdgcn_readfirstlane(sh.list[at]);
-    load(h, panel_row + (entry & 0xffff) * kTile);
+    load(h, panel_row + (entry & 0xffff) * kTile, buffer);
     for (; left > 0; --left) {
       const char* rows = sh.q[buffer];
       float* lses = sh.lse[turn];
-#pragma unroll
-      for (int i = 0; i < LOADS; ++i) {
-        const int piece = i * 256 + threadIdx.x;
-        *(u32x4*)(sh.q[buffer] + L::off(piece / PIECES, piece % PIECES * 16)) = staged[i];
-      }
-      if (threadIdx.x < kTile) lses[threadIdx.x] = minus_lse(staged_lse);
+      if (wave == 0) lses[lane] = minus_lse(staged_lse);
+      async_wait<0>();
+      barrier_nofence();   // the tile is there, and the one before has been read
       const int row = panel_row + (entry & 0xffff) * kTile, cls = entry >> (16 + 2 * wave) & 3;
       if (left > 1) {
         if (++at == listed) {
@@ -211,11 +207,10 @@ __global__ __launch_bounds__(256, 2) void weights_kernel(FmWeightsArgs a) {
           ++h;
         }
         entry = __builtin_amdgcn_readfirstlane(sh.list[at]);
-        load(h, panel_row + (entry & 0xffff) * kTile);
+        load(h, panel_row + (entry & 0xffff) * kTile, buffer ^ 1);
       }
       buffer ^= 1;
       turn = turn == 2 ? 0 : turn + 1;
-      barrier_nofence();   // the next tile's loads stay in flight
 
       if (cls == T_FULLY) {   // what waits does not wait longer than a tile
         if (waiting) add(lower, waiting, none);
@@ -229,12 +224,25 @@ __global__ __launch_bounds__(256, 2) void weights_kernel(FmWeightsArgs a) {
         waiting = lses + 32;
         continue;
       }
+      // The tile's rows that do not see a key are bits, spread over the elements with a bit-field extract each.  (With comparisons at every
+      // element a masked tile takes 1000 instructions instead of ???.)
+      unsigned hidden[2][2];
+#pragma unroll
+      for (int n = 0; n < 2; ++n) {
+        const auto below = [&](int i) { return i - row >= 64 ? ~0ull : i <= row ? 0ull : (1ull << (i - row)) - 1; };
+        const unsigned long long x =
+            (below(bound[n][1]) & ~below(bound[n][0])) | (below(bound[n][3]) & ~below(bound[n][2])) | ~below(a.N);
+        hidden[0][n] = (unsigned)x >> 4 * half;
+        hidden[1][n] = (unsigned)(x >> 32) >> 4 * half;
+      }
       const auto masked = [&](int m) {
-        return [&, m](f32x4& x, int n, int r0) {
-          hide4(x, 0, [&](int r) {
-            const int i = row + 32 * m + r0 + r;
-            return (i >= a.N) | ((bound[n][0] <= i) & (i < bound[n][1])) | ((bound[n][2] <= i) & (i < bound[n][3]));
-          });
+        return [&, m](f32x4& x, int n, int q) {
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            int hide = __builtin_amdgcn_sbfe(hidden[m][n], 8 * q + r, 1);
+            settle(hide);   // no comparison
+            x[r] = __int_as_float((__float_as_int(x[r]) & ~hide) | (hide & 0xff800000));
+          }
         };
       };
       add(upper, lses, masked(0));
