@@ -125,12 +125,19 @@ __global__ __launch_bounds__(256, 2) void weights_kernel(FmWeightsArgs a) {
       if constexpr (OLD) {
 #pragma unroll
         for (int e = 0; e < EACH; ++e) {
-          if (i > 1) tile[e % 2] += x[i % 2][e];
+          if (i > 1) {
+            tile[e % 2] += x[i % 2][e];
+            settle(tile[e % 2]);
+          }
           if (i < 2 * STEPS) {
             const int at = i * EACH + e, row = at / 2;
             x[i % 2][e] = fmaf(old[at % 2][row], scale, lse[row / 4][row % 4]);
+            settle(x[i % 2][e]);
           }
-          if (i > 0 && i < 2 * STEPS + 1) x[(i - 1) % 2][e] = fast_exp2(x[(i - 1) % 2][e]);
+          if (i > 0 && i < 2 * STEPS + 1) {
+            x[(i - 1) % 2][e] = fast_exp2(x[(i - 1) % 2][e]);
+            settle(x[(i - 1) % 2][e]);
+          }
         }
       }
       __builtin_amdgcn_sched_barrier(0);
