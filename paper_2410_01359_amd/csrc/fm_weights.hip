@@ -25,8 +25,8 @@ constexpr int kKeys = 256, kTile = 64, kPanel = 2048;   // kPanel: row tiles tha
 
 template <int D>
 struct WeightsShared {
-  alignas(16) char q[2][kTile * TileLayout<D>::RS];
-  alignas(16) float lse[3][kTile];   // one more: a wave may still be at the rows before the last
+  alignas(16) char q[3][kTile * TileLayout<D>::RS];
+  alignas(16) float lse[4][4][kTile];   // each wave's own; one more: a wave has use for the rows before
   int minmax[4][8];
   int list[kPanel], wave_count[4];   // row tiles that some key of the workgroup's sees: tile | class for wave w << (16 + 2 w)
 };
@@ -88,13 +88,13 @@ __global__ __launch_bounds__(256, 2) void weights_kernel(FmWeightsArgs a) {
   }
   CopyLanes<D> lanes;
   lanes.init(lane, 2 * (int)a.sq.n);
-  float staged_lse = 0.f;
-  // To LDS, by each wave 16 rows; a tile's rows past the last are copies of it.  (Through registers: ??.)
-  const auto load = [&](int h, int first, int buffer) {
+  // To LDS, by each wave 16 rows, and every row's lse for itself; a tile's rows past the last are copies of it.
+  constexpr int COPIES = CopyLanes<D>::NINST + 1;
+  const auto load = [&](int h, int first, int slot, int turn) {
     const char* rows = (const char*)a.q + 2 * ((long long)b * a.sq.b + (long long)(hk * G + h) * a.sq.h);
-    if (wave == 0) staged_lse = a.lse[((size_t)b * a.H + hk * G + h) * a.N + min(first + lane, a.N - 1)];
-    if (first + kTile <= a.N) tile_load_async<D>(CopyLanes<D>::wave_base(rows, wave, 2 * (int)a.sq.n) + 2 * first * a.sq.n, lanes, sh.q[buffer], wave);
-    else tile_load_async_clamped<D>((const __bf16*)rows, first, a.N, sh.q[buffer], wave, lane, 2 * (int)a.sq.n);
+    async_copy4(a.lse + ((size_t)b * a.H + hk * G + h) * a.N + min(first + lane, a.N - 1), lds_address(sh.lse[wave][turn]));
+    if (first + kTile <= a.N) tile_load_async<D>(CopyLanes<D>::wave_base(rows, wave, 2 * (int)a.sq.n) + 2 * first * a.sq.n, lanes, sh.q[slot], wave);
+    else tile_load_async_clamped<D>((const __bf16*)rows, first, a.N, sh.q[slot], wave, lane, 2 * (int)a.sq.n);
   };
 
   const float scale = a.scale * kLog2e;
@@ -172,7 +172,7 @@ __global__ __launch_bounds__(256, 2) void weights_kernel(FmWeightsArgs a) {
 
   f32x16 upper[2], lower[2];   // scores of a tile's halves; those of `lower` wait for the next products
   const float* waiting = nullptr;   // their rows' lse
-  int buffer = 0, turn = 0;
+  int slot = 0, turn = 0;   // of the tile at hand
   for (int panel = 0; panel < a.row_tiles; panel += kPanel) {
     const int panel_row = a.first_row + panel * kTile, tiles = min(kPanel, a.row_tiles - panel);
     int listed = 0;
@@ -199,25 +199,41 @@ __global__ __launch_bounds__(256, 2) void weights_kernel(FmWeightsArgs a) {
     if (left == 0) continue;
     const long long first = items * part / a.parts;
     int h = (int)(first / listed), at = (int)(first - (long long)h * listed);
-    int entry = __builtin_amdgcn_readfirstlane(sh.list[at]);
-    load(h, panel_row + (entry & 0xffff) * kTile, buffer);
-    for (; left > 0; --left) {
-      const char* rows = sh.q[buffer];
-      float* lses = sh.lse[turn];
-      if (wave == 0) lses[lane] = minus_lse(staged_lse);
-      async_wait<0>();
-      barrier_nofence();   // the tile is there, and the one before has been read
-      const int row = panel_row + (entry & 0xffff) * kTile, cls = entry >> (16 + 2 * wave) & 3;
-      if (left > 1) {
-        if (++at == listed) {
-          at = 0;
-          ++h;
-        }
-        entry = __builtin_amdgcn_readfirstlane(sh.list[at]);
-        load(h, panel_row + (entry & 0xffff) * kTile, buffer ^ 1);
+    // What comes from outside asynchronous copies has to be there before the loop: a wait for it in there would be one for the copies, too.
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+      settle(bound[n]);
+#pragma unroll
+      for (int s = 0; s < STEPS; ++s) settle(k[n][s]);
+    }
+    // Copies run two tiles ahead: ahead[0] is the tile at hand, ahead[1] the next.
+    int ahead[2];
+    const auto begin = [&](int entry, int far) {
+      load(h, panel_row + (entry & 0xffff) * kTile, slot + far - (slot + far > 2 ? 3 : 0), (turn + far) & 3);
+      if (++at == listed) {
+        at = 0;
+        ++h;
       }
-      buffer ^= 1;
-      turn = turn == 2 ? 0 : turn + 1;
+      return entry;
+    };
+    ahead[0] = begin(__builtin_amdgcn_readfirstlane(sh.list[at]), 0);
+    ahead[1] = left > 1 ? begin(__builtin_amdgcn_readfirstlane(sh.list[at]), 1) : 0;
+    int listed_next = sh.list[at];
+    for (; left > 0; --left) {
+      const char* rows = sh.q[slot];
+      float* lses = sh.lse[wave][turn];
+      if (left > 1) async_wait<COPIES>();
+      else async_wait<0>();
+      barrier_nofence();   // the tile is there, and the one before has been read
+      lses[lane] = minus_lse(lses[lane]);
+      const int row = panel_row + (ahead[0] & 0xffff) * kTile, cls = ahead[0] >> (16 + 2 * wave) & 3;
+      ahead[0] = ahead[1];
+      if (left > 2) {
+        ahead[1] = begin(__builtin_amdgcn_readfirstlane(listed_next), 2);
+        listed_next = sh.list[at];
+      }
+      slot = slot == 2 ? 0 : slot + 1;
+      turn = (turn + 1) & 3;
 
       if (cls == T_FULLY) {   // what waits does not wait longer than a tile
         if (waiting) add(lower, waiting, none);
