@@ -90,11 +90,15 @@ __global__ __launch_bounds__(256, 2) void weights_kernel(FmWeightsArgs a) {
   lanes.init(lane, 2 * (int)a.sq.n);
   // To LDS, by each wave 16 rows, and every row's lse for itself; a tile's rows past the last are copies of it.
   constexpr int COPIES = CopyLanes<D>::NINST + 1;
-  const auto load = [&](int h, int first, int slot, int turn) {
-    const char* rows = (const char*)a.q + 2 * ((long long)b * a.sq.b + (long long)(hk * G + h) * a.sq.h);
-    async_copy4(a.lse + ((size_t)b * a.H + hk * G + h) * a.N + min(first + lane, a.N - 1), lds_address(sh.lse[wave][turn]));
-    if (first + kTile <= a.N) tile_load_async<D>(CopyLanes<D>::wave_base(rows, wave, 2 * (int)a.sq.n) + 2 * first * a.sq.n, lanes, sh.q[slot], wave);
-    else tile_load_async_clamped<D>((const __bf16*)rows, first, a.N, sh.q[slot], wave, lane, 2 * (int)a.sq.n);
+  const int row_bytes = 2 * (int)a.sq.n;
+  const auto load = [&](const char* rows, const float* lse, int tile, int last, int slot, int turn) {
+    async_copy4(lse + min(tile * kTile + lane, last), lds_address(sh.lse[wave][turn]));
+    if (tile * kTile + kTile - 1 <= last) {
+      const char* source = CopyLanes<D>::wave_base(rows, wave, row_bytes) + (unsigned long long)(unsigned)tile * (unsigned)(kTile * row_bytes);
+      tile_load_async<D>(source, lanes, sh.q[slot], wave);
+    } else {
+      tile_load_async_clamped<D>((const __bf16*)rows, tile * kTile, last + 1, sh.q[slot], wave, lane, row_bytes);
+    }
   };
 
   const float scale = a.scale * kLog2e;
@@ -194,11 +198,14 @@ __global__ __launch_bounds__(256, 2) void weights_kernel(FmWeightsArgs a) {
       append_live(live, entry, sh.list, sh.wave_count, listed);
     }
     // this part's share of the heads' tiles
-    const long long items = (long long)G * listed;
-    int left = (int)(items * (part + 1) / a.parts - items * part / a.parts);
+    const int items = G * listed, each = fm_div(items, a.by_part), more = items - each * a.parts;
+    int left = each + (part < more);
     if (left == 0) continue;
-    const long long first = items * part / a.parts;
-    int h = (int)(first / listed), at = (int)(first - (long long)h * listed);
+    const int first = part * each + min(part, more);
+    const int h = first / listed;
+    int at = first - h * listed;
+    const char* head_rows = (const char*)a.q + 2 * ((long long)b * a.sq.b + (long long)(hk * G + h) * a.sq.h + panel_row * a.sq.n);
+    const float* head_lse = a.lse + ((size_t)b * a.H + hk * G + h) * a.N + panel_row;
     // What comes from outside asynchronous copies has to be there before the loop: a wait for it in there would be one for the copies, too.
 #pragma unroll
     for (int n = 0; n < 2; ++n) {
@@ -209,10 +216,11 @@ __global__ __launch_bounds__(256, 2) void weights_kernel(FmWeightsArgs a) {
     // Copies run two tiles ahead: ahead[0] is the tile at hand, ahead[1] the next.
     int ahead[2];
     const auto begin = [&](int entry, int far) {
-      load(h, panel_row + (entry & 0xffff) * kTile, slot + far - (slot + far > 2 ? 3 : 0), (turn + far) & 3);
+      load(head_rows, head_lse, entry & 0xffff, a.N - 1 - panel_row, slot + far - (slot + far > 2 ? 3 : 0), (turn + far) & 3);
       if (++at == listed) {
         at = 0;
-        ++h;
+        head_rows += 2 * a.sq.h;
+        head_lse += a.N;
       }
       return entry;
     };
