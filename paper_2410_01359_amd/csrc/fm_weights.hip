@@ -256,7 +256,7 @@ __global__ __launch_bounds__(256, 2) void weights_kernel(FmWeightsArgs a) {
         continue;
       }
       // The tile's rows that do not see a key are bits, spread over the elements with a bit-field extract each.  (With comparisons at every
-      // element a masked tile takes 1000 instructions instead of ???.)
+      // element a masked tile takes 1000 instructions instead of 550.)
       unsigned hidden[2][2];
 #pragma unroll
       for (int n = 0; n < 2; ++n) {
@@ -313,6 +313,7 @@ struct CacheWeightsShared {
   int flag[kSteps];
   alignas(16) char q[ONE ? 16 : kRows * TileLayout<D>::RS];
   alignas(16) float lse[ONE ? 4 : kRows];
+  alignas(4) unsigned char token[ONE ? 4 : kRows];   // which of the T a row is
 };
 
 // ONE: the rows of a K/V head are 16 at most.
@@ -375,6 +376,11 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache_weights_kernel(FmCacheWe
 #pragma unroll
     for (int r = 0; r < 4; ++r) lse[r] = lse_of(4 * g + r);
   }
+  // Which of the T a row is; of one past the last, what the last one is.
+  const auto token_of = [&](int r) {
+    const int at = min(r, R - 1);
+    return at - fm_div(at, a.tokens) * a.T;
+  };
 
   const char* k_head = a.k.base + (long long)hk * a.k.head;
   u32x4 kraw[kGroups][LOADS];
@@ -407,7 +413,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache_weights_kernel(FmCacheWe
         const int from = E4M3 ? 8 * (to / 8) + 2 * (to % 4) + to / 4 % 2 : to;
         *(u32x4*)(sh.q + L::off(r, 16 * to)) = ldg16(query(min(row0 + r, R - 1)) + 16 * from);
       }
-      if ((int)threadIdx.x < blocks * 16) sh.lse[threadIdx.x] = lse_of(row0 + threadIdx.x);
+      if ((int)threadIdx.x < blocks * 16) {
+        sh.lse[threadIdx.x] = lse_of(row0 + threadIdx.x);
+        sh.token[threadIdx.x] = (unsigned char)token_of(row0 + threadIdx.x);
+      }
       __syncthreads();
     }
     for (int panel = begin; panel < end; panel += kSteps * kStep) {
@@ -465,7 +474,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache_weights_kernel(FmCacheWe
           load_keys(panel + step * kStep);
         }
         float sum[kGroups] = {};
-        const auto block = [&](int r0, const u32x4 (&q)[STEPS], const f32x4& lse, const auto& mask) {
+        const auto block = [&](const u32x4 (&q)[STEPS], const f32x4& lse, const int (&token)[4], const auto& mask) {
           f32x4 score[kGroups];
 #pragma unroll
           for (int i = 0; i < kGroups; ++i) score[i] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -478,7 +487,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache_weights_kernel(FmCacheWe
             f32x4 x;
 #pragma unroll
             for (int r = 0; r < 4; ++r) x[r] = fmaf(score[i][r], scale, lse[r]);
-            mask(x, i, r0);
+            mask(x, i, token);
 #pragma unroll
             for (int r = 0; r < 4; ++r) x[r] = fast_exp2(x[r]);
             sum[i] += (x[0] + x[1]) + (x[2] + x[3]);
@@ -486,13 +495,14 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache_weights_kernel(FmCacheWe
         };
         const auto all_blocks = [&](const auto& mask) {
           if constexpr (ONE) {
-            block(0, q, lse, mask);
+            block(q, lse, {token_of(4 * g), token_of(4 * g + 1), token_of(4 * g + 2), token_of(4 * g + 3)}, mask);
           } else {
             for (int n = 0; n < blocks; ++n) {
               u32x4 rows[STEPS];
 #pragma unroll
               for (int s = 0; s < STEPS; ++s) rows[s] = *(const u32x4*)(sh.q + L::off(c, 16 * g) + n * 16 * L::RS + s * 1024);
-              block(row0 + n * 16, rows, *(const f32x4*)&sh.lse[n * 16 + 4 * g], mask);
+              const unsigned token = *(const unsigned*)&sh.token[n * 16 + 4 * g];
+              block(rows, *(const f32x4*)&sh.lse[n * 16 + 4 * g], {(int)(token & 255), (int)(token >> 8 & 255), (int)(token >> 16 & 255), (int)(token >> 24)}, mask);
             }
           }
         };
@@ -507,16 +517,41 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache_weights_kernel(FmCacheWe
             key[i] = at;
             behind[i] = real ? rows_end(at) : 0;
           }
-          all_blocks([&](f32x4& x, int i, int r0) {
+          if (ONE || a.T <= 64) {
+            // The tokens that do not see a key are bits, one extracted for each element.  (With comparisons at every element 16 rows of
+            // a masked step take 320 instructions instead of 150, the last rows of four prompts 29 us instead of 20.)
+            unsigned hidden[kGroups][2];
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-              const int at = min(r0 + 4 * g + r, R - 1), row = first_row + at - fm_div(at, a.tokens) * a.T;
-              const bool gone = (row < key[i]) | (row >= behind[i]) | ((bound[i][0] <= row) & (row < bound[i][1])) | ((bound[i][2] <= row) & (row < bound[i][3]));
-              x[r] = gone ? -INFINITY : x[r];
+            for (int i = 0; i < kGroups; ++i) {
+              const auto below = [&](int row) {
+                const int n = min(max(row, 0), 1 << 30) - first_row;
+                return n >= 64 ? ~0ull : n <= 0 ? 0ull : (1ull << n) - 1;
+              };
+              const unsigned long long x = ~below(behind[i]) | below(key[i]) | (below(bound[i][1]) & ~below(bound[i][0])) |
+                                           (below(bound[i][3]) & ~below(bound[i][2]));
+              hidden[i][0] = (unsigned)x;
+              hidden[i][1] = (unsigned)(x >> 32);
             }
-          });
+            all_blocks([&](f32x4& x, int i, const int (&token)[4]) {
+#pragma unroll
+              for (int r = 0; r < 4; ++r) {
+                int hide = __builtin_amdgcn_sbfe(ONE || token[r] < 32 ? hidden[i][0] : hidden[i][1], token[r] & 31, 1);
+                settle(hide);   // no comparison
+                x[r] = __int_as_float((__float_as_int(x[r]) & ~hide) | (hide & 0xff800000));
+              }
+            });
+          } else if constexpr (!ONE) {
+            all_blocks([&](f32x4& x, int i, const int (&token)[4]) {
+#pragma unroll
+              for (int r = 0; r < 4; ++r) {
+                const int row = first_row + token[r];
+                const bool gone = (row < key[i]) | (row >= behind[i]) | ((bound[i][0] <= row) & (row < bound[i][1])) | ((bound[i][2] <= row) & (row < bound[i][3]));
+                x[r] = gone ? -INFINITY : x[r];
+              }
+            });
+          }
         } else {
-          all_blocks([](f32x4&, int, int) {});
+          all_blocks([](f32x4&, int, const int (&)[4]) {});
         }
         float mine = 0.f;
 #pragma unroll
