@@ -313,6 +313,7 @@ struct CacheWeightsShared {
   int flag[kSteps];
   alignas(16) char q[ONE ? 16 : kRows * TileLayout<D>::RS];
   alignas(16) float lse[ONE ? 4 : kRows];
+  float part[ONE ? 1 : kWaves][ONE ? 1 : kStep];   // sums of waves that share a step
   alignas(4) unsigned char token[ONE ? 4 : kRows];   // which of the T a row is
 };
 
@@ -330,7 +331,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache_weights_kernel(FmCacheWe
   if (a.dealt) {
     const auto groups_of = [&](int n) { return (min(max(n, 0), a.places) + FM_KEY_GROUP - 1) / FM_KEY_GROUP; };
     Chunk chunk;
-    if (!find_chunk<false>(a.lens, a.B, a.chunks, kWaves * kGroups, kWaves * kGroups, unit, groups_of, chunk)) return;
+    constexpr int least = ONE ? kWaves * kGroups : kGroups;
+    if (!find_chunk<false>(a.lens, a.B, a.chunks, least, least, unit, groups_of, chunk)) return;
     b = chunk.b;
     len = chunk.len;
     const int keys = fm_even_chunk(groups_of(len), chunk.of, kGroups) * FM_KEY_GROUP;
@@ -445,8 +447,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache_weights_kernel(FmCacheWe
           const int s = __builtin_ctzll(none), j = panel + s * kStep + lane;
           if (s % kWaves == wave && j < panel_end) a.weights[row_of_weights + j] = old(j);
         }
-      // the wave takes every fourth of the others
-      for (int i = 0; i < wave; ++i) left &= left - 1;
+      // The wave takes every fourth of the others; where they are one or two, waves share one, each with some of the rows (32 new tokens of one
+      // sequence of 2000 keys 12.8 -> 9.5 us).
+      const int live = __popcll(left), share = ONE || live > 2 ? 1 : live == 2 ? 2 : 4, sharer = wave % share;
+      for (int i = 0; i < wave / share; ++i) left &= left - 1;
       if (!left) continue;
       int step = __builtin_ctzll(left);
       load_keys(panel + step * kStep);
@@ -468,7 +472,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache_weights_kernel(FmCacheWe
             }
           }
         const float before = j >= panel_end ? 0.f : row0 == 0 ? old(j) : a.weights[row_of_weights + j];
-        for (int i = 0; i < kWaves; ++i) left &= left - 1;
+        for (int i = 0; i < kWaves / share; ++i) left &= left - 1;
         if (left) {
           step = __builtin_ctzll(left);
           load_keys(panel + step * kStep);
@@ -497,7 +501,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache_weights_kernel(FmCacheWe
           if constexpr (ONE) {
             block(q, lse, {token_of(4 * g), token_of(4 * g + 1), token_of(4 * g + 2), token_of(4 * g + 3)}, mask);
           } else {
-            for (int n = 0; n < blocks; ++n) {
+            for (int n = blocks * sharer / share; n < blocks * (sharer + 1) / share; ++n) {
               u32x4 rows[STEPS];
 #pragma unroll
               for (int s = 0; s < STEPS; ++s) rows[s] = *(const u32x4*)(sh.q + L::off(c, 16 * g) + n * 16 * L::RS + s * 1024);
@@ -559,6 +563,15 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache_weights_kernel(FmCacheWe
           const float x = quad_sum(sum[i]);
           if (i == g) mine = x;
         }
+        if constexpr (!ONE) {
+          if (share > 1) {   // all waves come here, once in a panel
+            __syncthreads();   // the sums of the panel before have been read
+            sh.part[wave][lane] = mine;
+            __syncthreads();
+            if (sharer != 0) break;
+            for (int p = 1; p < share; ++p) mine += sh.part[wave + p][lane];
+          }
+        }
         if (j < panel_end) a.weights[row_of_weights + j] = before + mine;
       }
     }
@@ -606,9 +619,11 @@ bool fm_cut_cache_weights(FmCacheWeightsArgs& a, int cus) {
   // Every workgroup goes over all lengths, 64 at a time and about 1 us each; more sequences fill the chip by themselves.
   a.dealt = a.B <= 512;
   a.chunk_keys = std::min(a.places, 8192);
-  // Four rounds of the two workgroups that a compute unit holds: there is nothing to join, and 64 ragged sequences take 82 us, with one, two, three
-  // and eight rounds 90, 87, 83 and 85.
-  const int workgroups = 8 * (cus > 0 ? cus : 256);
+  // Up to 16 rows: four rounds of the two workgroups that a compute unit holds: there is nothing to join, and 64 ragged sequences take 82 us, with one,
+  // two, three and eight rounds 90, 87, 83 and 85.  More rows, which every workgroup lays into LDS: one round of three.  One, two, three, four, eight
+  // workgroups to a compute unit: 32 new tokens of four sequences, 8 heads to a K/V head, ragged caches of 20000 8-bit keys 23.6 21.8 19.2 21.0 23.1 us, of
+  // one sequence 15.5 13.2 12.8 12.7 16.4; 63 of 16 ragged sequences of 8192 keys, 4 heads, from two on 66 63 72 76.
+  const int workgroups = (a.H / a.Hk * a.T > 16 ? 3 : 8) * (cus > 0 ? cus : 256);
   a.chunks = fm_divisor(a.dealt ? std::max(1, workgroups / a.Hk) : (a.places + a.chunk_keys - 1) / a.chunk_keys);
   const long long units = a.dealt ? fm_most_units((int)a.chunks.n, a.B) : (long long)a.B * a.chunks.n;
   return (units + 8) * a.Hk < 1 << 24;   // a launch has fewer than 2^32 lanes

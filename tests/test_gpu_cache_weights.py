@@ -196,3 +196,45 @@ def test_more_rows_than_lie_in_lds(type, cache):
     """300 and 2048 query rows to a K/V head."""
     _run(_problem(21, [400, 33], 12, 1, 25, 128, 64, type, cache, mask="bounds"), 0.5)
     _run(_problem(22, [300], 8, 1, 256, 64, 16, type, cache, hide=False), 0.5)
+
+
+MANY_ROWS = [
+    # lens, H, Hk, T, d, page: more query rows than a workgroup holds at a time, more new tokens than a word has bits, few keys to share
+    ([150, 64, 3, 0], 3, 1, 100, 64, 16),
+    ([300, 65], 8, 1, 64, 64, 48),
+    ([520, 40], 4, 2, 256, 64, 64),
+    ([90, 61, 1], 16, 2, 63, 128, 32),
+    ([40, 200], 34, 2, 1, 128, 16),
+]
+
+
+@pytest.mark.parametrize("type,cache", [("bf16", "bf16"), ("f16", "e4m3")])
+@pytest.mark.parametrize("mask", ["none", "window", "bounds", "random"])
+@pytest.mark.parametrize("case", range(len(MANY_ROWS)))
+def test_many_rows(case, mask, type, cache):
+    lens, H, Hk, T, d, page = MANY_ROWS[case]
+    _run(_problem(200 + case, lens, H, Hk, T, d, page, type, cache, packed=case % 2 == 0, mask=mask), 0.5, in_place=case == 1)
+
+
+def test_a_window_at_the_seam_of_two_panels():
+    """More sequences than are dealt out in pieces of one size: each is one piece, whose live steps are few on both sides of key 4096.  They all
+    have the pages of the first, and its weights."""
+    import paper_2410_01359_amd as fm
+    B, T = 520, 20
+    one = _problem(30, [4166], 1, 1, T, 64, 16, "bf16", "bf16", hide=False)
+    one["window"] = 100
+    want = _run(one, 0.5, before=False)
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    k, _ = values_of(one)
+    k = np.where(np.isfinite(k), k, 0)
+    lse = cache_oracle.decode(f64(one["q"]), k, k, one["table"].cpu().numpy(), [4166], 0.125, 100, None)[1].astype(np.float32)
+    more = [x.expand(B, *x.shape[1:]).contiguous() for x in (one["q"], one["table"], torch.tensor(lse, device="cuda"))]
+    old = torch.rand((B, 1, 4176), device="cuda", generator=gen)
+    got = fm.flashmask_cache_weights(more[0], one["k_cache"], one["v_cache"], more[1], one["lens"].expand(B).contiguous(), more[2], 0.125, old.clone(),
+                                     decay=1.0, window=100)
+    assert (got[:, :, :4000] == old[:, :, :4000]).all()
+    new = torch.where(torch.arange(4176, device="cuda") < 4166 - T, old, 0)[:, :, :4166]
+    # Both are sums of the same 20 numbers in orders of their own: 19 additions each, off by half a step (2^-24) of what they give, which is no more than
+    # the sum; the old weight's addition is one more, of both together.
+    size, error = want[:, :, :4166].double(), got[:, :, :4166].double() - new.double() - want[:, :, :4166].double()
+    assert (error.abs() <= 2.0 ** -24 * 1.001 * (39 * size + new)).all()
