@@ -1,11 +1,14 @@
 """One attention layer generating text-like sequences with the library: the operators around the attention call, used together.
 
-    python examples/generate.py [--type bf16|f16] [--e4m3] [--steps N]
+    python examples/generate.py [--way steps|trees|forget] [--type bf16|f16] [--e4m3] [--steps N]
 
 Random weights, random token embeddings.  Prompts are written to a paged cache and attended to by flashmask_fwd_ex; each
 step then rotates and writes one new token per sequence (flashmask_cache_append) and attends to the cache (flashmask_decode).
 Half way, every sequence is forked into two that go on differently, some sequences end, and the cache is compacted.  At the
 end each sequence's last outputs are computed again from scratch, without a cache, and compared.
+`speculate` drafts trees of tokens instead, attends to all of a tree in one call (flashmask_decode_tree) and takes a path of it over
+(flashmask_cache_accept).  `forget` sums up what attention weight every key gets (flashmask_weights for the prompt, flashmask_cache_weights for
+each step) and drops the light ones when a sequence has become too long (flashmask_cache_evict).
 `train_step` is the same layer's share of a training step: rotation, attention, and the gradients of both.
 """
 from __future__ import annotations
@@ -50,6 +53,14 @@ class Layer:
         """Writes the tokens x [n, MODEL] to the cache; their rotated queries."""
         q, k, v = self.project(x)
         return fm.flashmask_cache_append(k, v, *self.pools, table, seqs, positions, q=q, freqs=self.freqs, **self.scales)
+
+    def write(self, x, table, positions, places):
+        """Writes the tokens x [B, T, MODEL], which are at `positions` [B, T] of their sequences, to other places; their rotated queries."""
+        q, k, v = (y.transpose(1, 2) for y in self.project(x))
+        q, k = fm.flashmask_rope(q, k, self.freqs, positions=positions)
+        seqs = torch.arange(len(x), dtype=torch.int32, device="cuda").repeat_interleave(x.shape[1])
+        fm.flashmask_cache_append(*(y.transpose(1, 2).flatten(0, 1) for y in (k, v)), *self.pools, table, seqs, places.flatten(), **self.scales)
+        return q
 
     def decode(self, q, table, lens):
         return fm.flashmask_decode(q[:, :, None], *self.pools, table, lens, D ** -0.5, **self.scales)[0][:, :, 0]
@@ -127,14 +138,100 @@ def generate(dtype=torch.bfloat16, cache_dtype=None, steps=40, prompts=(1, 17, 9
     return worst
 
 
+def speculate(dtype=torch.bfloat16, cache_dtype=None, rounds=6, drafted=13, prompts=(1, 17, 90, 33)):
+    """Largest difference between the outputs of accepted tokens and those computed from scratch, relative to the largest output."""
+    columns = -(-(max(prompts) + rounds * drafted) // PAGE)
+    B, T, pages = len(prompts), drafted, len(prompts) * columns
+    layer, rng = Layer(dtype, cache_dtype or dtype, pages), torch.Generator().manual_seed(3)
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    table = torch.randperm(pages, generator=rng).to(torch.int32).view(B, columns).cuda()
+    texts = [torch.randn((n, MODEL), device="cuda", generator=gen).to(dtype) for n in prompts]
+    for b, text in enumerate(texts):
+        at = torch.arange(len(text), dtype=torch.int32, device="cuda")
+        layer.append(text, table, torch.full_like(at, b), at)
+    lens, worst = torch.tensor(prompts, dtype=torch.int32, device="cuda"), 0.0
+    for _ in range(rounds):
+        # a random tree; a real program has the tokens that a small model thinks likely
+        parents = torch.stack([torch.cat([torch.randint(-1, t, (1,), generator=rng) if t else torch.tensor([-1]) for t in range(T)]) for _ in range(B)])
+        depth, path = torch.zeros((B, T), dtype=torch.int32), torch.full((B, T), -1, dtype=torch.int32)
+        for b in range(B):
+            for t in range(T):
+                depth[b, t] = depth[b, parents[b, t]] + 1 if parents[b, t] >= 0 else 0
+            t, n = -1, 0       # accepted: any way down; a real program goes by the outputs
+            while len(children := (parents[b] == t).nonzero().flatten()):
+                t = int(children[torch.randint(len(children), (1,), generator=rng)])
+                path[b, n], n = t, n + 1
+        x = torch.randn((B, T, MODEL), device="cuda", generator=gen).to(dtype)
+        places = lens[:, None] + torch.arange(T, dtype=torch.int32, device="cuda")
+        q = layer.write(x, table, lens[:, None] + depth.cuda(), places)
+        out, _ = fm.flashmask_decode_tree(q, *layer.pools, table, lens + T, parents.to(torch.int32).cuda(), D ** -0.5, **layer.scales)
+        lens = fm.flashmask_cache_accept(layer.pools, table, lens + T, T, path.cuda())
+        for b in range(B):
+            way = path[b][path[b] >= 0].long().cuda()
+            texts[b] = torch.cat((texts[b], x[b, way]))
+            assert len(texts[b]) == int(lens[b])
+            want = layer.full(texts[b][None])[0, :, -len(way):].float()
+            worst = max(worst, float((out[b][:, way].float() - want).abs().max() / want.abs().max()))
+    return worst
+
+
+def forget(dtype=torch.bfloat16, cache_dtype=None, steps=40, prompt=100, most=120, keep=64, sequences=3):
+    """Largest difference between the outputs of the last step and attention over the kept tokens' own keys and values, relative to the
+    largest output."""
+    columns, B = -(-max(most, prompt + 1) // PAGE), sequences
+    layer, gen = Layer(dtype, cache_dtype or dtype, 2 * B * columns), torch.Generator(device="cuda").manual_seed(4)
+    table, spare = torch.randperm(2 * B * columns, device="cuda", generator=gen).to(torch.int32).view(2, B, columns).unbind()
+    table, spare = table.contiguous(), spare.contiguous()
+    text = torch.randn((B, prompt, MODEL), device="cuda", generator=gen).to(dtype)
+
+    def places(n):
+        return torch.arange(n, dtype=torch.int32, device="cuda").repeat(B, 1)
+
+    # the prompt: what its last rows look at is what counts
+    layer.write(text, table, places(prompt), places(prompt))
+    q, k, v = (y.bfloat16().transpose(1, 2) for y in layer.project(text))
+    q, k = fm.flashmask_rope(q, k, layer.freqs)
+    bounds = causal_bounds(B, prompt)
+    _, lse = fm.flashmask_fwd_ex(q, k, v, *bounds, D ** -0.5)
+    weights = torch.zeros((B, KV_HEADS, columns * PAGE), device="cuda")
+    weights[:, :, :prompt] = fm.flashmask_weights(q, k, lse, *bounds, D ** -0.5, first_row=max(prompt - 32, 0))
+    lens = torch.full((B,), prompt, dtype=torch.int32, device="cuda")
+    # which token of the text a place has
+    who = torch.arange(columns * PAGE, device="cuda").expand(B, KV_HEADS, -1).clone()
+    for _ in range(steps):
+        if int(lens.max()) == most:
+            new, lens, weights, kept = fm.flashmask_cache_evict(*layer.pools, table, lens, weights, spare, keep, first=4, recent=16, **layer.scales)
+            who[:, :, :keep] = who.gather(2, kept.long())
+            assert torch.equal(new[:, :keep // PAGE], spare[:, :keep // PAGE])
+            table, spare = spare, table        # the old pages are free
+        x = torch.randn((B, 1, MODEL), device="cuda", generator=gen).to(dtype)
+        who.scatter_(2, lens.long()[:, None, None].expand(B, KV_HEADS, 1), text.shape[1])
+        q = layer.write(x, table, torch.full((B, 1), text.shape[1], dtype=torch.int32, device="cuda"), lens[:, None])
+        text, lens = torch.cat((text, x), 1), lens + 1
+        out, lse = fm.flashmask_decode(q, *layer.pools, table, lens, D ** -0.5, **layer.scales)
+        weights = fm.flashmask_cache_weights(q, *layer.pools, table, lens, lse, D ** -0.5, weights, decay=0.95, **layer.scales)
+    _, k, v = (y.transpose(1, 2) for y in layer.project(text))
+    _, k = fm.flashmask_rope(k, k, layer.freqs)
+    n = int(lens[0])
+    k, v = (y.float().gather(2, who[:, :, :n, None].expand(-1, -1, -1, D)).repeat_interleave(HEADS // KV_HEADS, 1) for y in (k, v))
+    want = torch.softmax(q.float() @ k.transpose(2, 3).contiguous() * D ** -0.5, -1) @ v
+    return float((out.float() - want).abs().max() / want.abs().max())
+
+
 def main():
     ap = argparse.ArgumentParser(description=__doc__.split("\n")[0])
     ap.add_argument("--type", choices=("bf16", "f16"), default="bf16")
     ap.add_argument("--e4m3", action="store_true", help="8-bit cache")
     ap.add_argument("--steps", type=int, default=40)
+    ap.add_argument("--way", choices=("steps", "trees", "forget"), default="steps")
     a = ap.parse_args()
     dtype = torch.bfloat16 if a.type == "bf16" else torch.float16
-    off = generate(dtype, torch.float8_e4m3fn if a.e4m3 else dtype, a.steps)
+    cache = torch.float8_e4m3fn if a.e4m3 else dtype
+    if a.way != "steps":
+        off = speculate(dtype, cache, a.steps) if a.way == "trees" else forget(dtype, cache, a.steps)
+        print(f"{a.steps} {a.way}: outputs differ from those without a cache by {off:.4f} of the largest")
+        return
+    off = generate(dtype, cache, a.steps)
     print(f"{a.steps} steps: last outputs differ from those without a cache by {off:.4f} of the largest")
     layer = Layer(torch.bfloat16, torch.bfloat16, 1)
     x = torch.randn((2, 500, MODEL), device="cuda").bfloat16()

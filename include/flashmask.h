@@ -481,7 +481,9 @@ int flashmask_cache_weights(const flashmask_cache* cache, const void* q, const i
  *               none of them in use or named twice.  What falls to "no page" is not written.
  *   table_out   int32 [sequences, columns], lens_out int32 [sequences]: the new pages and -1 behind them, and keep; or the old row and length
  *   weights_out as weights: those of the tokens in their new places, 0 behind them
- *  * A kept token whose old place has no page becomes zeros.  Outputs overlap nothing else.  At most 65535 sequences.
+ *   kept        int32 [sequences, weight_heads, keep]: the places that the tokens come from, -1 behind the last
+ *   workspace   at least flashmask_cache_evict_workspace_bytes(), 256-byte aligned
+ * A kept token whose old place has no page becomes zeros.  Outputs overlap nothing else.  At most 65535 sequences.
  */
 int flashmask_cache_evict(const flashmask_cache* cache, const int32_t* lens, const float* weights, int weight_heads, int weight_columns,
                           int keep, int first, int recent, const int32_t* new_table, int new_columns, int32_t* table_out, int32_t* lens_out,

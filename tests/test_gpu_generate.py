@@ -33,6 +33,18 @@ def test_steps_over_the_cache(type, cache, bar):
     assert _example().generate(type, cache, steps=24) <= bar
 
 
+@pytest.mark.parametrize("way,size", [("speculate", {"rounds": 4}), ("speculate", {"rounds": 3, "drafted": 70}), ("forget", {"steps": 70}),
+                                      ("forget", {"steps": 30, "prompt": 119, "most": 130, "keep": 128})])
+@pytest.mark.parametrize("type,cache,bar", [
+    # as above
+    (torch.bfloat16, torch.bfloat16, 8 * 2.0 ** -8),
+    (torch.float16, torch.float16, 8 * 2.0 ** -8),
+    (torch.bfloat16, torch.float8_e4m3fn, 4 * 2.0 ** -4),
+])
+def test_trees_and_eviction(type, cache, bar, way, size):
+    assert getattr(_example(), way)(type, cache, **size) <= bar
+
+
 def test_training_step():
     example = _example()
     layer = example.Layer(torch.bfloat16, torch.bfloat16, 1)

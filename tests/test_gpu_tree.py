@@ -134,6 +134,57 @@ def test_an_odd_value_reaches_those_that_see_it(type, odd, T, H, Hk):
         assert np.isfinite(np.delete(out[:, t], 5, -1)).all()
 
 
+MORE_CASES = [
+    # more sequences than a wave looks over at once; with that many workgroups the chunks of keys are listed by a launch of their own
+    ([(37 * b) % 150 for b in range(70)], 16, 16, 64, 64, 16),
+    ([(37 * b) % 150 for b in range(130)], 4, 2, 9, 64, 16),
+    ([(91 * b) % 700 for b in range(70)], 2, 1, 40, 128, 32),
+    # few chunks to a sequence, and many rows: a join of their own
+    ([1500, 700, 20, 0], 32, 16, 40, 64, 32),
+    ([2200, 900], 16, 4, 61, 128, 64),
+]
+
+
+@pytest.mark.parametrize("mask", ["none", "window", "bounds"])
+@pytest.mark.parametrize("case", range(len(MORE_CASES)))
+def test_many_sequences_and_heads(case, mask):
+    lens, H, Hk, T, d, page = MORE_CASES[case]
+    _check(_problem(300 + case, lens, H, Hk, T, d, page, ("bf16", "f16")[case % 2], ("e4m3", "f16", "bf16", "f16", "bf16")[case], mask=mask),
+           ("bf16", "f16")[case % 2])
+
+
+def test_two_graphs_at_once():
+    """Calls with workspaces of their own, captured and replayed on two streams at a time, give what each gives alone."""
+    import paper_2410_01359_amd as fm
+    problems = [_problem(400 + i, [2000, 700, 40], 8, 2, T, 64, 16, "bf16", "bf16") for i, T in enumerate((20, 40))]
+    graphs, results, wants = [], [], []
+    for p in problems:
+        p["parents_on_gpu"] = ints(p["parents"])
+        ws = torch.empty(fm.flashmask_decode_tree_workspace_bytes(3, 8, 2, p["q"].shape[2], 64), dtype=torch.uint8, device="cuda")
+
+        def call(p=p, ws=ws):
+            return fm.flashmask_decode_tree(p["q"], p["k_cache"], p["v_cache"], p["table"], p["lens"], p["parents_on_gpu"], p["scale"], workspace=ws)
+
+        wants.append([x.clone() for x in call()])
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=torch.cuda.Stream()):
+            results.append(call())
+        graphs.append(graph)
+    streams = [torch.cuda.Stream() for _ in graphs]
+    for _ in range(3):
+        for got in results:
+            for x in got:
+                x.fill_(-7)
+        torch.cuda.synchronize()
+        for graph, stream in zip(graphs, streams):
+            with torch.cuda.stream(stream):
+                graph.replay()
+        torch.cuda.synchronize()
+        for got, want in zip(results, wants):
+            assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
 def test_a_chain_is_flashmask_decode():
     import paper_2410_01359_amd as fm
     p = _problem(7, [900, 33], 4, 2, 4, 128, 16, "bf16", "bf16", kind="chain")
