@@ -157,12 +157,12 @@ def test_two_graphs_at_once():
     """Calls with workspaces of their own, captured and replayed on two streams at a time, give what each gives alone."""
     import paper_2410_01359_amd as fm
     problems = [_problem(400 + i, [2000, 700, 40], 8, 2, T, 64, 16, "bf16", "bf16") for i, T in enumerate((20, 40))]
-    graphs, results, wants = [], [], []
+    graphs, results, wants, spaces = [], [], [], []     # a graph's workspace lives as long as it does
     for p in problems:
         p["parents_on_gpu"] = ints(p["parents"])
-        ws = torch.empty(fm.flashmask_decode_tree_workspace_bytes(3, 8, 2, p["q"].shape[2], 64), dtype=torch.uint8, device="cuda")
+        spaces.append(torch.empty(fm.flashmask_decode_tree_workspace_bytes(3, 8, 2, p["q"].shape[2], 64), dtype=torch.uint8, device="cuda"))
 
-        def call(p=p, ws=ws):
+        def call(p=p, ws=spaces[-1]):
             return fm.flashmask_decode_tree(p["q"], p["k_cache"], p["v_cache"], p["table"], p["lens"], p["parents_on_gpu"], p["scale"], workspace=ws)
 
         wants.append([x.clone() for x in call()])
