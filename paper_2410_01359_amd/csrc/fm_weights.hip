@@ -18,9 +18,12 @@ __device__ __forceinline__ float minus_lse(float lse) { return lse == -INFINITY 
 
 // --- a prompt --------------------------------------------------------------------------------------------------
 // A workgroup has 256 keys of a K/V head, a wave 64 of them, whose fragments stay in registers (B operands of 32x32x16 products); 64 query rows at
-// a time come through LDS, two buffers, their loads in flight over the tile before.  Row tiles of all query heads of the group, one behind
+// a time come through LDS, copied two tiles ahead.  Row tiles of all query heads of the group, one behind
 // the other, are cut into `parts`; Equation 4 tells for the workgroup's and for the wave's keys which are skipped and which
 // take the element mask.
+// An element costs its product, a multiply-add, an exponential (8 cycles of a wave) and an addition: 64 of them as many cycles as their 32 products.
+// 16384 tokens with answers (32 heads on 8, d = 128): 890 us, with zeros for q and k 729: power.  The last 64 rows of 131072 tokens: 106 to 114 us, 56
+// without the loop over the rows.  With 32 keys to a wave and three workgroups to a compute unit 983 and 124.
 constexpr int kKeys = 256, kTile = 64, kPanel = 2048;   // kPanel: row tiles that are listed together
 
 template <int D>
