@@ -99,6 +99,12 @@ __global__ __launch_bounds__(kThreads, 2) void tree_kernel(FmTreeArgs a, FmDivis
   }
   u32x4 kraw[LOADS], vraw[LOADS];
   i32x4 bound_raw;
+  const auto copy_keys = [&](int buffer, int panel, int tile) {
+    tile_load_async<D>(rows_of(k_head, a.k, panel, tile, 0) - CopyLanes<D>::BIAS, k_lanes, sh.k[buffer], wave);
+  };
+  const auto copy_values = [&](int buffer, int panel, int tile) {
+    tile_load_async<D>(rows_of(v_head, a.v, panel, tile, 0) - CopyLanes<D>::BIAS, v_lanes, sh.v[buffer], wave);
+  };
   const auto load = [&](int buffer, int panel, int tile) {
     if constexpr (E4M3) {
 #pragma unroll
@@ -108,8 +114,8 @@ __global__ __launch_bounds__(kThreads, 2) void tree_kernel(FmTreeArgs a, FmDivis
         vraw[i] = ldg16(rows_of(v_head, a.v, panel, tile, i) + (row * a.v.token + at));
       }
     } else {
-      tile_load_async<D>(rows_of(k_head, a.k, panel, tile, 0) - CopyLanes<D>::BIAS, k_lanes, sh.k[buffer], wave);
-      tile_load_async<D>(rows_of(v_head, a.v, panel, tile, 0) - CopyLanes<D>::BIAS, v_lanes, sh.v[buffer], wave);
+      copy_keys(buffer, panel, tile);
+      copy_values(buffer, panel, tile);
     }
   };
   const auto load_bounds = [&](int start) {
@@ -215,7 +221,8 @@ __global__ __launch_bounds__(kThreads, 2) void tree_kernel(FmTreeArgs a, FmDivis
     return seen;
   };
 
-  const auto compute = [&](auto with_mask, int buffer, int turn, int start, int tile) {
+  // half_way() is called by waves without rows, too, by itself.
+  const auto compute = [&](auto with_mask, int buffer, int turn, int start, int tile, const auto& half_way) {
     constexpr bool MASKED = decltype(with_mask)::value;
     // operands from LDS a few products ahead
     f32x16 s[2] = {};
@@ -232,6 +239,7 @@ __global__ __launch_bounds__(kThreads, 2) void tree_kernel(FmTreeArgs a, FmDivis
         __builtin_amdgcn_sched_barrier(0);
       }
     }
+    half_way();
     unsigned seen = ~0u;
     if constexpr (MASKED) {
       seen = seen_keys(buffer, start, tile);
@@ -367,13 +375,52 @@ __global__ __launch_bounds__(kThreads, 2) void tree_kernel(FmTreeArgs a, FmDivis
         }
         clean(buffer, turn, start, now);
       }
-      if (!idle) compute(with_mask, buffer, turn, start, now);
+      if (!idle) compute(with_mask, buffer, turn, start, now, [] {});
       buffer ^= 1;
       turn = turn == 2 ? 0 : turn + 1;
       if (more) store(buffer);
       barrier_nofence();
       if (!more) break;
     }
+  };
+  // The same of unmasked tiles of 16 bits, with a tile and a half ahead: keys are copied where the products with those before the last are done, values
+  // where the tile before is done.  (All a tile ahead: ??.)
+  const auto run_far = [&](int panel, unsigned long long tiles) {
+    constexpr int COPIES = CopyLanes<D>::NINST;
+    const auto take = [&] {
+      const int tile = tiles ? __builtin_ctzll(tiles) : -1;
+      tiles &= tiles - 1;
+      return tile;
+    };
+    // what comes by ordinary loads is there before the first copy, so that no wait for it counts the copies
+#pragma unroll
+    for (int g = 0; g < kTile / FM_KEY_GROUP; ++g) settle(entry[g]);
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s) settle(q[s]);
+    int now = take(), next = take();
+    buffer = 0;
+    copy_keys(0, panel, now);
+    copy_values(0, panel, now);
+    if (next >= 0) copy_keys(1, panel, next);
+    while (now >= 0) {
+      const int far = take();
+      if (next >= 0) async_wait<2 * COPIES>();
+      else async_wait<COPIES>();
+      barrier_nofence();   // the keys are there, the values before have been read
+      if (next >= 0) copy_values(buffer ^ 1, panel, next);
+      const auto half_way = [&] {
+        if (next >= 0) async_wait<2 * COPIES>();
+        else async_wait<0>();
+        barrier_nofence();   // the values are there, the keys have been read
+        if (far >= 0) copy_keys(buffer, panel, far);
+      };
+      if (idle) half_way();
+      else compute(std::false_type(), buffer, 0, panel + now * kTile, now, half_way);
+      now = next;
+      next = far;
+      buffer ^= 1;
+    }
+    barrier_nofence();
   };
   if (a.bounds[0] || a.window > 0) plant_tree();
   for (int panel = begin; panel < end; panel += kPanelTiles * kTile) {
@@ -417,7 +464,10 @@ __global__ __launch_bounds__(kThreads, 2) void tree_kernel(FmTreeArgs a, FmDivis
       live = __ballot(lane < tiles);
       partly = __ballot(hole || start + kTile > panel_end || start + kTile > first_row || (a.window > 0 && start <= rows_end - 1 - a.window));
     }
-    if (live & ~partly) run(std::false_type(), panel, live & ~partly);
+    if (live & ~partly) {
+      if constexpr (E4M3) run(std::false_type(), panel, live & ~partly);
+      else run_far(panel, live & ~partly);
+    }
     if (live & partly) {
       if (!a.bounds[0] && a.window <= 0) plant_tree();
       run(std::true_type(), panel, live & partly);
