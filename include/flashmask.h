@@ -432,7 +432,7 @@ size_t flashmask_decode_tree_workspace_bytes(int sequences, int H, int H_kv, int
  *   path        int32 [sequences, path_columns], path_columns <= T: ascending numbers of drafted tokens.  It ends in front of the first value that
  *               is not one of 0 .. T - 1 or not above the one before (-1 by custom).
  *   lens_out    int32 [sequences], not lens itself;  a sequence of fewer than T tokens stays as it is
- *   pools       HOST array of num_pools device pointers to pages of `type` (BF16, F16 or E4M3), 16-byte aligned, one layout for all: strides as in
+ *   pools       HOST array of num_pools device pointers to pages of `type` (BF16, F16 or E4M3), 16-byte aligned, none twice, one layout for all: strides as in
  *               flashmask_cache, `heads` rows of d elements to a token
  * A place without a page is not written; from a place without one come zeros.  At most 65535 sequences.
  */
