@@ -267,9 +267,12 @@ def flashmask_cache_accept(pools, table, lens, T: int, path):
             raise FlashMaskError("the pools must have one shape, layout and type, on one GPU")
     if not _fits(T):
         raise FlashMaskError(f"T is out of range: {T}")
+    at = [p.data_ptr() for p in pools]
+    if len(set(at)) != len(at):
+        raise FlashMaskError("a pool is named twice")
     pages, heads, page, d = shape
     lens_out = torch.empty_like(lens)
-    _check(load_library().flashmask_cache_accept(struct.pack(f"@{len(pools)}P", *[p.data_ptr() for p in pools]), len(pools), _ONE.pack(*strides[:3]),
+    _check(load_library().flashmask_cache_accept(struct.pack(f"@{len(at)}P", *at), len(at), _ONE.pack(*strides[:3]),
                                                  type_id, heads, d, pages, page, table.data_ptr(), lens.data_ptr(), path.data_ptr(),
                                                  lens_out.data_ptr(), B, entries[1], T, path.shape[1], _stream()), "flashmask_cache_accept")
     return lens_out

@@ -260,6 +260,15 @@ def test_accept_odd_paths_and_missing_pages():
     _accept(p, [p["k_cache"], p["v_cache"]], 16, paths)
 
 
+def test_accept_a_pool_named_twice_is_refused():
+    import paper_2410_01359_amd as fm
+    p = paged(3, [40], 2, 16, 64, "bf16")
+    before = p["k_cache"].clone()
+    with pytest.raises(fm.FlashMaskError):
+        fm.flashmask_cache_accept([p["k_cache"], p["v_cache"], p["k_cache"]], p["table"], p["lens"], 5, ints([[1, 2]]))
+    assert torch.equal(raw(before), raw(p["k_cache"]))
+
+
 def test_accept_a_graph_of_it():
     import paper_2410_01359_amd as fm
     p = paged(52, [60, 44], 2, 16, 64, "bf16")
