@@ -172,9 +172,46 @@ __device__ __forceinline__ void write_rest(const FmEvictArgs& a, const Row& row,
   for (int j = at; j < min(row.n, row.columns); j += step) row.weights_out[j] = row.weights[j];
 }
 
-// One workgroup to a row.
-__global__ __launch_bounds__(kSelectThreads) void select_kernel(FmEvictArgs a) {
+// Rows of the tokens that stay go to their new places, keys and values, 16 bytes a lane.  A token without a page becomes zeros.  Memory: 2048 tokens of 256
+// bytes of 8 heads of up to 48 sequences 52 us, 5.9 TB/s.
+template <int TOKENS>
+struct Moves {
+  long long from[TOKENS], to[TOKENS];   // page << 32 | slot, -1: none
+  // Of a head's kept tokens [first, first + count), by a workgroup; pieces: of 16 bytes of a row.
+  template <int THREADS>
+  __device__ __forceinline__ void run(const FmEvictArgs& a, int b, int h, const int* kept, int first, int count, const FmDivisor& pieces) {
+    static_assert(TOKENS <= THREADS);
+    if ((int)threadIdx.x < count) {
+      const auto place = [&](const int* row, int j) {
+        const int column = fm_div(j, a.page), page = fm_known_page(row[column], a.num_pages);
+        return page < 0 ? -1ll : (long long)page << 32 | (j - column * (int)a.page.n);
+      };
+      const int i = first + threadIdx.x;
+      from[threadIdx.x] = place(a.table + (size_t)b * a.columns, kept[i]);
+      to[threadIdx.x] = place(a.new_table + (size_t)b * a.new_columns, i);
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < count * (int)pieces.n; i += THREADS) {
+      const int token = fm_div(i, pieces), piece = i - token * (int)pieces.n;
+      const long long source = from[token], target = to[token];
+      if (target < 0) continue;
+#pragma unroll
+      for (int w = 0; w < 2; ++w) {
+        const FmPages& p = a.cache[w];
+        const auto at = [&](long long x) { return p.base + (x >> 32) * p.page + h * p.head + (unsigned)x * (long long)p.token + piece * 16; };
+        u32x4 v = {0, 0, 0, 0};
+        if (source >= 0) v = ldg16(at(source));
+        *(u32x4*)at(target) = v;
+      }
+    }
+  }
+};
+
+// One workgroup to a row.  MOVE: it moves the tokens that stay, too, of its one head, one to a thread at most.
+template <bool MOVE>
+__global__ __launch_bounds__(kSelectThreads) void select_kernel(FmEvictArgs a, FmDivisor pieces) {
   __shared__ SelectShared sh;
+  __shared__ Moves<MOVE ? kSelectThreads : 1> moves;
   const int b = blockIdx.y, h = blockIdx.x;
   const Row row(a, b, h);
   float w[kEach];
@@ -198,6 +235,10 @@ __global__ __launch_bounds__(kSelectThreads) void select_kernel(FmEvictArgs a) {
   for (int base = 0; base < row.n; base += kChunk) {
     if (row.n > kChunk) row.load(w, base, row.n);
     keep_places(sh, row, w, base, row.n, prefix, (int)wanted, stayed, equals);
+  }
+  if constexpr (MOVE) {
+    __syncthreads();   // the list is there
+    moves.template run<kSelectThreads>(a, b, h, row.kept, 0, row.keep, pieces);
   }
 }
 
@@ -287,39 +328,14 @@ __global__ __launch_bounds__(kSelectThreads) void split_kernel(FmEvictArgs a) {
   }
 }
 
-// Rows of the tokens that stay go to their new places, keys and values, 16 bytes a lane.  A token without a page becomes zeros.  Memory: 2048 tokens of 256
-// bytes of 8 heads of up to 48 sequences 52 us, 5.9 TB/s.
 constexpr int kGatherTokens = 64;
-__global__ __launch_bounds__(256) void gather_kernel(FmEvictArgs a, int pieces) {
-  __shared__ long long from[kGatherTokens], to[kGatherTokens];   // page << 32 | slot, -1: none
+__global__ __launch_bounds__(256) void gather_kernel(FmEvictArgs a, FmDivisor pieces) {
+  __shared__ Moves<kGatherTokens> moves;
   const int b = blockIdx.z, h = blockIdx.y, first = blockIdx.x * kGatherTokens;
   const int places = (int)a.page.n * a.columns;
   if (min(max(a.lens[b], 0), places) <= a.keep) return;
-  const int count = min(kGatherTokens, a.keep - first);
   const int* kept = a.kept + ((size_t)b * a.weight_heads + (a.weight_heads > 1 ? h : 0)) * a.keep;
-  if ((int)threadIdx.x < count) {
-    const auto place = [&](const int* row, int j) {
-      const int column = fm_div(j, a.page), page = fm_known_page(row[column], a.num_pages);
-      return page < 0 ? -1ll : (long long)page << 32 | (j - column * (int)a.page.n);
-    };
-    const int i = first + threadIdx.x;
-    from[threadIdx.x] = place(a.table + (size_t)b * a.columns, kept[i]);
-    to[threadIdx.x] = place(a.new_table + (size_t)b * a.new_columns, i);
-  }
-  __syncthreads();
-  for (int i = threadIdx.x; i < count * pieces; i += 256) {
-    const int token = i / pieces, piece = i - token * pieces;
-    const long long source = from[token], target = to[token];
-    if (target < 0) continue;
-#pragma unroll
-    for (int w = 0; w < 2; ++w) {
-      const FmPages& p = a.cache[w];
-      const auto at = [&](long long x) { return p.base + (x >> 32) * p.page + h * p.head + (unsigned)x * (long long)p.token + piece * 16; };
-      u32x4 v = {0, 0, 0, 0};
-      if (source >= 0) v = ldg16(at(source));
-      *(u32x4*)at(target) = v;
-    }
-  }
+  moves.run<256>(a, b, h, kept, first, min(kGatherTokens, a.keep - first), pieces);
 }
 
 // --- the accepted path -----------------------------------------------------------------------------------------
@@ -374,6 +390,7 @@ size_t fm_evict_bytes(int sequences, int weight_heads, int weight_columns) {
 }
 
 hipError_t fm_launch_evict(const FmEvictArgs& a, hipStream_t stream) {
+  const FmDivisor pieces = fm_divisor(a.row_bytes / 16);
   if (fm_evict_bytes(a.B, a.weight_heads, a.weight_columns)) {
     const dim3 grid(FM_EVICT_PARTS, a.weight_heads, a.B), threads(fm::kSelectThreads);
     hipLaunchKernelGGL(fm::split_kernel<0>, grid, threads, 0, stream, a);
@@ -381,9 +398,14 @@ hipError_t fm_launch_evict(const FmEvictArgs& a, hipStream_t stream) {
     hipLaunchKernelGGL(fm::split_kernel<2>, grid, threads, 0, stream, a);
     hipLaunchKernelGGL(fm::split_kernel<3>, grid, threads, 0, stream, a);
   } else {
-    hipLaunchKernelGGL(fm::select_kernel, dim3(a.weight_heads, a.B), dim3(fm::kSelectThreads), 0, stream, a);
+    // A launch less, and no more workgroups than rows: up to 64 KiB of keys to a row.  One launch / two, us: 4 heads of 100 tokens of 128 bytes 13.7 / 16.0, 32 of 250
+    // of 256 bytes 14.9 / 16.7, of 500 17.1 / 16.4, of 1000 25 / 18.
+    static_assert((64 << 10) / 64 <= fm::kSelectThreads);   // rows have 64 bytes at least
+    const bool move = a.weight_heads == a.Hk && (long long)a.keep * a.row_bytes <= 64 << 10;
+    hipLaunchKernelGGL(move ? fm::select_kernel<true> : fm::select_kernel<false>, dim3(a.weight_heads, a.B), dim3(fm::kSelectThreads), 0, stream, a, pieces);
+    if (move) return hipGetLastError();
   }
-  hipLaunchKernelGGL(fm::gather_kernel, dim3((a.keep + fm::kGatherTokens - 1) / fm::kGatherTokens, a.Hk, a.B), dim3(256), 0, stream, a, a.row_bytes / 16);
+  hipLaunchKernelGGL(fm::gather_kernel, dim3((a.keep + fm::kGatherTokens - 1) / fm::kGatherTokens, a.Hk, a.B), dim3(256), 0, stream, a, pieces);
   return hipGetLastError();
 }
 
