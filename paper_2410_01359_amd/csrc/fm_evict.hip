@@ -10,8 +10,9 @@ namespace fm {
 // --- eviction --------------------------------------------------------------------------------------------------
 // The m heaviest of the tokens between the first and the last ones: the m-th heaviest weight is found digit by digit (11, 11, 10 bits) from
 // histograms of the digits of those that agree with it so far, of weights as whole numbers of the same order.  What is heavier
-// stays, and of what is as heavy the first ones.  384 rows of up to 6000: 14 us (digits counted in four banks by lane: 15).  A workgroup takes 8192 places at a time, eight to a thread with their loads in flight together; a row
-// of no more stays in registers.
+// stays, and of what is as heavy the first ones.  A workgroup takes 8192 places at a time, eight to a thread with their loads in flight together; a row
+// of no more stays in registers.  A chain of steps between barriers: 384 rows of up to 6000 take 14 us, one of 300 11 (digits counted in four banks by
+// lane: 15).
 constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / 64, kEach = 8, kChunk = kSelectThreads * kEach;
 constexpr int kDigitBits = 11, kDigits = 1 << kDigitBits, kStages = 3;
 __device__ __forceinline__ int digit_shift(int stage) { return stage == 0 ? 21 : stage == 1 ? 10 : 0; }

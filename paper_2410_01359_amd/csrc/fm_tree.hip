@@ -280,7 +280,8 @@ __global__ __launch_bounds__(kThreads, 2) void tree_kernel(FmTreeArgs a, FmDivis
       u32x4 ring[RING], hi, lo;
       const auto fetch = [&](int i) {
         const char* rows = sh.v[buffer] + i / NDB * 16 * L::RS;
-        ring[i % RING] = __builtin_bit_cast(u32x4, cat4(lds_read_tr16(rows + L::add_col(v_off[0], i % NDB * 64)), lds_read_tr16(rows + L::add_col(v_off[1], i % NDB * 64))));
+        const auto part = [&](int hi) { return lds_read_tr16(rows + L::add_col(v_off[hi], i % NDB * 64)); };
+        ring[i % RING] = __builtin_bit_cast(u32x4, cat4(part(0), part(1)));
       };
       fetch(0);
       fetch(1);
