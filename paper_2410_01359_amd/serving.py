@@ -262,8 +262,9 @@ def flashmask_cache_accept(pools, table, lens, T: int, path):
             and 0 <= device == table.get_device() == lens.get_device() == path.get_device() == torch._C._cuda_getDevice()):
         _refuse((first, "pools", tuple(_CACHE_TYPE), (None,) * 4, 1), (table, "table", (ints,), (None, None), 2), (lens, "lens", (ints,), (B,), 2),
                 (path, "path", (ints,), (B, None), 2))
+    dense = first.is_contiguous()     # of contiguous tensors of one shape the strides need not be looked at
     for p in pools:
-        if not (p.dtype is dtype and p.shape == shape and p.stride() == strides and p.get_device() == device):
+        if not (p.dtype is dtype and p.shape == shape and (p.is_contiguous() if dense else p.stride() == strides) and p.get_device() == device):
             raise FlashMaskError("the pools must have one shape, layout and type, on one GPU")
     if not _fits(T):
         raise FlashMaskError(f"T is out of range: {T}")

@@ -269,6 +269,17 @@ def test_accept_a_pool_named_twice_is_refused():
     assert torch.equal(raw(before), raw(p["k_cache"]))
 
 
+def test_accept_pools_of_another_layout_are_refused():
+    import paper_2410_01359_amd as fm
+    p = paged(3, [40], 2, 16, 64, "bf16")
+    k, other = p["k_cache"], torch.zeros_like(p["k_cache"].transpose(1, 2).contiguous()).transpose(1, 2)
+    for pools in ([k, other], [other, k], [k, other.float()], [k, other[1:]]):
+        with pytest.raises(fm.FlashMaskError):
+            fm.flashmask_cache_accept(pools, p["table"], p["lens"], 5, ints([[1, 2]]))
+    fm.flashmask_cache_accept([other, torch.zeros_like(other)], p["table"], p["lens"], 5, ints([[1, 2]]))
+    torch.cuda.synchronize()
+
+
 def test_accept_a_graph_of_it():
     import paper_2410_01359_amd as fm
     p = paged(52, [60, 44], 2, 16, 64, "bf16")
