@@ -62,7 +62,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void decode_kernel(Args a, int memb
   constexpr int TW = kWaves / TEAMS;   // waves of a team
   using C = Decode<D, F16, E4M3, NB>;
   __shared__ typename C::Shared sh;
-  __shared__ std::conditional_t<kTree<Args>, Tree, char> tree;
+  __shared__ std::conditional_t<kTree<Args>, SmallTree, char> tree;   // of few rows, so of few tokens
   // Barriers here order LDS alone (barrier_nofence): loads stay in flight across them.
   // The launch arguments that come first, read together: left where they are first needed they are six round trips in a row.
   asm volatile("" ::"s"(a.units), "s"(a.plan), "s"(a.lens), "s"(a.B), "s"(a.T), "s"(a.window), "s"(a.columns), "s"(a.page_tokens), "s"(a.cut.least),
@@ -129,7 +129,20 @@ __global__ __launch_bounds__(64 * kWaves, 2) void decode_kernel(Args a, int memb
   const int j_begin = range.lo + chunk * size * kGroup;
   const int j_end = (int)std::min<long long>(range.hi, j_begin + (long long)size * kGroup);
   const int first_row = range.len - a.T;   // row of query 0
-  if constexpr (kTree<Args>) plant(tree, a.parents + (size_t)b * a.T, a.T);
+  // The tree is planted where it is first needed, which not all chunks do: its parents are asked for here
+  int parent = -1;
+  bool planted = false;
+  if constexpr (kTree<Args>) {
+    static_assert(!fm_tree_is_wide(1, 1, 63) && fm_tree_is_wide(1, 1, 64));
+    if (lane < a.T) parent = a.parents[(size_t)b * a.T + lane];
+  }
+  const auto plant_tree = [&] {
+    if constexpr (kTree<Args>) {
+      if (!planted) plant_small(tree, parent, a.T);
+      planted = true;
+    }
+  };
+  if (a.bounds[0]) plant_tree();
   // Row of query t, and whether it sees key j, bounds apart
   const auto row_of = [&](int t) {
     if constexpr (kTree<Args>) return first_row + tree.depth[t];
@@ -234,15 +247,23 @@ __global__ __launch_bounds__(64 * kWaves, 2) void decode_kernel(Args a, int memb
   const auto seen_keys = [&](int start, int panel, unsigned pages_there, int t) {
     unsigned seen = 0;
     const int row_i = row_of(t);
+    unsigned long long line = 0;   // drafted tokens that a drafted one sees, windows apart
+    if constexpr (kTree<Args>) line = (unsigned long long)tree.ancestors[t][1] << 32 | tree.ancestors[t][0];
     const int last = min(j_end - 1, row_i), first = a.window > 0 ? row_i - a.window + 1 : 0;
 #pragma unroll 1
     for (int i = 0; i < C::GROUPS; ++i) {
       const int j = start + i * kGroup + 4 * g;
       unsigned four = 0;
+      if (kTree<Args> && a.window <= 0) {
+        const int u = j - first_row, left = j_end - j;   // the first of the four keys as a drafted token, and keys
+        four = u >= 64 ? 0u : u >= 0 ? (unsigned)(line >> u) : u > -4 ? (unsigned)line << -u | ((1u << -u) - 1u) : 15u;
+        four &= left >= 4 ? 15u : left > 0 ? (1u << left) - 1u : 0u;
+      } else {
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        if constexpr (kTree<Args>) four |= (j + r < j_end && reaches(j + r, t) ? 1u : 0u) << r;
-        else four |= (j + r <= last && j + r >= first ? 1u : 0u) << r;
+        for (int r = 0; r < 4; ++r) {
+          if constexpr (kTree<Args>) four |= (j + r < j_end && reaches(j + r, t) ? 1u : 0u) << r;
+          else four |= (j + r <= last && j + r >= first ? 1u : 0u) << r;
+        }
       }
       if (a.bounds[0]) {
 #pragma unroll
@@ -355,6 +376,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void decode_kernel(Args a, int memb
           // element mask; values that no row sees become 0 (the keys of a lane's scores are those of its value pieces).  Which of its
           // keys a column sees is gathered as bits by a loop: unrolled, the bounds' addresses alone would fill the registers.
           if (masked) {
+            plant_tree();
             unsigned pages_there = 0;
 #pragma unroll
             for (int i = 0; i < C::GROUPS; ++i) pages_there |= (now.page(i) >= 0 ? 1u : 0u) << i;

@@ -89,7 +89,7 @@ hipError_t fm_launch_decode_tree(const FmTreeArgs& a, bool f16, bool e4m3, hipSt
 // Many query rows to a K/V head go through a kernel of their own, cut by fm_tree_cut in multiples of FM_TREE_ROUND groups of keys.  decode_kernel / that
 // one, us, 32 heads on 8, at 48, 64, 80, 128 and 252 rows: 16 trees over ragged caches of 8192 keys, d 128, 61/56 66/57 81/60 107/69 160/105, of e4m3
 // 56/61 59/62 73/66 90/76 141/123; one tree 21/25 26/25 27/26 36/31 57/38; 64 over ragged 1500 keys 62/66 68/69 83/74 98/89 140/146.
-inline bool fm_tree_is_wide(int H, int Hk, int T) { return H / Hk * T >= 64; }
+constexpr bool fm_tree_is_wide(int H, int Hk, int T) { return H / Hk * T >= 64; }
 constexpr int FM_TREE_ROUND = 4;
 FmDecodeCut fm_tree_cut(int H, int Hk, int T, int d, int B, int cus);
 hipError_t fm_launch_tree_wide(const FmTreeArgs& a, bool f16, bool e4m3, hipStream_t stream);

@@ -7,11 +7,35 @@ namespace fm {
 
 // Token t follows token parents[t] < t, or the sequence itself (any other value).  Its row is as many rows behind the first
 // new one as it has ancestors in the tree, and of the drafted tokens it sees those and itself.
-struct Tree {
-  unsigned ancestors[FM_MOST_NEW_TOKENS][FM_MOST_NEW_TOKENS / 32];   // of a token, itself among them
-  int depth[FM_MOST_NEW_TOKENS];
+template <int MOST>
+struct TreeOf {
+  unsigned ancestors[MOST][MOST / 32];   // of a token, itself among them
+  int depth[MOST];
   __device__ __forceinline__ bool on_path(int t, int u) const { return ancestors[t][u / 32] >> (u % 32) & 1; }
 };
+using Tree = TreeOf<FM_MOST_NEW_TOKENS>;
+using SmallTree = TreeOf<64>;
+
+// Of up to 64 tokens, by a wave for itself: lane t has token t's parent.  Lines double their reach in each turn.  Waves that share the tree write the same,
+// so that none waits for another (8 trees of 60 tokens over ragged caches of 3000, 8 heads of 64: 25.5 us by all waves together ahead of everything, 21.1).
+__device__ __forceinline__ void plant_small(SmallTree& tree, int parent, int T) {
+  const int lane = threadIdx.x & 63;
+  int ahead = lane < T && parent >= 0 && parent < lane ? parent : -1;   // the first of the line that is not among the bits
+  unsigned long long line = 1ull << lane;
+  while (__any(ahead >= 0)) {
+    const int from = ahead >= 0 ? ahead : lane;
+    const unsigned low = __shfl((unsigned)line, from), high = __shfl((unsigned)(line >> 32), from);
+    const int next = __shfl(ahead, from);
+    if (ahead >= 0) {
+      line |= (unsigned long long)high << 32 | low;
+      ahead = next;
+    }
+  }
+  tree.ancestors[lane][0] = (unsigned)line;
+  tree.ancestors[lane][1] = (unsigned)(line >> 32);
+  tree.depth[lane] = __popcll(line) - 1;
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // LDS serves a wave in order
+}
 
 // By a workgroup of at least T threads.  Every token walks up its line; parents come before their children, so that ends.
 __device__ __forceinline__ void plant(Tree& tree, const int* parents, int T) {
