@@ -153,6 +153,24 @@ def test_many_sequences_and_heads(case, mask):
            ("bf16", "f16")[case % 2])
 
 
+NARROW_CASES = [
+    # few rows to a K/V head, many tokens
+    ([700, 90, 61, 0], 4, 4, 60, 64, 16),
+    ([300, 63, 20], 3, 3, 63, 128, 32),
+    ([130, 40, 1], 2, 2, 33, 64, 48),
+    ([2100], 2, 1, 31, 128, 16),
+]
+
+
+@pytest.mark.parametrize("type,cache", [("bf16", "bf16"), ("f16", "e4m3")])
+@pytest.mark.parametrize("mask,kind", [("none", "random"), ("none", "chain"), ("none", "star"), ("window", "random"), ("narrow", "chain"), ("bounds", "random"),
+                                       ("random", "random"), ("none", "odd")])
+@pytest.mark.parametrize("case", range(len(NARROW_CASES)))
+def test_many_tokens_of_few_rows(case, mask, kind, type, cache):
+    lens, H, Hk, T, d, page = NARROW_CASES[case]
+    _check(_problem(500 + case, lens, H, Hk, T, d, page, type, cache, mask=mask, kind=kind), type)
+
+
 def test_two_graphs_at_once():
     """Calls with workspaces of their own, captured and replayed on two streams at a time, give what each gives alone."""
     import paper_2410_01359_amd as fm
