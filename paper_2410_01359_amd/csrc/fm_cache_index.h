@@ -37,6 +37,17 @@ FM_HOST_DEVICE inline FmKeyRange fm_key_range(int len, int T, int window, int ta
 }
 FM_HOST_DEVICE inline int fm_key_groups(const FmKeyRange& r) { return (r.hi - r.lo + FM_KEY_GROUP - 1) / FM_KEY_GROUP; }
 
+// Rows of [lo, hi) that are neither in [lts, lte) nor in [uts, ute).  Bounds are any numbers of 32 bits, such as an end far below its start for an empty
+// interval: they are held to the rows first, so that no difference is larger than hi - lo, which the caller keeps within 32 bits.
+FM_HOST_DEVICE inline int fm_rows_left(int lo, int hi, int lts, int lte, int uts, int ute) {
+  if (lo >= hi) return 0;
+  const auto held = [=](int i) { return i < lo ? lo : i > hi ? hi : i; };
+  const int a0 = held(lts), b0 = held(lte), a1 = held(uts), b1 = held(ute);
+  const int first = b0 > a0 ? b0 - a0 : 0, second = b1 > a1 ? b1 - a1 : 0;
+  const int begin = a0 > a1 ? a0 : a1, end = b0 < b1 ? b0 : b1;   // of what both have
+  return hi - lo - first - second + (end > begin ? end - begin : 0);
+}
+
 // Groups of a chunk where sequences of `total` groups together are meant to be cut into `chunks`: a multiple of `round`, at least `least`.
 FM_HOST_DEVICE inline int fm_chunk_groups(unsigned total, const FmDivisor& chunks, int least, int round) {
   unsigned size = fm_div((int)(total + chunks.n - 1), chunks);

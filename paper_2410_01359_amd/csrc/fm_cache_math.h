@@ -1,6 +1,7 @@
 // Arithmetic that the kernels over a paged cache share: products in 16 bits, probabilities as sums of two 16-bit values, 8-bit values to
 // 16 bits, sums and maxima over lanes.
 #pragma once
+#include "fm_cache_index.h"
 #include "fm_common.h"
 
 namespace fm {
@@ -123,12 +124,7 @@ __device__ __forceinline__ bool hides(const i32x4& bound, int i) {
   return (bound[0] <= i && i < bound[1]) || (bound[2] <= i && i < bound[3]);
 }
 
-
 // Rows of [lo, hi) that the bounds of a key leave.
-__device__ __forceinline__ int rows_left(int lo, int hi, const i32x4& bound) {
-  if (lo >= hi) return 0;
-  const int a0 = max(bound[0], lo), b0 = min(bound[1], hi), a1 = max(bound[2], lo), b1 = min(bound[3], hi);
-  return hi - lo - max(b0 - a0, 0) - max(b1 - a1, 0) + max(min(b0, b1) - max(a0, a1), 0);
-}
+__device__ __forceinline__ int rows_left(int lo, int hi, const i32x4& bound) { return fm_rows_left(lo, hi, bound[0], bound[1], bound[2], bound[3]); }
 
 }  // namespace fm
