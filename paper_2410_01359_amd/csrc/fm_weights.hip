@@ -532,7 +532,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache_weights_kernel(FmCacheWe
 #pragma unroll
             for (int i = 0; i < kGroups; ++i) {
               const auto below = [&](int row) {
-                const int n = min(max(row, 0), 1 << 30) - first_row;
+                const int n = min(max(row, 0), len) - first_row;   // T at most: no row is behind the sequence
                 return n >= 64 ? ~0ull : n <= 0 ? 0ull : (1ull << n) - 1;
               };
               const unsigned long long x = ~below(behind[i]) | below(key[i]) | (below(bound[i][1]) & ~below(bound[i][0])) |
