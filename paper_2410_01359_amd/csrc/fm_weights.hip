@@ -13,8 +13,12 @@
 
 namespace fm {
 
-// What is added to a row's score: -lse in the log2 domain.  A row that sees nothing (lse = -inf) gives nothing.
-__device__ __forceinline__ float minus_lse(float lse) { return lse == -INFINITY ? -INFINITY : -lse * kLog2e; }
+// What is added to a row's score: -lse in the log2 domain, and -inf for a row that gives nothing (lse = -inf), for no other.  Such a row's scores may be infinite
+// or NaN, which the sum alone does not take away: it goes the way of rows that do not see a key.
+__device__ __forceinline__ float minus_lse(float lse) {
+  const float x = -lse * kLog2e;
+  return lse == -INFINITY ? -INFINITY : x < -3.0e38f ? -3.0e38f : x;
+}
 
 // --- a prompt --------------------------------------------------------------------------------------------------
 // A workgroup has 256 keys of a K/V head, a wave 64 of them, whose fragments stay in registers (B operands of 32x32x16 products); 64 query rows at
@@ -236,7 +240,9 @@ __global__ __launch_bounds__(256, 2) void weights_kernel(FmWeightsArgs a) {
       if (left > 1) async_wait<COPIES>();
       else async_wait<0>();
       barrier_nofence();   // the tile is there, and the one before has been read
-      lses[lane] = minus_lse(lses[lane]);
+      const float mine = minus_lse(lses[lane]);
+      lses[lane] = mine;
+      const unsigned long long silent = __ballot(mine == -INFINITY);
       const int row = panel_row + (ahead[0] & 0xffff) * kTile, cls = ahead[0] >> (16 + 2 * wave) & 3;
       ahead[0] = ahead[1];
       if (left > 2) {
@@ -253,7 +259,7 @@ __global__ __launch_bounds__(256, 2) void weights_kernel(FmWeightsArgs a) {
       }
       if (waiting) scores(with_old, 0, rows, upper, lower, waiting);
       else scores(alone, 0, rows, upper, upper, lses);
-      if (cls == T_UNMASKED && row + kTile <= a.N) {
+      if (cls == T_UNMASKED && row + kTile <= a.N && !silent) {
         scores(with_old, 1, rows, lower, upper, lses);
         waiting = lses + 32;
         continue;
@@ -265,7 +271,7 @@ __global__ __launch_bounds__(256, 2) void weights_kernel(FmWeightsArgs a) {
       for (int n = 0; n < 2; ++n) {
         const auto below = [&](int i) { return i - row >= 64 ? ~0ull : i <= row ? 0ull : (1ull << (i - row)) - 1; };
         const unsigned long long x =
-            (below(bound[n][1]) & ~below(bound[n][0])) | (below(bound[n][3]) & ~below(bound[n][2])) | ~below(a.N);
+            (below(bound[n][1]) & ~below(bound[n][0])) | (below(bound[n][3]) & ~below(bound[n][2])) | ~below(a.N) | silent;
         hidden[0][n] = (unsigned)x >> 4 * half;
         hidden[1][n] = (unsigned)(x >> 32) >> 4 * half;
       }
@@ -373,20 +379,26 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache_weights_kernel(FmCacheWe
     return (const char*)a.q + 2 * ((long long)b * a.sq.b + (long long)(hk * G + hq) * a.sq.h + (long long)(r - hq * a.T) * a.sq.n);
   };
   const auto lse_of = [&](int r) { return r < R ? minus_lse(a.lse[((size_t)b * a.H + hk * G) * a.T + r]) : -INFINITY; };   // [b, head, t] is contiguous
-  u32x4 q[STEPS];
-  f32x4 lse;
-  if constexpr (ONE) {
-    const char* p = query(min(c, R - 1));
-#pragma unroll
-    for (int s = 0; s < STEPS; ++s) q[s] = ldg16(p + 2 * (E4M3 ? 64 * (s / 2) + 16 * g + 8 * (s % 2) : 32 * s + 8 * g));
-#pragma unroll
-    for (int r = 0; r < 4; ++r) lse[r] = lse_of(4 * g + r);
-  }
   // Which of the T a row is; of one past the last, what the last one is.
   const auto token_of = [&](int r) {
     const int at = min(r, R - 1);
     return at - fm_div(at, a.tokens) * a.T;
   };
+  u32x4 q[STEPS];
+  f32x4 lse;
+  int silent = 0;   // some of the rows at hand have lse = -inf (known to be the same in all lanes)
+  if constexpr (ONE) {
+    const char* p = query(min(c, R - 1));
+    bool some = false;
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s) q[s] = ldg16(p + 2 * (E4M3 ? 64 * (s / 2) + 16 * g + 8 * (s % 2) : 32 * s + 8 * g));
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      lse[r] = lse_of(4 * g + r);
+      some |= 4 * g + r < R && lse[r] == -INFINITY;
+    }
+    silent = __builtin_amdgcn_readfirstlane(__any(some));
+  }
 
   const char* k_head = a.k.base + (long long)hk * a.k.head;
   u32x4 kraw[kGroups][LOADS];
@@ -424,6 +436,11 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache_weights_kernel(FmCacheWe
         sh.token[threadIdx.x] = (unsigned char)token_of(row0 + threadIdx.x);
       }
       __syncthreads();
+      const f32x4 four = *(const f32x4*)&sh.lse[4 * lane];
+      bool some = false;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) some |= 4 * lane + r < min(R - row0, kRows) && four[r] == -INFINITY;
+      silent = __builtin_amdgcn_readfirstlane(__any(some));
     }
     for (int panel = begin; panel < end; panel += kSteps * kStep) {
       const int panel_end = min(end, panel + kSteps * kStep), steps = (panel_end - panel + kStep - 1) / kStep;
@@ -461,7 +478,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache_weights_kernel(FmCacheWe
       while (left) {
         const int start = panel + step * kStep, j = start + lane;
         const unsigned pages = there;
-        const bool masked = (partly >> step & 1) || pages != (1u << kGroups) - 1u;
+        const bool masked = (partly >> step & 1) || pages != (1u << kGroups) - 1u || silent;
         u32x4 keys[kGroups][STEPS];
 #pragma unroll
         for (int i = 0; i < kGroups; ++i)
@@ -495,7 +512,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache_weights_kernel(FmCacheWe
             f32x4 x;
 #pragma unroll
             for (int r = 0; r < 4; ++r) x[r] = fmaf(score[i][r], scale, lse[r]);
-            mask(x, i, token);
+            mask(x, i, token, lse);
 #pragma unroll
             for (int r = 0; r < 4; ++r) x[r] = fast_exp2(x[r]);
             sum[i] += (x[0] + x[1]) + (x[2] + x[3]);
@@ -510,7 +527,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache_weights_kernel(FmCacheWe
 #pragma unroll
               for (int s = 0; s < STEPS; ++s) rows[s] = *(const u32x4*)(sh.q + L::off(c, 16 * g) + n * 16 * L::RS + s * 1024);
               const unsigned token = *(const unsigned*)&sh.token[n * 16 + 4 * g];
-              block(rows, *(const f32x4*)&sh.lse[n * 16 + 4 * g], {(int)(token & 255), (int)(token >> 8 & 255), (int)(token >> 16 & 255), (int)(token >> 24)}, mask);
+              const f32x4 lse = *(const f32x4*)&sh.lse[n * 16 + 4 * g];   // a copy: what is read in place is read again behind every settle
+              block(rows, lse, {(int)(token & 255), (int)(token >> 8 & 255), (int)(token >> 16 & 255), (int)(token >> 24)}, mask);
             }
           }
         };
@@ -526,40 +544,40 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache_weights_kernel(FmCacheWe
             behind[i] = real ? rows_end(at) : 0;
           }
           if (ONE || a.T <= 64) {
-            // The tokens that do not see a key are bits, one extracted for each element.  (With comparisons at every element 16 rows of
-            // a masked step take 320 instructions instead of 150, the last rows of four prompts 29 us instead of 20.)
-            unsigned hidden[kGroups][2];
+            // The tokens that see a key are bits, one extracted for each element, of a row with lse = -inf none.  (With comparisons at every element 16
+            // rows of a masked step take 320 instructions instead of 150, the last rows of four prompts 29 us instead of 20.)
+            unsigned seen[kGroups][2];
 #pragma unroll
             for (int i = 0; i < kGroups; ++i) {
               const auto below = [&](int row) {
                 const int n = min(max(row, 0), len) - first_row;   // T at most: no row is behind the sequence
                 return n >= 64 ? ~0ull : n <= 0 ? 0ull : (1ull << n) - 1;
               };
-              const unsigned long long x = ~below(behind[i]) | below(key[i]) | (below(bound[i][1]) & ~below(bound[i][0])) |
-                                           (below(bound[i][3]) & ~below(bound[i][2]));
-              hidden[i][0] = (unsigned)x;
-              hidden[i][1] = (unsigned)(x >> 32);
+              const unsigned long long x = below(behind[i]) & ~(below(key[i]) | (below(bound[i][1]) & ~below(bound[i][0])) |
+                                                                (below(bound[i][3]) & ~below(bound[i][2])));
+              seen[i][0] = (unsigned)x;
+              seen[i][1] = (unsigned)(x >> 32);
             }
-            all_blocks([&](f32x4& x, int i, const int (&token)[4]) {
+            all_blocks([&](f32x4& x, int i, const int (&token)[4], const f32x4& lse) {
 #pragma unroll
               for (int r = 0; r < 4; ++r) {
-                int hide = __builtin_amdgcn_sbfe(ONE || token[r] < 32 ? hidden[i][0] : hidden[i][1], token[r] & 31, 1);
-                settle(hide);   // no comparison
-                x[r] = __int_as_float((__float_as_int(x[r]) & ~hide) | (hide & 0xff800000));
+                int sees = __builtin_amdgcn_sbfe(ONE || token[r] < 32 ? seen[i][0] : seen[i][1], token[r] & 31, lse[r] == -INFINITY ? 0 : 1);
+                settle(sees);   // no comparison
+                x[r] = __int_as_float((__float_as_int(x[r]) & sees) | (~sees & 0xff800000));
               }
             });
           } else if constexpr (!ONE) {
-            all_blocks([&](f32x4& x, int i, const int (&token)[4]) {
+            all_blocks([&](f32x4& x, int i, const int (&token)[4], const f32x4& lse) {
 #pragma unroll
               for (int r = 0; r < 4; ++r) {
-                const int row = first_row + token[r];
+                const int row = lse[r] == -INFINITY ? -1 : first_row + token[r];
                 const bool gone = (row < key[i]) | (row >= behind[i]) | ((bound[i][0] <= row) & (row < bound[i][1])) | ((bound[i][2] <= row) & (row < bound[i][3]));
                 x[r] = gone ? -INFINITY : x[r];
               }
             });
           }
         } else {
-          all_blocks([](f32x4&, int, const int (&)[4]) {});
+          all_blocks([](f32x4&, int, const int (&)[4], const f32x4&) {});
         }
         float mine = 0.f;
 #pragma unroll
