@@ -380,7 +380,7 @@ __global__ __launch_bounds__(kThreads, 2) void tree_kernel(FmTreeArgs a, FmDivis
       }
       if (!idle) compute(with_mask, buffer, turn, start, now, [] {});
       buffer ^= 1;
-      turn = turn == 2 ? 0 : turn + 1;
+      if (MASKED) turn = turn == 2 ? 0 : turn + 1;   // of masked tiles alone, so that each clears what the one before has noted
       if (more) store(buffer);
       barrier_nofence();
       if (!more) break;
