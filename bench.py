@@ -15,6 +15,7 @@ import ctypes
 import json
 import math
 import os
+import re
 import sys
 import time
 
@@ -125,20 +126,32 @@ def run_workload(name, steps, warmup, torch, fm, orc, workloads, hip, with_event
     return res
 
 
-# Sources of kernels that no workload here launches: the measurement kernels and the operators around the attention call.
-NOT_TIMED = ("fm_probe.hip", "fm_rope.hip", "fm_decode.hip", "fm_pages.hip", "fm_serving_api.hip", "fm_serving.h", "fm_cache_index.h")
+CSRC = os.path.join(ROOT, "paper_2410_01359_amd", "csrc")
+# What the workloads here launch, and what launches it.
+TIMED = ("fm_preprocess.hip", "fm_fwd.hip", "fm_bwd.hip")
+TIMED_FROM = ("fm_api.hip",)
 
 
-def kernels_digest():
+def timed_sources(csrc=CSRC):
+    """Names of the timed kernels' sources: their files, all headers of the folder that those include, and the calls'."""
+    names, todo = set(TIMED_FROM), list(TIMED)
+    while todo:
+        name = todo.pop()
+        if name not in names:
+            names.add(name)
+            text = open(os.path.join(csrc, name)).read()
+            todo += re.findall(r'^\s*#\s*include\s+"([^"/]+)"', text, re.M)
+    return sorted(names)
+
+
+def kernels_digest(csrc=CSRC):
     """Digest of the timed kernels' HIP sources: recorded with the counter-derived traffic figures, which are only
     reported while the kernels they were measured on are the ones being timed."""
     import hashlib
     h = hashlib.sha256()
-    csrc = os.path.join(ROOT, "paper_2410_01359_amd", "csrc")
-    for name in sorted(os.listdir(csrc)):
-        if name.endswith((".hip", ".h")) and name not in NOT_TIMED:
-            h.update(name.encode())
-            h.update(open(os.path.join(csrc, name), "rb").read())
+    for name in timed_sources(csrc):
+        h.update(name.encode())
+        h.update(open(os.path.join(csrc, name), "rb").read())
     return h.hexdigest()[:16]
 
 
