@@ -82,6 +82,19 @@ FM_HOST_DEVICE inline long long fm_whole_keys(int round, long long workgroups, i
   if (keys > 1024) keys = 1024;
   return keys > (long long)least * FM_KEY_GROUP ? keys : (long long)least * FM_KEY_GROUP;
 }
+// Which of two joins a call on trees takes behind its chunks: true: a few lanes to a row, all of a sequence's chunks one behind the other
+// (tree_join_kernel); false: a workgroup to a row, chunks side by side (join_kernel).  rows: of all heads; chunks: that all sequences are meant to be cut into;
+// keys: of a row of the table.  The first takes as long as the longest sequence has chunks, 0.15 us each; the other 0.35 us for every 1000
+// rows of all sequences.  The longest is taken to have four times its share.  us, join_kernel / tree_join_kernel, d = 128: 16 sequences of up to
+// 8192 keys, 2016 rows, 32 chunks 16.2/6.2, 128 rows, 256 chunks 5.1/11.0; one, 2016 rows 7.8/9.4, 512 rows, 64 chunks 4.9/15.6, 8064 rows, 8 chunks
+// 10.0/7.3; four of 2000, 2016 rows, 32 chunks 10.2/6.8; 64 of up to 1500, 2016 rows, 64 chunks 44/10, 128 rows, 256 chunks 7.2/4.6.
+FM_HOST_DEVICE inline bool fm_tree_joins_by_lanes(long long rows, int sequences, int chunks, int least, long long keys) {
+  long long longest = (4ll * chunks + sequences - 1) / sequences;
+  if (longest > chunks) longest = chunks;
+  const long long most = (keys + least * FM_KEY_GROUP - 1) / (least * FM_KEY_GROUP);
+  if (longest > most) longest = most;
+  return rows * sequences >= 200 * longest;
+}
 // Split sequences at most: each has two partial results at least.  Units of a launch: those above, in whole rounds of the XCDs.
 FM_HOST_DEVICE inline int fm_most_splits(int chunks, int sequences) { return chunks < sequences ? chunks : sequences; }
 FM_HOST_DEVICE inline int fm_listed_units(int chunks, int sequences) { return (fm_most_units(chunks, sequences) + 7) / 8 * 8; }

@@ -515,8 +515,7 @@ __global__ __launch_bounds__(kThreads, 2) void tree_kernel(FmTreeArgs a, FmDivis
   }
 }
 
-// Joins the chunks of split sequences where they are few and rows many: D / 4 lanes to a row, four chunks at a time.  (join_kernel, which has a workgroup for
-// every row, took 22 us where this took 9, at 16 trees of 63 tokens, 32 heads and up to 42 chunks to a sequence.)
+// Joins the chunks of split sequences where they are few and rows many (fm_tree_joins_by_lanes): D / 4 lanes to a row, four chunks at a time.
 template <int D, bool F16>
 __global__ __launch_bounds__(kThreads) void tree_join_kernel(FmTreeArgs a, FmDivisor rows, FmDivisor tokens) {
   constexpr int LANES = D / 4, BATCH = 4;
@@ -568,7 +567,7 @@ static void launch(FmTreeArgs a, hipStream_t stream) {
   for (a.first_workgroup = 0; a.first_workgroup < workgroups; a.first_workgroup += kMost)
     hipLaunchKernelGGL((tree_kernel<D, F16, E4M3>), dim3((unsigned)std::min(workgroups - a.first_workgroup, kMost)), dim3(kThreads), 0, stream, a,
                        fm_divisor(cut.workgroups), fm_divisor(cut.row_blocks), fm_divisor(a.T), fm_divisor(cut.chunks));
-  if (a.plan && cut.chunks <= 32 && !a.split) {
+  if (a.plan && !a.split && fm_tree_joins_by_lanes((long long)a.H * a.T, a.B, cut.chunks, cut.least, (long long)a.columns * a.page_tokens)) {
     const int R = a.H / a.Hk * a.T, each = kThreads / (D / 4);
     hipLaunchKernelGGL((tree_join_kernel<D, F16>), dim3((a.Hk * R + each - 1) / each, a.B), dim3(kThreads), 0, stream, a, fm_divisor(R), fm_divisor(a.T));
   } else if (a.plan) {
