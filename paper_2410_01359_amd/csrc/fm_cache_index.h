@@ -82,6 +82,15 @@ FM_HOST_DEVICE inline long long fm_whole_keys(int round, long long workgroups, i
   if (keys > 1024) keys = 1024;
   return keys > (long long)least * FM_KEY_GROUP ? keys : (long long)least * FM_KEY_GROUP;
 }
+// Whether trees of T tokens with `rows` query rows to a K/V head go through tree_kernel, which reads keys and values once for 128 rows, or decode_kernel, which has
+// room for 64 tokens.  8-bit values of 128 elements cost the first more to widen than they save until there are more rows.  us, decode_kernel / tree_kernel, at 32, 48,
+// 64, 80, 128 and 252 rows: 16 trees over ragged caches of up to 8192 keys, 8 K/V heads, d = 128, 16 bits 50/49 61/52 64/53 81/56 108/63 159/105, 8 bits
+// 38/51 53/58 56/59 70/62 87/70 132/123, d = 64 36/31 45/38 47/38 60/40 77/43 111/70, 8 bits 32/32 42/39 45/39 57/41 73/45 104/73; one over 8192 19/21 21/24
+// 24/24 26/26 34/32 55/36; 64 over up to 1500 47/51 60/55 64/56 80/59 95/68 127/111, 8 bits 38/58 53/61 57/62 72/65 83/74 103/130.  Over 504 such points calls take
+// 1.4 % more than on the better side of each (from 64 rows on whatever the type: 2.8 %), at most 1.4 times as much: 100 over up to 500 keys, 2 K/V heads, 8 bits
+// 13/26 18/27 19/29 24/29 22/31 36/36.
+FM_HOST_DEVICE constexpr bool fm_tree_is_wide(long long rows, int T, int d, bool e4m3) { return T > 63 || rows >= (e4m3 && d == 128 ? 80 : 48); }
+
 // Which of two joins a call on trees takes behind its chunks: true: a few lanes to a row, all of a sequence's chunks one behind the other
 // (tree_join_kernel); false: a workgroup to a row, chunks side by side (join_kernel).  rows: of all heads; chunks: that all sequences are meant to be cut into;
 // keys: of a row of the table.  The first takes as long as the longest sequence has chunks, 0.15 us each; the other 0.35 us for every 1000

@@ -62,7 +62,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void decode_kernel(Args a, int memb
   constexpr int TW = kWaves / TEAMS;   // waves of a team
   using C = Decode<D, F16, E4M3, NB>;
   __shared__ typename C::Shared sh;
-  __shared__ std::conditional_t<kTree<Args>, SmallTree, char> tree;   // of few rows, so of few tokens
+  __shared__ std::conditional_t<kTree<Args>, SmallTree, char> tree;   // of few tokens (fm_tree_is_wide)
   // Barriers here order LDS alone (barrier_nofence): loads stay in flight across them.
   // The launch arguments that come first, read together: left where they are first needed they are six round trips in a row.
   asm volatile("" ::"s"(a.units), "s"(a.plan), "s"(a.lens), "s"(a.B), "s"(a.T), "s"(a.window), "s"(a.columns), "s"(a.page_tokens), "s"(a.cut.least),
@@ -133,7 +133,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void decode_kernel(Args a, int memb
   int parent = -1;
   bool planted = false;
   if constexpr (kTree<Args>) {
-    static_assert(!fm_tree_is_wide(1, 1, 63) && fm_tree_is_wide(1, 1, 64));
+    static_assert(fm_tree_is_wide(1, 64, D, E4M3));   // SmallTree
     if (lane < a.T) parent = a.parents[(size_t)b * a.T + lane];
   }
   const auto plant_tree = [&] {

@@ -86,11 +86,7 @@ struct FmTreeArgs : FmDecodeArgs {
   const int* parents;     // [B, T]
 };
 hipError_t fm_launch_decode_tree(const FmTreeArgs& a, bool f16, bool e4m3, hipStream_t stream);
-// Many query rows to a K/V head go through a kernel of their own, cut by fm_tree_cut in multiples of FM_TREE_ROUND groups of keys.  decode_kernel / that
-// one, us, 32 heads on 8, at 48, 64, 80, 128 and 252 rows: 16 trees over ragged caches of 8192 keys, d 128, 64/56 66/56 81/59 108/68 157/104, of e4m3
-// 55/62 57/62 71/66 88/76 134/123; one tree 21/24 24/25 26/26 34/35 58/38; 64 over ragged 1500 keys 62/63 67/67 80/71 95/86 127/143, of e4m3 53/69 58/74
-// 72/78 84/94 105/163.  8 heads on 2 at 64: 26/29 25/29 22/18 27/30 26/31.
-constexpr bool fm_tree_is_wide(int H, int Hk, int T) { return H / Hk * T >= 64; }
+// Trees of many query rows to a K/V head (fm_tree_is_wide) go through a kernel of their own, cut by fm_tree_cut in multiples of FM_TREE_ROUND groups of keys.
 constexpr int FM_TREE_ROUND = 4;
 FmDecodeCut fm_tree_cut(int H, int Hk, int T, int d, int B, int cus);
 hipError_t fm_launch_tree_wide(const FmTreeArgs& a, bool f16, bool e4m3, hipStream_t stream);

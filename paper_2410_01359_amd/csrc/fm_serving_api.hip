@@ -101,26 +101,27 @@ size_t decode_bytes(const DecodeCuts& cuts, int sequences, int H, int T, int d) 
   return std::max(decode_space(cuts.of[0], sequences, H, T, d).total, decode_space(cuts.of[1], sequences, H, T, d).total);
 }
 
-// Of a tree's call: that of many query rows to a K/V head has a cut of its own.
-int check_tree_shape(int sequences, int H, int Hk, int T, int d, DecodeCuts& cuts, FmDecodeCut& wide) {
+// Of a tree's call over a cache of 8 or 16 bits: that of many query rows to a K/V head has a cut of its own.
+int check_tree_shape(int sequences, int H, int Hk, int T, int d, bool e4m3, DecodeCuts& cuts, bool& is_wide, FmDecodeCut& wide) {
   if (int rc = check_decode_shape(sequences, H, Hk, T, d, cuts)) return rc;
-  if (!fm_tree_is_wide(H, Hk, T)) return FM_OK;
+  is_wide = fm_tree_is_wide((long long)H / Hk * T, T, d, e4m3);
+  if (!is_wide) return FM_OK;
   wide = fm_tree_cut(H, Hk, T, d, sequences, fm_compute_units());
   return (fm_most_units(wide.chunks, sequences) + 8ll) * wide.workgroups < 1 << 24 ? FM_OK : FM_ERR_SHAPE;
 }
 
-// Checks of a decoding call and its launch arguments.
+// Checks of a decoding call and its launch arguments.  wide: whether a tree's has many query rows to a K/V head.
 int decode_args(bool tree, const flashmask_cache* cache, const void* q, const int32_t* lens, const int32_t* lts, const int32_t* lte, const int32_t* uts,
                 const int32_t* ute, int bound_columns, int window, float scale, void* out, float* lse, int type, int H, int T,
-                const flashmask_strides* strides, void* workspace, size_t workspace_bytes, FmDecodeArgs& a) {
+                const flashmask_strides* strides, void* workspace, size_t workspace_bytes, FmDecodeArgs& a, bool& wide) {
   if (int rc = check_cache(cache)) return rc;
   if (!q || !lens || !out || !lse || !strides) return FM_ERR_NULL;
   const bool bounds = lts || lte || uts || ute;
   if (bounds && (!lts || !lte || !uts || !ute)) return FM_ERR_NULL;
   if (int rc = check_row_type(type, *cache)) return rc;
   DecodeCuts cuts;
-  const bool wide = tree && fm_tree_is_wide(H, cache->heads, T);
-  if (int rc = tree ? check_tree_shape(cache->sequences, H, cache->heads, T, cache->d, cuts, a.cut)
+  wide = false;
+  if (int rc = tree ? check_tree_shape(cache->sequences, H, cache->heads, T, cache->d, cache->type == FM_TYPE_E4M3, cuts, wide, a.cut)
                     : check_decode_shape(cache->sequences, H, cache->heads, T, cache->d, cuts)) return rc;
   if (bounds && bound_columns <= 0) return FM_ERR_SHAPE;
   if ((long long)cache->sequences * cache->columns * cache->page > 1ll << 34) return FM_ERR_SHAPE;   // groups of 16 keys are added up in 32 bits
@@ -238,16 +239,22 @@ int flashmask_decode(const flashmask_cache* cache, const void* q, const int32_t*
                      void* out, float* lse, int type, int H, int T, const flashmask_strides* strides, void* workspace,
                      size_t workspace_bytes, void* hip_stream) {
   FmDecodeArgs a;
+  bool wide;
   if (int rc = decode_args(false, cache, q, lens, lts, lte, uts, ute, bound_columns, window, scale, out, lse, type, H, T, strides, workspace,
-                           workspace_bytes, a)) return rc;
+                           workspace_bytes, a, wide)) return rc;
   return done(fm_launch_decode(a, type == FM_TYPE_F16, cache->type == FM_TYPE_E4M3, (hipStream_t)hip_stream));
 }
 
 size_t flashmask_decode_tree_workspace_bytes(int sequences, int H, int H_kv, int T, int d) {
-  DecodeCuts cuts;
-  FmDecodeCut wide;
-  if (check_tree_shape(sequences, H, H_kv, T, d, cuts, wide) != FM_OK) return 0;
-  return fm_tree_is_wide(H, H_kv, T) ? decode_space(wide, sequences, H, T, d).total : decode_bytes(cuts, sequences, H, T, d);
+  size_t most = 0;   // of whatever cache
+  for (const bool e4m3 : {false, true}) {
+    DecodeCuts cuts;
+    FmDecodeCut cut;
+    bool wide;
+    if (check_tree_shape(sequences, H, H_kv, T, d, e4m3, cuts, wide, cut) != FM_OK) return 0;
+    most = std::max(most, wide ? decode_space(cut, sequences, H, T, d).total : decode_bytes(cuts, sequences, H, T, d));
+  }
+  return most;
 }
 
 int flashmask_decode_tree(const flashmask_cache* cache, const void* q, const int32_t* lens, const int32_t* parents, const int32_t* lts,
@@ -256,10 +263,11 @@ int flashmask_decode_tree(const flashmask_cache* cache, const void* q, const int
                           size_t workspace_bytes, void* hip_stream) {
   if (!parents) return FM_ERR_NULL;
   FmTreeArgs a;
+  bool wide;
   if (int rc = decode_args(true, cache, q, lens, lts, lte, uts, ute, bound_columns, window, scale, out, lse, type, H, T, strides, workspace,
-                           workspace_bytes, a)) return rc;
+                           workspace_bytes, a, wide)) return rc;
   a.parents = parents;
-  return done((fm_tree_is_wide(H, cache->heads, T) ? fm_launch_tree_wide : fm_launch_decode_tree)(a, type == FM_TYPE_F16, cache->type == FM_TYPE_E4M3, (hipStream_t)hip_stream));
+  return done((wide ? fm_launch_tree_wide : fm_launch_decode_tree)(a, type == FM_TYPE_F16, cache->type == FM_TYPE_E4M3, (hipStream_t)hip_stream));
 }
 
 size_t flashmask_weights_workspace_bytes(int B, int H, int H_kv, int N, int d, int first_row) {
