@@ -417,7 +417,7 @@ size_t flashmask_decode_workspace_bytes(int sequences, int H, int H_kv, int T, i
  *   parents     int32 [sequences, T]
  *   workspace   at least flashmask_decode_tree_workspace_bytes(), 256-byte aligned
  * All else is as for flashmask_decode, its limits and guarantees among it.  (New tokens are written to places that are not their positions by
- * flashmask_rope and flashmask_cache_append without freqs.)
+ * flashmask_rope and flashmask_cache_append without freqs; keys of an E4M3 cache are then rounded twice, to `type` and to 8 bits.)
  */
 int flashmask_decode_tree(const flashmask_cache* cache, const void* q, const int32_t* lens, const int32_t* parents, const int32_t* lts,
                           const int32_t* lte, const int32_t* uts, const int32_t* ute, int bound_columns, int window, float scale,
@@ -484,6 +484,12 @@ int flashmask_cache_weights(const flashmask_cache* cache, const void* q, const i
  *   kept        int32 [sequences, weight_heads, keep]: the places that the tokens come from, -1 behind the last
  *   workspace   at least flashmask_cache_evict_workspace_bytes(), 256-byte aligned
  * A kept token whose old place has no page becomes zeros.  Outputs overlap nothing else.  At most 65535 sequences.
+ * From then on a token's place is not its position, and what the calls over the cache count, they count by place: the row of the last tokens is lens_out[b] - T + t,
+ * a window of w reaches over the last w tokens that are left, however far back they were, and a key's bounds are those at its new place, of rows counted so.
+ * Where all heads keep the same tokens, bounds of the kept keys are gathered by `kept`, their ends turned into the new count of rows; with a selection for each
+ * head a place has other tokens in every head, and one vector of bounds to a sequence cannot tell them apart: such sequences have none.
+ * New tokens are rotated to their position and written to their place by flashmask_rope and flashmask_cache_append without freqs, where keys of an E4M3
+ * cache are rounded twice, to `type` and to 8 bits.
  */
 int flashmask_cache_evict(const flashmask_cache* cache, const int32_t* lens, const float* weights, int weight_heads, int weight_columns,
                           int keep, int first, int recent, const int32_t* new_table, int new_columns, int32_t* table_out, int32_t* lens_out,

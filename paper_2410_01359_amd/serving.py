@@ -349,7 +349,8 @@ def flashmask_cache_evict(k_cache, v_cache, table, lens, weights, new_table, kee
     """Sequences of more than `keep` tokens keep their `first` first, their `recent` last and the heaviest of the tokens between, in their order, in
     the pages new_table[b] (int32 [sequences, at least keep / page]).  weights fp32 [sequences, H_kv or 1, places]: a selection for each K/V head or
     one for all; equally heavy tokens: the first ones stay.  Returns table, lens, weights (of the tokens in their new places, 0 behind
-    them) and the places that they come from (int32 [sequences, H_kv or 1, keep], -1 behind the last)."""
+    them) and the places that they come from (int32 [sequences, H_kv or 1, keep], -1 behind the last).  From then on places are not positions: the
+    calls over the cache count rows, windows and bounds by place, and where each head keeps tokens of its own no bounds describe a sequence."""
     device, ints, f32 = k_cache.get_device(), torch.int32, torch.float32
     cache, heads, d, B = _cache(k_cache, v_cache, table, k_scale, v_scale, device)
     which, columns = weights.shape[1:] if weights.dim() == 3 else (heads, 0)
