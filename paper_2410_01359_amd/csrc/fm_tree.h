@@ -17,7 +17,8 @@ using Tree = TreeOf<FM_MOST_NEW_TOKENS>;
 using SmallTree = TreeOf<64>;
 
 // Of up to 64 tokens, by a wave for itself: lane t has token t's parent.  Lines double their reach in each turn.  Waves that share the tree write the same,
-// so that none waits for another (8 trees of 60 tokens over ragged caches of 3000, 8 heads of 64: 25.5 us by all waves together ahead of everything, 21.1).
+// so that none waits for another (8 trees of 60 tokens over ragged caches of 3000, 8 heads of 64, by decode_kernel: 25.5 us by all waves together ahead of
+// everything, 21.1 so).
 __device__ __forceinline__ void plant_small(SmallTree& tree, int parent, int T) {
   const int lane = threadIdx.x & 63;
   int ahead = lane < T && parent >= 0 && parent < lane ? parent : -1;   // the first of the line that is not among the bits

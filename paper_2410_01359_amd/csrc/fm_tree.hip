@@ -5,7 +5,7 @@
 //     S^T = K Q^T (a lane has 16 keys of each half of the tile, of one query), O^T += V^T P^T (V^T by transpose reads),
 // softmax statistics are per lane, a lane's probabilities are the second product's operand as they are, and enter it as sums of two 16-bit values
 // (see split2).  Tiles without a masked pair take a short way.
-// 16 trees of 63 tokens, 32 heads on 8 of 128, ragged caches of up to 8192 tokens (208 MB): 102 us and the join, of which power takes a part (the clock falls
+// 16 trees of 63 tokens, 32 heads on 8 of 128, ragged caches of up to 8192 tokens (208 MB): 101 us and the join, of which power takes a part (the clock falls
 // to 1.6 - 1.8 GHz).  256 rows to a workgroup of eight waves, half of them at the scores while the others are at the products with the values: the same.
 #include <algorithm>
 

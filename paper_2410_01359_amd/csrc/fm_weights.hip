@@ -313,7 +313,8 @@ __global__ __launch_bounds__(256) void join_weights_kernel(const float* __restri
 // so that a lane's results are four rows of its keys.  A wave has the next step's keys in flight.  Of up to 16 rows to a K/V head the
 // operand stays in registers and reading the keys is what takes the time; of more, 256 at a time lie in LDS.
 // Chunks of keys are dealt as in attention over the cache: all sequences' keys in as many pieces as the chip has places, each sequence in whole ones.
-// 64 ragged sequences of up to 8192 keys of 128 elements, one new token: 82 us, 4.6 TB/s; 32 new tokens of four sequences, 256 rows to a K/V head, 8 bits: 19 us.
+// 64 ragged sequences of up to 8192 keys of 128 elements, one new token: 82 us, 4.6 TB/s, of 8 bits 40 us, 4.8; of 64 elements 36 us, 5.3, and 26 us, 3.9 (4 KiB
+// of a wave in flight); 32 new tokens of four sequences, 256 rows to a K/V head, 8 bits: 20 us.
 // With bounds every lane first works out for its own key how many of the T rows see it: steps that none sees are not read, and only steps with keys that
 // some rows do not see take the element mask.
 constexpr int kStep = 64, kGroups = kStep / FM_KEY_GROUP, kWaves = 4, kSteps = 64, kRows = 256;   // kSteps: of a panel, whose flags lie together
