@@ -483,7 +483,7 @@ int flashmask_cache_weights(const flashmask_cache* cache, const void* q, const i
  *   weights_out as weights: those of the tokens in their new places, 0 behind them
  *   kept        int32 [sequences, weight_heads, keep]: the places that the tokens come from, -1 behind the last
  *   workspace   at least flashmask_cache_evict_workspace_bytes(), 256-byte aligned
- * A kept token whose old place has no page becomes zeros.  Outputs overlap nothing else.  At most 65535 sequences.
+ * A kept token whose old place has no page becomes zeros.  Outputs overlap nothing else.  At most 65535 sequences, keep at most 2^30 - 64.
  * From then on a token's place is not its position, and what the calls over the cache count, they count by place: the row of the last tokens is lens_out[b] - T + t,
  * a window of w reaches over the last w tokens that are left, however far back they were, and a key's bounds are those at its new place, of rows counted so.
  * Where all heads keep the same tokens, bounds of the kept keys are gathered by `kept`, their ends turned into the new count of rows; with a selection for each

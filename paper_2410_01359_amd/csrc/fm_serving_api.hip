@@ -342,7 +342,7 @@ int flashmask_cache_evict(const flashmask_cache* cache, const int32_t* lens, con
   if (int rc = check_cache(cache)) return rc;
   if (!lens || !weights || !new_table || !table_out || !lens_out || !weights_out || !kept) return FM_ERR_NULL;
   if (weight_columns <= 0 || weight_columns > (1 << 30) || (weight_heads != 1 && weight_heads != cache->heads) || cache->sequences > 65535 ||
-      keep <= 0 || keep > (1 << 30) || first < 0 || recent < 0 || (long long)first + recent > keep || new_columns <= 0)
+      keep <= 0 || keep > (1 << 30) - 64 || first < 0 || recent < 0 || (long long)first + recent > keep || new_columns <= 0)
     return FM_ERR_SHAPE;
   const int pages_kept = (keep + cache->page - 1) / cache->page;
   if (new_columns < pages_kept || cache->columns < pages_kept) return FM_ERR_SHAPE;
